@@ -401,6 +401,134 @@ int sim_update(sim_ctx* ctx, const sim_update_cfg* cfg, void* d_weights, float* 
                const uint8_t* d_actions, const float* d_logp_old, const double* d_adv,
                const double* d_ret, double* d_losses);
 
+/* Operators for policies that the caller's own network computes (a sequence model, a router, an
+ * action set of any size): the recurrence, the policy loss and a router's balance loss, each
+ * with its gradient. They use a context for its stream, its device and its error flags only,
+ * whatever its configuration; the sizes are their own. Common to them:
+ *   - Work memory is the caller's: the *_work calls (no device work) give the bytes, 16-byte
+ *     aligned memory; nothing need be in it, and calls that may overlap (two streams, two
+ *     graphs) take one each. They allocate nothing and may be captured into a graph (with
+ *     sim_set_timing off); the current device may be another than the context's.
+ *   - Values are fp64, fp32, bf16 or fp16 (SIM_DT_*), computed in fp32 (fp64 for fp64) and
+ *     rounded once, to nearest, on output.
+ *   - Strides are in elements. An input may be broadcast by a stride of 0; the elements of an
+ *     output must not share memory (SIM_EINVAL). Outputs may not overlap inputs but where
+ *     stated. Every array must be aligned to its element. Sizes of 0 are allowed.
+ *   - Sums run in a fixed order: repeated calls return the same bits.                      */
+enum { SIM_DT_F64 = 0, SIM_DT_F32 = 1, SIM_DT_BF16 = 2, SIM_DT_F16 = 3 };
+enum { SIM_IT_U8 = 0, SIM_IT_I32 = 1, SIM_IT_I64 = 2 };
+enum { SIM_GATE_LINEAR = 0, SIM_GATE_SIGMOID = 1 };
+
+/* An array over sequences, steps and channels: element (b, t, d) at b*stride_b + t*stride_t + d. */
+typedef struct sim_seq {
+  void* data;
+  int64_t stride_b, stride_t;
+} sim_seq;
+
+/* A matrix over samples and actions: element (n, a) at n*stride_n + a*stride_a. Of logits and
+ * their gradient one of the two strides is 1 (rows of actions, or sim_policy's [A][E] logits),
+ * unless a dimension is 1.                                                               */
+typedef struct sim_mat {
+  void* data;
+  int64_t stride_n, stride_a;
+} sim_mat;
+
+/* Gated linear recurrence: the recurrence of returns_gae with a gate per step and channel
+ * (episodes that end inside a rollout, per-token discounts; Sec. 4.3) and the state of a
+ * recurrent policy.
+ *  dtype      type of the arrays over steps; states are fp64 for SIM_DT_F64 and fp32 otherwise
+ *  kind       SIM_GATE_LINEAR:  h = gate_t h + x_t
+ *             SIM_GATE_SIGMOID: f = 1 / (1 + exp(-gate_t)), h = f h + (1 - f) x_t
+ *  reverse    0: t = 0, 1, ..; 1: from the last step back to t = 0
+ *  B, T, D    sequences, steps, channels                                                 */
+typedef struct sim_scan {
+  int32_t dtype, kind, reverse;
+  int64_t B, T, D;
+} sim_scan;
+
+/* y_t = the state after step t, from the state d_h0 [B][D] (NULL: 0); d_state [B][D] (NULL: not
+ * wanted) receives the state after the last step and may be d_h0 itself (serving: T = 1, the
+ * state updated in place). y may be NULL (only the state is wanted). d_len [B] int32 (NULL: all
+ * T): steps t >= d_len[b] are padding, whatever they hold: they leave the state as it is and
+ * their y is 0; a length outside [0, T] latches SIM_ESTATE and is taken as the nearer bound.
+ * Long sequences of few channels are split over time, so results differ from a step-by-step
+ * sum by rounding; the products of the gates over any run of steps must then be finite in the
+ * state's type (always so for |gate| <= 1).                                              */
+int gated_scan_work(const sim_scan* s, size_t* bytes);
+int gated_scan(sim_ctx* ctx, const sim_scan* s, const sim_seq* gate, const sim_seq* x,
+               const int32_t* d_len, const void* d_h0, const sim_seq* y, void* d_state,
+               void* d_work, size_t work_bytes);
+
+/* Its gradient: from dy and d_dstate [B][D] (gradient of the last state, NULL: 0) the gradients
+ * of gate, x and h0 (dgate, dx, d_dh0; each may be NULL). In the opposite order of steps, with
+ * C = dstate at first and h' the state before a step (y of the step before it as stored, or h0):
+ *   G_t = dy_t + C;  linear:  dx_t = G_t,          dgate_t = G_t h',                 C = gate_t G_t
+ *                    sigmoid: dx_t = (1 - f) G_t,  dgate_t = G_t (h' - x_t) f (1 - f),  C = f G_t
+ * and dh0 = C at the end. Padding gets 0. x is read for SIM_GATE_SIGMOID only, y only if dgate
+ * is wanted (either may be NULL otherwise). The gradient of a broadcast input is the sum over
+ * the dimension it is broadcast along of what is written here, which is left to the caller. */
+int gated_scan_grad_work(const sim_scan* s, size_t* bytes);
+int gated_scan_grad(sim_ctx* ctx, const sim_scan* s, const sim_seq* gate, const sim_seq* x,
+                    const sim_seq* y, const sim_seq* dy, const int32_t* d_len, const void* d_h0,
+                    const void* d_dstate, const sim_seq* dgate, const sim_seq* dx, void* d_dh0,
+                    void* d_work, size_t work_bytes);
+
+/* Clipped policy loss with a KL term over logits of any network, and its gradient: the
+ * surrogate of ppo_minibatch_grad (Sec. 4.3) without its network.
+ *  N, A         samples (below 2^31) and actions
+ *  dtype        of logits and gradient (not SIM_DT_F64)
+ *  action_type  SIM_IT_*;  adv_type  SIM_DT_F32 or SIM_DT_F64 (as returns_gae writes them)
+ *  clip         in (0, 1); c_kl, c_entropy >= 0                                          */
+typedef struct sim_policy_loss {
+  int64_t N;
+  int32_t A, dtype, action_type, adv_type;
+  float clip, c_kl, c_entropy;
+} sim_policy_loss;
+
+/* With p the softmax of a sample's logits over its allowed actions, logp that of the taken
+ * action, rho = exp(logp - logp_old), d = logp_ref - logp and H the entropy of p:
+ *   L = sum_n w_n (-min(rho adv, clip(rho, 1-clip, 1+clip) adv) + c_kl (e^d - d - 1) - c_entropy H)
+ * (e^d - d - 1: an estimate of KL(p || reference) at the taken action, never negative).
+ * mask [N][A] bytes (NULL: all allowed; any strides, stride_n = 0 to share a row): 0 forbids
+ * an action, whatever its logit holds, and so does a logit of -inf. d_weight [N] (NULL:
+ * 1/N each): samples of weight 0 are not looked at. d_logp_old NULL: logp itself (the first step
+ * after a rollout: rho = 1). d_logp_ref may be NULL if c_kl = 0. Outputs: grad dL/dlogits (may be
+ * NULL, or the logits themselves: same pointer and strides), d_logp [N] (may be NULL), d_loss [4]
+ * fp32: L and its policy, KL and entropy terms (sums of w times each, without the c's; summed in
+ * fp64). A sample of weight 0, or with no allowed action, gives nothing: gradient 0, logp 0. So
+ * does one whose action is out of range or forbidden, which also latches SIM_ESTATE.       */
+int policy_loss_work(const sim_policy_loss* c, size_t* bytes);
+int policy_loss(sim_ctx* ctx, const sim_policy_loss* c, const sim_mat* logits, const sim_mat* mask,
+                const void* d_actions, const float* d_weight, const float* d_logp_old,
+                const float* d_logp_ref, const void* d_adv, const sim_mat* grad, float* d_logp,
+                float* d_loss, void* d_work, size_t work_bytes);
+
+/* Balance loss of a router (a policy that sends each request to one of several servers, Sec. 4.1,
+ * or each token to k of A experts), its counts and its gradient.
+ *  N, A, k      rows (below 2^31), columns, choices per row (N k below 2^31)
+ *  group        consecutive columns that count as one target: 1, or 6 for this simulator's
+ *               actions (server a/6); divides A, A/group <= 4096
+ *  dtype        of logits and gradient (not SIM_DT_F64);  index_type  SIM_IT_*
+ *  coef         the loss's factor                                                        */
+typedef struct sim_balance {
+  int64_t N;
+  int32_t A, k, group, dtype, index_type;
+  float coef;
+} sim_balance;
+
+/* With W live rows (d_live [N] bytes, NULL: all), G = A/group targets, p the softmax of a row's
+ * logits: f_g = counts_g / (k W), P_g the mean over live rows of p summed over g's columns,
+ *   L = coef G sum_g f_g P_g,   dL/dlogit_nj = coef G / W p_nj (f_g(j) - sum_i f_g(i) p_ni)
+ * (f held constant). d_index [N][k]: the chosen columns; -1 (not with SIM_IT_U8) is no choice, any
+ * other value outside [0, A) latches SIM_ESTATE and counts for nothing. Outputs: d_counts
+ * [G] int64, the live rows' choices; d_loss [1] fp32 (summed in fp64); grad (may be NULL, or the
+ * logits themselves). Rows that are not live, or whose logits are all -inf, add nothing to P
+ * and have gradient 0; W = 0 gives L = 0.                                                  */
+int balance_loss_work(const sim_balance* c, size_t* bytes);
+int balance_loss(sim_ctx* ctx, const sim_balance* c, const sim_mat* logits, const void* d_index,
+                 const uint8_t* d_live, const sim_mat* grad, int64_t* d_counts, float* d_loss,
+                 void* d_work, size_t work_bytes);
+
 /* Per-environment counters [2][SIM_NCNT][E] int64 and sums [2][SIM_NSUM][E] fp64 into
  * device buffers (either may be NULL).                                                  */
 int sim_counters(sim_ctx* ctx, int64_t* d_cnt, double* d_sum);

@@ -24,10 +24,13 @@ SYMBOLS = ("sim_last_error", "sim_abi_version", "sim_create", "sim_destroy", "si
            "ppo_minibatch_grad", "sim_ppo_grad_count", "reinforce_minibatch_grad",
            "sim_params_from_weights", "adam_update", "sim_update", "sim_attn_weights_layout",
            "sim_get_state", "sim_set_state", "sim_device_primitive", "sim_policy_hidden", "sim_set_graphs", "sim_graph_stats",
-           "ppo_minibatch_grad_noalloc", "sim_set_fused_rollout")
+           "ppo_minibatch_grad_noalloc", "sim_set_fused_rollout", "gated_scan_work", "gated_scan",
+           "gated_scan_grad_work", "gated_scan_grad", "policy_loss_work", "policy_loss",
+           "balance_loss_work", "balance_loss")
 ALGO_PPO, ALGO_REINFORCE = 0, 1
 KERNEL_CLASSES = ("policy", "step", "static", "gae", "reset", "other", "ppo", "rollout")
 FUSE_OFF, FUSE_AUTO, FUSE_ON = 0, 1, 2
+GATE_KINDS = {"linear": 0, "sigmoid": 1}
 
 
 class SimCfg(C.Structure):
@@ -77,6 +80,30 @@ class SimUpdateCfg(C.Structure):
                 ("M", C.c_int32), ("seed", C.c_uint64), ("clip", C.c_float),
                 ("c_value", C.c_float), ("c_entropy", C.c_float), ("lr", C.c_float),
                 ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float)]
+
+
+class SimSeq(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_b", C.c_int64), ("stride_t", C.c_int64)]
+
+
+class SimMat(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_n", C.c_int64), ("stride_a", C.c_int64)]
+
+
+class SimScan(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("kind", C.c_int32), ("reverse", C.c_int32),
+                ("B", C.c_int64), ("T", C.c_int64), ("D", C.c_int64)]
+
+
+class SimPolicyLoss(C.Structure):
+    _fields_ = [("N", C.c_int64), ("A", C.c_int32), ("dtype", C.c_int32),
+                ("action_type", C.c_int32), ("adv_type", C.c_int32), ("clip", C.c_float),
+                ("c_kl", C.c_float), ("c_entropy", C.c_float)]
+
+
+class SimBalance(C.Structure):
+    _fields_ = [("N", C.c_int64), ("A", C.c_int32), ("k", C.c_int32), ("group", C.c_int32),
+                ("dtype", C.c_int32), ("index_type", C.c_int32), ("coef", C.c_float)]
 
 
 class SimTotals(C.Structure):
@@ -129,6 +156,10 @@ def load():
         "sim_attn_weights_layout": [vp, vp],
         "sim_get_state": [vp, vp, vp], "sim_set_state": [vp, vp, C.c_size_t],
         "sim_device_primitive": [i32, C.c_int64, u64, vp, vp, vp],
+        "gated_scan_work": [vp, vp], "gated_scan_grad_work": [vp, vp],
+        "gated_scan": [vp] * 9 + [C.c_size_t], "gated_scan_grad": [vp] * 13 + [C.c_size_t],
+        "policy_loss_work": [vp, vp], "policy_loss": [vp] * 13 + [C.c_size_t],
+        "balance_loss_work": [vp, vp], "balance_loss": [vp] * 9 + [C.c_size_t],
     }
     for name, args in sig.items():
         f = getattr(L, name)

@@ -1,0 +1,38 @@
+// ops_dev.hpp -- element types of the operators' arrays: loads widened to the type they are
+// computed in, stores rounded once to nearest even.
+#pragma once
+#include "devmath.hpp"
+#include "ops.hpp"
+#include "params.hpp"
+
+namespace bsim {
+namespace {
+
+struct F64 { typedef double T; typedef double W; };
+struct F32 { typedef float T; typedef float W; };
+struct BF16 { typedef __bf16 T; typedef float W; };
+struct F16 { typedef _Float16 T; typedef float W; };
+
+// f = 1 / (1 + e^-g) and r = 1 - f, each to its own relative accuracy: with e = e^-|g| the
+// larger of the two is 1 / (1 + e) and the smaller one e times that.
+__device__ __forceinline__ void sigmoid_pair(float g, float& f, float& r) {
+  const float e = __builtin_amdgcn_exp2f(fabsf(g) * -1.4426950408889634f);
+  const float big = __builtin_amdgcn_rcpf(1.0f + e), small = e * big;
+  f = g < 0.0f ? small : big;
+  r = g < 0.0f ? big : small;
+}
+__device__ __forceinline__ void sigmoid_pair(double g, double& f, double& r) {
+  const double e = exp(-fabs(g)), big = 1.0 / (1.0 + e), small = e * big;
+  f = g < 0.0 ? small : big;
+  r = g < 0.0 ? big : small;
+}
+
+// an index or action of any of the three integer types
+__device__ __forceinline__ int64_t load_int(const void* p, int type, int64_t i) {
+  if (type == SIM_IT_U8) return static_cast<const uint8_t*>(p)[i];
+  if (type == SIM_IT_I32) return static_cast<const int32_t*>(p)[i];
+  return static_cast<const int64_t*>(p)[i];
+}
+
+}  // namespace
+}  // namespace bsim

@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "batchsim.h"
+#include "ops.hpp"
 #include "params.hpp"
 
 using namespace bsim;
@@ -132,6 +133,24 @@ struct sim_ctx {
     return hipSuccess;
   }
 };
+
+// what the operators (ops.cpp) use of a context
+namespace bsim {
+OpCtx op_ctx(sim_ctx* x) { return OpCtx{x->stream, x->device, x->s.err}; }
+
+int op_fail(int code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return fail(code, "%s", buf);
+}
+
+hipError_t op_timed(sim_ctx* x, int cls, hipError_t (*launch)(void*), void* arg) {
+  return x->timed(cls, [&] { return launch(arg); });
+}
+}  // namespace bsim
 
 extern "C" {
 
@@ -1360,10 +1379,11 @@ int sim_sync(sim_ctx* x) {
   HIPCHK(hipMemcpy(&err, x->s.err, 4, hipMemcpyDeviceToHost), "copy error flags");
   if (err) {
     HIPCHK(hipMemset(x->s.err, 0, 4), "clear error flags");
-    return fail(SIM_ESTATE, "device error flags 0x%x:%s%s%s", err,
+    return fail(SIM_ESTATE, "device error flags 0x%x:%s%s%s%s", err,
                 (err & ERR_ACTION) ? " action out of range;" : "",
                 (err & ERR_EVENTS) ? " event bound exceeded in a tick;" : "",
-                (err & ERR_TRACE) ? " trace overrun;" : "");
+                (err & ERR_TRACE) ? " trace overrun;" : "",
+                (err & ERR_LENGTH) ? " sequence length out of range;" : "");
   }
   return SIM_OK;
 }

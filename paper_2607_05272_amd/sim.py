@@ -16,6 +16,28 @@ def _p(t):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
+_FLOAT = {torch.float64: 0, torch.float32: 1, torch.bfloat16: 2, torch.float16: 3}
+_INT = {torch.uint8: 0, torch.int32: 1, torch.int64: 2}
+
+
+def _seq(t):
+    """sim_seq of a [B][T][D] tensor (None: absent)."""
+    if t is None:
+        return None
+    sb, st, sd = t.stride()
+    if sd != 1 and t.shape[2] > 1:
+        raise ValueError("channels (the last dimension) must be adjacent in memory")
+    return L.SimSeq(t.data_ptr(), sb, st)
+
+
+def _mat(t):
+    return None if t is None else L.SimMat(t.data_ptr(), *t.stride())
+
+
+def _ref(s):
+    return None if s is None else C.byref(s)
+
+
 def weights_layout(w):
     """Byte offsets of the policy weight buffer for workload `w` (sim_weights_layout)."""
     lib = L.load()
@@ -151,11 +173,15 @@ class Sim:
         self.A = 6 * self.K
         self.Ap = self.A + (1 if w["value_head"] else 0)
         self.device = torch.device(device)
+        self._index = (self.device.index if self.device.index is not None
+                       else torch.cuda.current_device())
+        self._device = torch.device("cuda", self._index)
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
         self._ctx = C.c_void_p()
         self._keep = []
-        L.check(self.lib.sim_create(C.byref(self.cfg), C.c_void_p(self.stream.cuda_stream),
-                                    C.byref(self._ctx)), "sim_create")
+        with torch.cuda.device(self._device):
+            L.check(self.lib.sim_create(C.byref(self.cfg), C.c_void_p(self.stream.cuda_stream),
+                                        C.byref(self._ctx)), "sim_create")
 
     def close(self):
         if self._ctx:
@@ -294,6 +320,163 @@ class Sim:
                                                   c_entropy, _p(grads), _p(loss), _p(idx)),
                 "reinforce_minibatch_grad")
         return grads, loss, idx
+
+    # -- operators for the caller's own networks -------------------------------------------
+    def _check(self, name, t, shape, dtypes):
+        """`t` is a tensor on the context's device, of this shape and one of these types."""
+        if t.device.type != "cuda" or t.device.index != self._index:
+            raise ValueError(f"{name} is on {t.device}, the context on cuda:{self._index}")
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+        if t.dtype not in dtypes:
+            raise ValueError(f"{name} is {t.dtype}, expected {' or '.join(map(str, dtypes))}")
+        return t
+
+    def _flat(self, name, t, shape, dtypes):
+        """As _check, of a tensor that is read as one contiguous array."""
+        if t is None:
+            return None
+        self._check(name, t, shape, dtypes)
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        return t
+
+    def _call(self, name, sizes, *args):
+        """An operator's entry point with work memory from torch, ordered after the work of the
+        current stream, and that stream after it, where the context has another one."""
+        need = C.c_size_t()
+        L.check(getattr(self.lib, name + "_work")(C.byref(sizes), C.byref(need)), name)
+        work = torch.empty(need.value, dtype=torch.uint8, device=self._device) if need.value else None
+        now = torch.cuda.current_stream(self._device)
+        other = now.cuda_stream != self.stream.cuda_stream
+        if other:
+            self.stream.wait_stream(now)
+        rc = getattr(self.lib, name)(self._ctx, C.byref(sizes), *args, _p(work), need.value)
+        if other:
+            now.wait_stream(self.stream)
+        L.check(rc, name)
+
+    def gated_scan(self, gate, x, h0=None, lengths=None, kind="linear", reverse=False, y=None,
+                   state=None, want_y=True):
+        """The recurrence h = gate_t h + x_t (kind "linear") or, with f = sigmoid(gate_t),
+        h = f h + (1 - f) x_t ("sigmoid") over gate, x [B][T][D], or [T][D] for one sequence, from
+        h0 [B][D] (fp64 for fp64 inputs, otherwise fp32; default 0), backwards in t with
+        `reverse`. lengths [B] int32: later steps are padding. Returns (y, state): the state
+        after each step, in the inputs' type (None unless want_y), and the last state, which
+        may be written over h0 (state=h0)."""
+        one = gate.dim() == 2
+        if one:
+            gate, x, y = gate[None], x[None], None if y is None else y[None]
+            h0, state = (None if s is None else s.reshape(1, -1) for s in (h0, state))
+        B, T, D = gate.shape
+        wide = torch.float64 if gate.dtype == torch.float64 else torch.float32
+        self._check("gate", gate, (B, T, D), _FLOAT)
+        self._check("x", x, (B, T, D), (gate.dtype,))
+        self._flat("h0", h0, (B, D), (wide,))
+        self._flat("lengths", lengths, (B,), (torch.int32,))
+        if y is not None:
+            self._check("y", y, (B, T, D), (gate.dtype,))
+        elif want_y:
+            y = torch.empty((B, T, D), dtype=gate.dtype, device=self._device)
+        if state is None:
+            state = torch.empty((B, D), dtype=wide, device=self._device)
+        self._flat("state", state, (B, D), (wide,))
+        sizes = L.SimScan(_FLOAT[gate.dtype], L.GATE_KINDS[kind], int(reverse), B, T, D)
+        self._call("gated_scan", sizes, _ref(_seq(gate)), _ref(_seq(x)), _p(lengths), _p(h0),
+                   _ref(_seq(y)), _p(state))
+        return (None if y is None else y[0], state[0]) if one else (y, state)
+
+    def gated_scan_grad(self, gate, x, y, dy, h0=None, dstate=None, lengths=None, kind="linear",
+                        reverse=False, dgate=None, dx=None, dh0=None, want_gate=True):
+        """Gradient of gated_scan: gate, x, y (its output), dy [B][T][D] or [T][D], dstate [B][D]
+        the gradient of its last state. Returns (dgate, dx, dh0) of the inputs' full shapes (sum
+        over the dimensions that an input was broadcast along); with want_gate=False dgate is
+        None and y (and x) may be."""
+        one = gate.dim() == 2
+        if one:
+            gate, x, y, dy, dgate, dx = (None if t is None else t[None]
+                                         for t in (gate, x, y, dy, dgate, dx))
+            h0, dstate, dh0 = (None if s is None else s.reshape(1, -1) for s in (h0, dstate, dh0))
+        B, T, D = gate.shape
+        wide = torch.float64 if gate.dtype == torch.float64 else torch.float32
+        self._check("gate", gate, (B, T, D), _FLOAT)
+        for name, t in (("x", x), ("y", y), ("dy", dy), ("dgate", dgate), ("dx", dx)):
+            if t is not None:
+                self._check(name, t, (B, T, D), (gate.dtype,))
+        self._flat("h0", h0, (B, D), (wide,))
+        self._flat("dstate", dstate, (B, D), (wide,))
+        self._flat("lengths", lengths, (B,), (torch.int32,))
+        if dgate is None and want_gate:
+            dgate = torch.empty((B, T, D), dtype=gate.dtype, device=self._device)
+        if dx is None:
+            dx = torch.empty((B, T, D), dtype=gate.dtype, device=self._device)
+        if dh0 is None:
+            dh0 = torch.empty((B, D), dtype=wide, device=self._device)
+        self._flat("dh0", dh0, (B, D), (wide,))
+        sizes = L.SimScan(_FLOAT[gate.dtype], L.GATE_KINDS[kind], int(reverse), B, T, D)
+        self._call("gated_scan_grad", sizes, _ref(_seq(gate)), _ref(_seq(x)), _ref(_seq(y)),
+                   _ref(_seq(dy)), _p(lengths), _p(h0), _p(dstate), _ref(_seq(dgate)),
+                   _ref(_seq(dx)), _p(dh0))
+        if one:
+            return None if dgate is None else dgate[0], dx[0], dh0[0]
+        return dgate, dx, dh0
+
+    def _grad_like(self, logits, grad, want):
+        if grad is not None:
+            return self._check("grad", grad, logits.shape, (logits.dtype,))
+        if not want:
+            return None
+        N, A = logits.shape
+        if logits.stride(1) == 1 or A == 1:
+            return torch.empty((N, A), dtype=logits.dtype, device=self._device)
+        return torch.empty((A, N), dtype=logits.dtype, device=self._device).t()
+
+    def policy_loss(self, logits, actions, adv, logp_old=None, logp_ref=None, weight=None,
+                    mask=None, clip=0.2, c_kl=0.0, c_entropy=0.0, grad=None, want_grad=True):
+        """Clipped policy loss with a KL term over logits [N][A] of any network (rows of actions,
+        or sim.policy's [A][E] logits transposed) and its gradient: actions [N] uint8, int32 or
+        int64, adv [N] fp32 or fp64, logp_old, logp_ref, weight [N] fp32 (0: padding; default
+        1/N), mask [N][A] bool or uint8 (0 forbids). Returns dict(loss [4] fp32: total, policy, KL and
+        entropy terms; logp [N]; grad [N][A] in the logits' type, which may be the logits
+        themselves: grad=logits)."""
+        N, A = logits.shape
+        self._check("logits", logits, (N, A), (torch.float32, torch.bfloat16, torch.float16))
+        self._flat("actions", actions, (N,), _INT)
+        self._flat("adv", adv, (N,), (torch.float32, torch.float64))
+        for name, t in (("logp_old", logp_old), ("logp_ref", logp_ref), ("weight", weight)):
+            self._flat(name, t, (N,), (torch.float32,))
+        if mask is not None:
+            self._check("mask", mask, (N, A), (torch.bool, torch.uint8))
+        grad = self._grad_like(logits, grad, want_grad)
+        loss = torch.empty(4, dtype=torch.float32, device=self._device)
+        logp = torch.empty(N, dtype=torch.float32, device=self._device)
+        sizes = L.SimPolicyLoss(N, A, _FLOAT[logits.dtype], _INT[actions.dtype], _FLOAT[adv.dtype],
+                                clip, c_kl, c_entropy)
+        self._call("policy_loss", sizes, _ref(_mat(logits)), _ref(_mat(mask)), _p(actions),
+                   _p(weight), _p(logp_old), _p(logp_ref), _p(adv), _ref(_mat(grad)), _p(logp),
+                   _p(loss))
+        return dict(loss=loss, logp=logp, grad=grad)
+
+    def balance_loss(self, logits, index, live=None, group=1, coef=1.0, grad=None, want_grad=True):
+        """Balance loss of a router's logits [N][A] whose rows chose the columns index [N][k]
+        (uint8, int32 or int64; -1: none), its counts and its gradient; `group` consecutive
+        columns count as one target (6 for the simulator's actions). live [N] bool or uint8: the
+        other rows are padding. Returns dict(loss (fp32 scalar), counts [A/group] int64, grad
+        [N][A])."""
+        N, A = logits.shape
+        self._check("logits", logits, (N, A), (torch.float32, torch.bfloat16, torch.float16))
+        if index.dim() != 2:
+            raise ValueError("index has shape [N][k]")
+        k = index.shape[1]
+        self._flat("index", index, (N, k), _INT)
+        self._flat("live", live, (N,), (torch.bool, torch.uint8))
+        grad = self._grad_like(logits, grad, want_grad)
+        counts = torch.empty(max(1, A // max(1, group)), dtype=torch.int64, device=self._device)
+        loss = torch.empty((), dtype=torch.float32, device=self._device)
+        sizes = L.SimBalance(N, A, k, group, _FLOAT[logits.dtype], _INT[index.dtype], coef)
+        self._call("balance_loss", sizes, _ref(_mat(logits)), _p(index), _p(live), _ref(_mat(grad)),
+                   _p(counts), _p(loss))
+        return dict(loss=loss, counts=counts, grad=grad)
 
     def params_from_weights(self, weights):
         p = torch.empty(self.ppo_grad_count(), dtype=torch.float32, device=self.device)

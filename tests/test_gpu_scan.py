@@ -1,0 +1,308 @@
+"""The gated recurrence and its gradient against the fp64 form (oracle/ops.py) within the bounds of
+scan_check.py: types, kinds, directions, layouts, lengths and sizes around the kernels' tiles; the
+single-token form; refusals; streams, graphs and far offsets."""
+import numpy as np
+import pytest
+
+from workloads import preset
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+import scan_check as sc   # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def sim():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2607_05272_amd as bs
+    with bs.Sim(preset("C1"), n_envs=1) as s:
+        yield s
+
+
+def both(sim, d, kind, reverse, y=None):
+    """Forward and gradient checked; padding filled with NaN first."""
+    if d["lengths"] is not None:
+        T = d["gate"].shape[1]
+        pad = torch.arange(T, device="cuda")[None] >= d["lengths"][:, None].long()
+        clean = dict(d)
+        for k in ("gate", "x", "dy"):
+            d[k] = d[k].masked_fill(pad[..., None], float("nan"))
+        want = clean
+    else:
+        want = d
+    y, state = sim.gated_scan(d["gate"], d["x"], d["h0"], d["lengths"], kind, reverse)
+    sim.sync()
+    sc.check_forward(want, y, state, kind, reverse)
+    dg, dx, dh0 = sim.gated_scan_grad(d["gate"], d["x"], y, d["dy"], d["h0"], d["dstate"], d["lengths"],
+                                      kind, reverse)
+    sim.sync()
+    sc.check_grad(want, y, dg, dx, dh0, kind, reverse)
+
+
+SHAPES = [(1, 1, 1), (3, 1, 64), (2, 5, 7), (1, 128, 8), (1, 130, 8), (2, 257, 64), (1, 1030, 3),
+          (3, 300, 40), (1, 513, 65), (5, 33, 1), (2, 300, 1), (64, 1, 256), (2, 127, 136), (1, 640, 16),
+          (4, 64, 72), (7, 2, 33), (1, 2048, 1)]
+
+
+@pytest.mark.parametrize("dtype", ["f64", "f32", "bf16", "f16"])
+@pytest.mark.parametrize("kind", ["linear", "sigmoid"])
+@pytest.mark.parametrize("B,T,D", SHAPES)
+def test_shapes(sim, B, T, D, kind, dtype):
+    seed = B + 10 * T + D
+    for reverse in (False, True):
+        d = sc.inputs(B, T, D, sc.TYPES[dtype], kind, seed, h0=seed % 3 > 0, device="cuda")
+        if reverse and seed % 2:
+            d["dstate"] = None
+        both(sim, d, kind, reverse)
+
+
+@pytest.mark.parametrize("dtype", ["f64", "f32", "bf16"])
+@pytest.mark.parametrize("kind", ["linear", "sigmoid"])
+@pytest.mark.parametrize("B,T,D", [(5, 40, 16), (4, 300, 1), (6, 200, 24), (3, 1, 5), (3, 700, 64), (4, 2100, 8)])
+def test_lengths(sim, B, T, D, kind, dtype):
+    for reverse in (False, True):
+        both(sim, sc.inputs(B, T, D, sc.TYPES[dtype], kind, T, h0=not reverse, lengths=True, device="cuda"),
+             kind, reverse)
+
+
+@pytest.mark.parametrize("dtype", ["f64", "f32", "bf16"])
+@pytest.mark.parametrize("B,T,D", [(1, 5000, 64), (2, 9001, 5), (1, 20000, 1), (3, 3001, 16), (1, 4100, 520),
+                                   (1, 16500, 24)])
+def test_long(sim, B, T, D, dtype):
+    """Sequences that are split over time where there are few channels."""
+    for kind, reverse in (("linear", True), ("sigmoid", False)):
+        both(sim, sc.inputs(B, T, D, sc.TYPES[dtype], kind, D, lengths=B > 1, device="cuda"), kind, reverse)
+
+
+@pytest.mark.parametrize("layout", ["tbd", "fused", "offset", "rows"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_layouts(sim, layout, dtype):
+    B, T, D, dt = 3, 150, 24, sc.TYPES[dtype]
+    d = sc.inputs(B, T, D, dt, "sigmoid", 7, lengths=True, device="cuda")
+    def put(big, v):                 # v's values in a view of the same shape elsewhere   # noqa: E306
+        big.copy_(v)
+        return big
+    out = {}
+    for k in ("gate", "x", "dy"):
+        v = d[k]
+        if layout == "tbd":
+            d[k] = v.transpose(0, 1).contiguous().transpose(0, 1)
+        elif layout == "fused":      # one projection's slices
+            d[k] = put(torch.zeros(B, T, 3 * D, dtype=dt, device="cuda")[..., D:2 * D], v)
+        elif layout == "offset":     # a start that is aligned to the type alone
+            d[k] = put(torch.zeros(B * T * D + 1, dtype=dt, device="cuda")[1:].view(B, T, D), v)
+        else:                        # rows of an odd length
+            d[k] = put(torch.zeros(B, T, D + 1, dtype=dt, device="cuda")[..., :D], v)
+    for k in ("y", "dgate", "dx"):   # outputs between guards
+        big = torch.full((T, B, D + 5), 77.0, dtype=dt, device="cuda")
+        out[k] = big, big[:, :, 2:2 + D].transpose(0, 1)
+    y, state = sim.gated_scan(d["gate"], d["x"], d["h0"], d["lengths"], "sigmoid", False, y=out["y"][1])
+    dg, dx, dh0 = sim.gated_scan_grad(d["gate"], d["x"], y, d["dy"], d["h0"], d["dstate"], d["lengths"], "sigmoid",
+                                      dgate=out["dgate"][1], dx=out["dx"][1])
+    sim.sync()
+    sc.check_forward(d, y, state, "sigmoid", False)
+    sc.check_grad(d, y, dg, dx, dh0, "sigmoid", False)
+    for big, _ in out.values():
+        assert (big[:, :, :2] == 77).all() and (big[:, :, 2 + D:] == 77).all()
+
+
+def test_broadcast_gate_and_flat_sequence(sim):
+    """One gate for all steps (stride 0), a [T][D] sequence: the returns' recurrence, as returns_gae
+    computes it to rounding; the gate's gradient summed by the caller."""
+    import paper_2607_05272_amd as bs
+    T, E = 300, 40
+    g = torch.Generator().manual_seed(3)
+    r = torch.randn(T, E, generator=g, dtype=torch.float64).cuda()
+    v = torch.randn(T + 1, E, generator=g).cuda()
+    with bs.Sim(preset("C1"), n_envs=E) as s:
+        adv, _ = s.returns_gae(r, v, 0.99, 0.95)
+        delta = (r + 0.99 * v[1:].double()) - v[:-1].double()
+        gate = torch.tensor(0.99 * 0.95, dtype=torch.float64, device="cuda").expand(T, E)
+        full = torch.full((T, E), 0.99 * 0.95, dtype=torch.float64, device="cuda")
+        got, last = s.gated_scan(full[:1].expand(T, E), delta, reverse=True)
+        s.sync()
+        np.testing.assert_allclose(got.cpu().numpy(), adv.cpu().numpy(), rtol=1e-12, atol=1e-12)
+        assert torch.equal(last, got[0])
+        with pytest.raises(ValueError):          # channels of a stride of 0 are not adjacent
+            s.gated_scan(gate, delta)
+        y, dy = got, torch.randn(T, E, generator=g, dtype=torch.float64).cuda()
+        a = s.gated_scan_grad(full, None, y, dy, reverse=True)
+        b = s.gated_scan_grad(full[:1].expand(T, E), None, y, dy, reverse=True)
+        none, dx, _ = s.gated_scan_grad(full[:1].expand(T, E), None, None, dy, reverse=True, want_gate=False)
+        s.sync()
+        assert none is None and torch.equal(dx, a[1])
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_single_tokens(sim, dtype):
+    """Token by token, the state updated in place, against the whole sequence."""
+    B, T, D = 5, 12, 200
+    d = sc.inputs(B, T, D, sc.TYPES[dtype], "sigmoid", 5, device="cuda")
+    h = d["h0"].clone()
+    ys = []
+    for t in range(T):
+        y, s = sim.gated_scan(d["gate"][:, t:t + 1], d["x"][:, t:t + 1], h0=h, kind="sigmoid", state=h)
+        assert s is h
+        ys.append(y)
+    sim.sync()
+    sc.check_forward(d, torch.cat(ys, 1), h, "sigmoid", False)
+
+
+@pytest.mark.parametrize("T,D", [(70, 30), (6000, 8)])
+def test_state_in_place_and_alone(sim, T, D):
+    """The last state over h0, also where a sequence is split over time; no y wanted."""
+    d = sc.inputs(2, T, D, torch.float32, "linear", 6, device="cuda")
+    y, want = sim.gated_scan(d["gate"], d["x"], d["h0"])
+    h = d["h0"].clone()
+    none, _ = sim.gated_scan(d["gate"], d["x"], h, state=h, want_y=False)
+    sim.sync()
+    assert none is None and torch.equal(h, want) and torch.equal(y[:, -1], want)
+
+
+def test_empty(sim):
+    z = torch.empty(2, 0, 3, device="cuda")
+    h0 = torch.randn(2, 3, device="cuda")
+    y, s = sim.gated_scan(z, z, h0)
+    _, _, dh0 = sim.gated_scan_grad(z, z, z, z, h0, dstate=h0)
+    _, s0 = sim.gated_scan(z, z)
+    for shape in ((0, 4, 3), (2, 4, 0)):
+        e = torch.empty(shape, device="cuda")
+        sim.gated_scan(e, e)
+        sim.gated_scan_grad(e, e, e, e)
+    sim.sync()
+    assert y.numel() == 0 and torch.equal(s, h0) and torch.equal(dh0, h0) and (s0 == 0).all()
+
+
+def test_not_finite(sim):
+    """A NaN or infinite input reaches the steps after it in its channel and no others; a zero gate does
+    not stop it (0 times infinity), padding does not bring it in."""
+    for T in (90, 5000):
+        d = sc.inputs(1, T, 9, torch.float32, "linear", 8, device="cuda")
+        want, _ = sim.gated_scan(d["gate"], d["x"], d["h0"])
+        x = d["x"].clone()
+        x[0, 40, 2], x[0, 50, 5] = float("nan"), float("inf")
+        got, last = sim.gated_scan(d["gate"], x, d["h0"])
+        sim.sync()
+        ok = torch.isfinite(got)[0]
+        assert ok[:40, 2].all() and not ok[40:, 2].any() and ok[:50, 5].all() and not ok[50:, 5].any()
+        keep = ok.clone()
+        assert ok[:, [0, 1, 3, 4, 6, 7, 8]].all()
+        assert torch.equal(got[0][keep], want[0][keep])
+        assert torch.equal(torch.isfinite(last[0]), ok[-1])
+
+
+def test_lengths_out_of_range_are_latched(sim):
+    import paper_2607_05272_amd as bs
+    d = sc.inputs(3, 20, 8, torch.float32, "linear", 9, device="cuda")
+    n = torch.tensor([25, -3, 20], dtype=torch.int32, device="cuda")
+    y, s = sim.gated_scan(d["gate"], d["x"], d["h0"], n)
+    with pytest.raises(bs.SimError, match="length out of range"):
+        sim.sync()
+    d["lengths"] = torch.tensor([20, 0, 20], dtype=torch.int32, device="cuda")
+    sc.check_forward(d, y, s, "linear", False)
+    sim.sync()
+
+
+def test_refusals(sim):
+    import paper_2607_05272_amd as bs
+    a = torch.zeros(2, 4, 6, device="cuda")
+    for bad in (lambda: sim.gated_scan(a, a[:, :3]), lambda: sim.gated_scan(a, a.double()),
+                lambda: sim.gated_scan(a.long(), a.long()), lambda: sim.gated_scan(a.cpu(), a),
+                lambda: sim.gated_scan(a.transpose(1, 2), a.transpose(1, 2)),
+                lambda: sim.gated_scan(a, a, h0=torch.zeros(2, 5, device="cuda")),
+                lambda: sim.gated_scan(a, a, h0=torch.zeros(2, 6, dtype=torch.float64, device="cuda")),
+                lambda: sim.gated_scan(a, a, h0=torch.zeros(6, 2, device="cuda").t()),
+                lambda: sim.gated_scan(a, a, lengths=torch.zeros(2, dtype=torch.int64, device="cuda"))):
+        with pytest.raises((ValueError, KeyError)):
+            bad()
+    with pytest.raises(KeyError):
+        sim.gated_scan(a, a, kind="tanh")
+    shared = torch.zeros(1, 4, 6, device="cuda").expand(2, 4, 6)
+    with pytest.raises(bs.SimError, match="share memory"):
+        sim.gated_scan(a, a, y=shared)
+    with pytest.raises(bs.SimError, match="share memory"):
+        sim.gated_scan(a, a, y=torch.zeros(40, device="cuda").as_strided((2, 4, 6), (5, 6, 1)))
+    with pytest.raises(bs.SimError, match="x is NULL"):
+        sim.gated_scan_grad(a, None, a, a, kind="sigmoid")
+    sim.sync()
+
+
+def test_far_offsets(sim):
+    """Two sequences more than 2^31 elements apart, in every array."""
+    B, T, D, far = 2, 70, 40, (1 << 31) + 24
+    d = sc.inputs(B, T, D, torch.bfloat16, "linear", 11, device="cuda")
+    room = torch.empty(far + 6 * T * D, dtype=torch.bfloat16, device="cuda")
+    v = [room[i * T * D:].as_strided((B, T, D), (far, D, 1)) for i in range(6)]
+    for t, k in zip(v, ("gate", "x", "dy")):
+        t.copy_(d[k])
+        d[k] = t
+    y, s = sim.gated_scan(d["gate"], d["x"], d["h0"], y=v[3])
+    dg, dx, dh0 = sim.gated_scan_grad(d["gate"], d["x"], y, d["dy"], d["h0"], d["dstate"], dgate=v[4], dx=v[5])
+    sim.sync()
+    sc.check_forward(d, y, s, "linear", False)
+    sc.check_grad(d, y, dg, dx, dh0, "linear", False)
+
+
+def test_graphs_and_streams(sim):
+    """Two captured calls on streams of their own, replayed side by side and in turn with eager work
+    between, give the eager results each time; a context used from another stream is ordered after
+    that stream's work and before what follows there."""
+    import paper_2607_05272_amd as bs
+    sets = [sc.inputs(2, 5000, 8, torch.float32, "sigmoid", s, device="cuda") for s in (1, 2)]
+
+    def call(s, d):
+        y, h = s.gated_scan(d["gate"], d["x"], d["h0"], kind="sigmoid")
+        return (y, h, *s.gated_scan_grad(d["gate"], d["x"], y, d["dy"], d["h0"], d["dstate"], kind="sigmoid"))
+    want = [call(sim, d) for d in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    with bs.Sim(preset("C1"), n_envs=1, stream=streams[0]) as s0:
+        torch.cuda.synchronize()
+        graphs, got = [], []
+        for d in sets:               # both on one context
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=streams[0]):
+                got.append(call(s0, d))
+            graphs.append(g)
+        for r in range(4):
+            for o in got:
+                for t in o:
+                    t.fill_(-1.0)
+            torch.cuda.synchronize()
+            for g, st in zip(graphs, streams):
+                with torch.cuda.stream(st):
+                    g.replay()
+            call(sim, sets[0])
+            torch.cuda.synchronize()
+            for w, o in zip(want, got):
+                assert all(torch.equal(p, q) for p, q in zip(w, o)), r
+        # the context's stream is streams[0]; the tensors' is streams[1]
+        with torch.cuda.stream(streams[1]):
+            d = {k: None if v is None else v.clone() for k, v in sets[0].items()}
+            torch.cuda._sleep(2_000_000)
+            d["x"].mul_(0.5)
+            y, h = s0.gated_scan(d["gate"], d["x"], d["h0"], kind="sigmoid")
+            total = (y * 1.0, h * 1.0)
+        torch.cuda.synchronize()
+        sc.check_forward(d, total[0], total[1], "sigmoid", False)
+
+
+def test_two_contexts_at_once(sim):
+    """Calls of two contexts on two streams, issued in turn."""
+    import paper_2607_05272_amd as bs
+    st = torch.cuda.Stream()
+    d = sc.inputs(1, 6000, 16, torch.float32, "linear", 4, device="cuda")
+    want = sim.gated_scan(d["gate"], d["x"], d["h0"])[0]
+    torch.cuda.synchronize()
+    with bs.Sim(preset("C1"), n_envs=1, stream=st) as other:
+        torch.cuda.synchronize()
+        outs = []
+        for _ in range(8):
+            outs.append(sim.gated_scan(d["gate"], d["x"], d["h0"])[0])
+            with torch.cuda.stream(st):
+                outs.append(other.gated_scan(d["gate"], d["x"], d["h0"])[0])
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, want) for o in outs)
