@@ -440,7 +440,7 @@ typedef struct sim_mat {
  *  kind       SIM_GATE_LINEAR:  h = gate_t h + x_t
  *             SIM_GATE_SIGMOID: f = 1 / (1 + exp(-gate_t)), h = f h + (1 - f) x_t
  *  reverse    0: t = 0, 1, ..; 1: from the last step back to t = 0
- *  B, T, D    sequences, steps, channels                                                 */
+ *  B, T, D    sequences, steps (below 2^30), channels (B D below 2^31)                    */
 typedef struct sim_scan {
   int32_t dtype, kind, reverse;
   int64_t B, T, D;

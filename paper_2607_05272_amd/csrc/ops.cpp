@@ -68,8 +68,8 @@ int check_scan(const sim_scan* s, const char* who) {
     return op_fail(SIM_EINVAL, "%s: unknown kind %d", who, s->kind);
   if (s->reverse != 0 && s->reverse != 1) return op_fail(SIM_EINVAL, "%s: reverse must be 0 or 1", who);
   if (s->B < 0 || s->T < 0 || s->D < 0) return op_fail(SIM_EINVAL, "%s: B, T and D must be >= 0", who);
-  if (s->T > kMax31 || s->B > kMax31 || s->D > kMax31 || s->B * s->D > kMax31)
-    return op_fail(SIM_EUNSUPPORTED, "%s: T and B*D must stay below 2^31", who);
+  if (s->T >= (1 << 30) || s->B > kMax31 || s->D > kMax31 || s->B * s->D > kMax31)
+    return op_fail(SIM_EUNSUPPORTED, "%s: T must stay below 2^30, B*D below 2^31", who);
   return SIM_OK;
 }
 

@@ -2,13 +2,26 @@
 //
 //   linear   h = g_t h + x_t,        sigmoid  f = 1/(1 + exp(-g_t)), h = f h + (1 - f) x_t
 //
-// One multiplication and one addition per element over two reads and a write: bound by HBM.
-// Positions p = 0..T-1 are taken in processing order, t = p or T-1-p; padding is the
-// identity, so the state passes through it on either side of a sequence.
+// A run of steps maps the state h before it to A h + X, with A the product of its gates and X its
+// result from 0; two runs in a row join to (A2 A1, A2 X1 + X2). So a workgroup takes a tile of
+// segments, a thread each: it scans its segment from 0 in registers, the segments' (A, X) are
+// scanned across the workgroup, and each thread then adds A_l times the state that its segment starts
+// from. Each element is read once and written once; a multiplication and an addition per element
+// (and a sigmoid): bound by HBM.
+//
+// Positions p = 0..T-1 are taken in processing order, t = p, or from the end. Padding is the
+// identity (A, X) = (1, 0), so the state passes through it on either side of a sequence.
+#include <algorithm>
+
 #include "ops_dev.hpp"
 
 namespace bsim {
 namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+
+__device__ __forceinline__ float fma_w(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ double fma_w(double a, double b, double c) { return fma(a, b, c); }
 
 // a step's gate and the factor of its input: h = a h + r x
 template <class W, bool SIG>
@@ -21,82 +34,632 @@ __device__ __forceinline__ void gate_of(W g, W& a, W& r) {
   }
 }
 
-__device__ __forceinline__ int64_t seq_len(const ScanArgs& s, int64_t b, bool tell) {
-  if (!s.len) return s.c.T;
-  int64_t n = s.len[b];
-  if (n < 0 || n > s.c.T) {
+__device__ __forceinline__ int seq_len(const ScanArgs& s, int64_t b, bool tell) {
+  const int T = (int)s.c.T;
+  if (!s.len) return T;
+  int n = s.len[b];
+  if (n < 0 || n > T) {
     if (tell) atomicOr(s.err, ERR_LENGTH);
-    n = n < 0 ? 0 : s.c.T;
+    n = n < 0 ? 0 : T;
   }
   return n;
 }
 
-// One lane per channel, step after step.
-template <class E, bool SIG>
-__global__ __launch_bounds__(256) void scan_step_k(ScanArgs s) {
+// How a launch cuts its arrays. Channels adjacent (time = 0): a thread has L steps of V channels,
+// 1 << lx threads stand beside each other along the channels and the others along the steps. One
+// channel whose steps are adjacent (time = 1): a thread has L adjacent steps, a sequence has
+// 1 << gs threads.
+struct ScanPlan {
+  int time, vec;      // vec: 16-byte accesses
+  int lx, gs;
+  int64_t tiles;      // workgroups side by side
+  int64_t per;        // time = 0: channel tiles of a sequence
+  int chunks;         // time-wise pieces, each a workgroup that goes over `ctiles` tiles
+  int ctiles;
+};
+
+template <class T, int N>
+struct VecOf { typedef T V __attribute__((ext_vector_type(N), aligned(sizeof(T) * N < 16 ? sizeof(T) * N : 16))); };
+template <class T>
+struct VecOf<T, 1> { typedef T V; };
+
+// What a thread is to its tile.
+struct Place {
+  int unit, segw, nsw;   // lanes from one segment to the next; its place in the wave; their number
+  int wave, wv, nwv;     // its wave in the workgroup and in the scan, and their number
+  int seg, nseg;         // its segment in the tile
+  int col;               // its column of the scan's LDS
+};
+__device__ __forceinline__ Place place_of(const ScanPlan& p) {
+  Place q;
+  const int tid = threadIdx.x, lane = tid & 63;
+  q.wave = tid >> 6;
+  if (p.time) {
+    const int gs = 1 << p.gs;
+    q.unit = 1;
+    q.nsw = gs < 64 ? gs : 64;
+    q.segw = lane & (q.nsw - 1);
+    q.nwv = gs < 64 ? 1 : gs >> 6;
+    q.wv = q.wave & (q.nwv - 1);
+    q.seg = tid & (gs - 1);
+    q.nseg = gs;
+    q.col = 0;
+  } else {
+    q.unit = 1 << p.lx;
+    q.nsw = 64 >> p.lx;
+    q.segw = lane >> p.lx;
+    q.nwv = kWaves;
+    q.wv = q.wave;
+    q.seg = tid >> p.lx;
+    q.nseg = kThreads >> p.lx;
+    q.col = lane & (q.unit - 1);
+  }
+  return q;
+}
+
+// One run's (A, X) of V channels per thread, scanned over the tile's segments in order. On return
+// (A, X) is the run of all segments of this wave before this one, and `carry`, the state at the
+// tile's start, has become the state at the wave's start; total: the state at the tile's end.
+// `lds` holds kWaves rows of 64 columns of V pairs and is free again after the next barrier.
+template <class W, int V>
+__device__ __forceinline__ void scan_tile(const Place& q, W (&A)[V], W (&X)[V], W (&carry)[V], W (&total)[V],
+                                          W (*lds)[64][V][2]) {
+  for (int d = 1; d < q.nsw; d <<= 1) {
+    const bool take = q.segw >= d;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const W a = __shfl_up(A[v], d * q.unit), x = __shfl_up(X[v], d * q.unit);
+      X[v] = take ? fma_w(A[v], x, X[v]) : X[v];
+      A[v] = take ? A[v] * a : A[v];
+    }
+  }
+  if (q.nwv > 1 && q.segw == q.nsw - 1) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      lds[q.wave][q.col][v][0] = A[v];
+      lds[q.wave][q.col][v][1] = X[v];
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const W a = __shfl_up(A[v], q.unit), x = __shfl_up(X[v], q.unit);
+    A[v] = q.segw > 0 ? a : (W)1;
+    X[v] = q.segw > 0 ? x : (W)0;
+  }
+  if (q.nwv > 1) {
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < V; ++v) total[v] = carry[v];
+    for (int w = 0; w < q.nwv; ++w) {
+      auto row = lds[q.wave - q.wv + w][q.col];
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        carry[v] = w == q.wv ? total[v] : carry[v];
+        total[v] = fma_w(row[v][0], total[v], row[v][1]);
+      }
+    }
+  }
+}
+
+// The L steps by V channels (or L adjacent steps) that a thread reads of one array.
+template <class E, int V, int L, bool TV>
+struct Block {
   typedef typename E::T T;
   typedef typename E::W W;
-  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (c >= s.c.B * s.c.D) return;
-  const int64_t b = c / s.c.D, d = c % s.c.D, n = seq_len(s, b, d == 0);
+  typedef typename VecOf<T, TV ? L : V>::V Vec;
+  Vec r[TV ? 1 : L];
+  __device__ __forceinline__ W get(int l, int v) const {
+    if constexpr (TV) return (W)r[0][l];
+    else if constexpr (V == 1) return (W)r[l];
+    else return (W)r[l][v];
+  }
+};
+
+// Where a thread's block lies: steps t0 + l (or t0 + L - 1 - l, back) of its channels.
+struct Where {
+  int t0;        // the first step in memory
+  int n, T;      // steps of the sequence, of the arrays
+  int d;         // channel
+  bool back, vec;
+  __device__ __forceinline__ int t(int l, int L) const { return back ? t0 + L - 1 - l : t0 + l; }
+};
+
+// Reads steps t + shift; those outside the sequence read some other step of it (or, where it has none,
+// nothing): the caller does not use them.
+template <class E, int V, int L, bool TV>
+__device__ __forceinline__ void load(Block<E, V, L, TV>& blk, const sim_seq& q, int64_t b, const Where& w,
+                                     int shift = 0) {
+  typedef typename E::T T;
+  typedef typename Block<E, V, L, TV>::Vec Vec;
+  const T* p = static_cast<const T*>(q.data) + b * q.stride_b;
+  if constexpr (TV) {
+    if (w.vec && shift == 0 && w.t0 >= 0 && w.t0 + L <= w.T) {
+      blk.r[0] = *reinterpret_cast<const Vec*>(p + w.t0);
+    } else if (w.n > 0) {
+#pragma unroll
+      for (int l = 0; l < L; ++l) {
+        int t = w.t0 + l + shift;
+        t = t < 0 ? 0 : (t >= w.n ? w.n - 1 : t);
+        blk.r[0][l] = p[(int64_t)t * q.stride_t];
+      }
+    }
+    if (w.back) {
+      Vec o = blk.r[0];
+#pragma unroll
+      for (int l = 0; l < L; ++l) blk.r[0][l] = o[L - 1 - l];
+    }
+  } else if (w.n > 0) {
+#pragma unroll
+    for (int l = 0; l < L; ++l) {
+      int t = w.t(l, L) + shift;
+      t = t < 0 ? 0 : (t >= w.n ? w.n - 1 : t);
+      blk.r[l] = *reinterpret_cast<const Vec*>(p + (int64_t)t * q.stride_t + w.d);
+    }
+  }
+}
+
+template <class E, int V, int L, bool TV>
+__device__ __forceinline__ void store(const Block<E, V, L, TV>& blk, const sim_seq& q, int64_t b, const Where& w) {
+  typedef typename E::T T;
+  typedef typename Block<E, V, L, TV>::Vec Vec;
+  T* p = static_cast<T*>(q.data) + b * q.stride_b;
+  if constexpr (TV) {
+    Vec o = blk.r[0];
+    if (w.back) {
+#pragma unroll
+      for (int l = 0; l < L; ++l) o[l] = blk.r[0][L - 1 - l];
+    }
+    if (w.vec && w.t0 >= 0 && w.t0 + L <= w.T) {
+      *reinterpret_cast<Vec*>(p + w.t0) = o;
+    } else {
+#pragma unroll
+      for (int l = 0; l < L; ++l)
+        if (w.t0 + l >= 0 && w.t0 + l < w.T) p[(int64_t)(w.t0 + l) * q.stride_t] = o[l];
+    }
+  } else {
+#pragma unroll
+    for (int l = 0; l < L; ++l) {
+      const int t = w.t(l, L);
+      if (t >= 0 && t < w.T) *reinterpret_cast<Vec*>(p + (int64_t)t * q.stride_t + w.d) = blk.r[l];
+    }
+  }
+}
+
+// The block of position p: for one channel whose steps are adjacent, blocks start at multiples
+// of L in memory in either direction (the first one back is cut off by T instead).
+template <int L, bool TV>
+__device__ __forceinline__ int first_step(int p, int T, bool back) {
+  const int end = TV ? (T + L - 1) / L * L : T;
+  return back ? end - L - p : p;
+}
+
+// LDS rows of the scan, two so that one barrier per tile is enough
+template <class W, int V>
+struct ScanLds { W v[2][kWaves][64][V][2]; };
+
+// What a workgroup's thread is in the whole launch.
+struct Job {
+  int64_t b;
+  int d;
+  bool live;    // it has channels of its own (others read some channel and write none)
+};
+template <int V, bool TV>
+__device__ __forceinline__ Job job_of(const ScanPlan& p, const Place& q, const sim_scan& c, int64_t blk) {
+  Job j;
+  if (TV) {
+    j.b = (blk << (8 - p.gs)) + (threadIdx.x >> p.gs);
+    j.d = 0;
+    j.live = j.b < c.B;
+    if (!j.live) j.b = c.B - 1;
+  } else {
+    j.b = blk / p.per;
+    const int64_t d = (((blk % p.per) << p.lx) + q.col) * V;
+    j.live = d < c.D;
+    j.d = (int)(j.live ? d : c.D - V);
+  }
+  return j;
+}
+
+// The states before each chunk are found from the chunks' runs, which a launch before this one left
+// in the work memory: slot 0 holds the state before the first, slot i + 1 the run of chunk i.
+template <class W>
+__device__ __forceinline__ W* slot(const ScanArgs& s, int64_t i) {
+  return static_cast<W*>(s.work) + i * 2 * s.c.B * s.c.D;
+}
+
+template <class W, int V>
+__device__ __forceinline__ void state_before(const ScanArgs& s, const ScanPlan& p, const Place& q, const Job& j,
+                                             int chunk, const void* first, W (&h)[V], ScanLds<W, V>& lds) {
+  const int64_t at = j.b * s.c.D + j.d, n = s.c.B * s.c.D;
+  const W* h0 = p.chunks > 1 ? slot<W>(s, 0) : static_cast<const W*>(first);
+#pragma unroll
+  for (int v = 0; v < V; ++v) h[v] = h0 ? h0[at + v] : (W)0;
+  for (int base = 0; base < chunk; base += q.nseg) {
+    const int i = base + q.seg;
+    W A[V], X[V], end[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      A[v] = i < chunk ? slot<W>(s, i + 1)[at + v] : (W)1;
+      X[v] = i < chunk ? slot<W>(s, i + 1)[n + at + v] : (W)0;
+    }
+    __syncthreads();
+    scan_tile<W, V>(q, A, X, h, end, lds.v[0]);
+#pragma unroll
+    for (int v = 0; v < V; ++v) h[v] = end[v];
+  }
+  __syncthreads();
+}
+
+// A chunk's run: each thread takes a contiguous part of it, then one scan.
+template <class E, bool SIG, int V, int L, bool TV, bool GRAD>
+__global__ __launch_bounds__(kThreads) void scan_runs_k(ScanArgs s, ScanPlan p) {
+  typedef typename E::W W;
+  __shared__ ScanLds<W, V> lds;
+  const Place q = place_of(p);
+  const bool back = GRAD ? !s.c.reverse : s.c.reverse != 0;
+  const Job j = job_of<V, TV>(p, q, s.c, blockIdx.x);
+  const int n = seq_len(s, j.b, false), T = (int)s.c.T;
+  const int64_t at = j.b * s.c.D + j.d, bd = s.c.B * s.c.D;
+  W A[V], X[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) { A[v] = (W)1; X[v] = (W)0; }
+  const int p0 = ((int)blockIdx.y * q.nseg + q.seg) * p.ctiles * L;
+  for (int i = 0; i < p.ctiles; ++i) {
+    Where w{first_step<L, TV>(p0 + i * L, T, back), n, T, j.d, back, p.vec != 0};
+    Block<E, V, L, TV> g{}, x{};
+    load(g, s.g, j.b, w);
+    load(x, GRAD ? s.dy : s.x, j.b, w);
+#pragma unroll
+    for (int l = 0; l < L; ++l) {
+      const int t = w.t(l, L);
+      const bool on = t >= 0 && t < n;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        W a, r;
+        gate_of<W, SIG>(g.get(l, v), a, r);
+        // gradient: C = a (dy + C)
+        const W nx = GRAD ? a * (x.get(l, v) + X[v]) : fma_w(a, X[v], r * x.get(l, v));
+        X[v] = on ? nx : X[v];
+        A[v] = on ? A[v] * a : A[v];
+      }
+    }
+  }
+  W carry[V], end[V], run[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) { carry[v] = (W)0; run[v] = A[v]; }
+  // the product of all gates: the same scan with the inputs left out, from 1
+  W A2[V], Z[V], one[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) { A2[v] = run[v]; Z[v] = (W)0; one[v] = (W)1; }
+  scan_tile<W, V>(q, A, X, carry, end, lds.v[0]);
+  W prod[V];
+  scan_tile<W, V>(q, A2, Z, one, prod, lds.v[1]);
+  if (q.seg == 0 && j.live) {
+    const void* first = GRAD ? s.ds : s.h0;
+    W* o = slot<W>(s, blockIdx.y + 1);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      o[at + v] = prod[v];
+      o[bd + at + v] = end[v];
+      if (blockIdx.y == 0) slot<W>(s, 0)[at + v] = first ? static_cast<const W*>(first)[at + v] : (W)0;
+    }
+  }
+}
+
+template <class E, bool SIG, int V, int L, bool TV>
+__global__ __launch_bounds__(kThreads) void scan_tile_k(ScanArgs s, ScanPlan p) {
+  typedef typename E::T El;
+  typedef typename E::W W;
+  __shared__ ScanLds<W, V> lds;
+  const Place q = place_of(p);
+  const bool back = s.c.reverse != 0;
+  for (int64_t blk = blockIdx.x; blk < p.tiles; blk += gridDim.x) {
+    const Job j = job_of<V, TV>(p, q, s.c, blk);
+    const int n = seq_len(s, j.b, q.seg == 0 && blockIdx.y == 0), T = (int)s.c.T;
+    const int64_t at = j.b * s.c.D + j.d;
+    W h[V];
+    state_before<W, V>(s, p, q, j, blockIdx.y, s.h0, h, lds);
+    const int span = q.nseg * L;
+    const int p0 = (int)blockIdx.y * p.ctiles * span + q.seg * L;
+    Where w{first_step<L, TV>(p0, T, back), n, T, j.d, back, p.vec != 0};
+    Block<E, V, L, TV> g{}, x{};
+    load(g, s.g, j.b, w);
+    load(x, s.x, j.b, w);
+    for (int i = 0; i < p.ctiles; ++i) {
+      // the segment from a state of 0, and its gates' products
+      W A[L][V], X[L][V];
+#pragma unroll
+      for (int l = 0; l < L; ++l) {
+        const int t = w.t(l, L);
+        const bool on = t >= 0 && t < n;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          W a, r;
+          gate_of<W, SIG>(g.get(l, v), a, r);
+          W u = r * x.get(l, v);
+          a = on ? a : (W)1;
+          u = on ? u : (W)0;
+          A[l][v] = l ? A[l - (l > 0)][v] * a : a;
+          X[l][v] = l ? fma_w(a, X[l - (l > 0)][v], u) : u;
+        }
+      }
+      const Where now = w;
+      if (i + 1 < p.ctiles) {   // the next tile's loads fly during the scan
+        w.t0 = first_step<L, TV>(p0 + (i + 1) * span, T, back);
+        load(g, s.g, j.b, w);
+        load(x, s.x, j.b, w);
+      }
+      W a[V], u[V], end[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) { a[v] = A[L - 1][v]; u[v] = X[L - 1][v]; }
+      scan_tile<W, V>(q, a, u, h, end, lds.v[i & 1]);
+      Block<E, V, L, TV> y;
+      W last[V];
+      bool ends = false;   // whether the sequence's last step is here
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const W in = fma_w(a[v], h[v], u[v]);
+        last[v] = in;
+#pragma unroll
+        for (int l = 0; l < L; ++l) {
+          const int t = now.t(l, L);
+          const bool on = t >= 0 && t < n;
+          const W hl = fma_w(A[l][v], in, X[l][v]);
+          if (on && t == (back ? 0 : n - 1)) {
+            ends = true;
+            last[v] = hl;
+          }
+          const El o = (El)(on ? hl : (W)0);
+          if constexpr (TV) y.r[0][l] = o;
+          else if constexpr (V == 1) y.r[l] = o;
+          else y.r[l][v] = o;
+        }
+      }
+      if (s.y.data && j.live) store(y, s.y, j.b, now);
+      if (s.state && j.live && (ends || (n == 0 && i == 0 && blockIdx.y == 0 && q.seg == 0))) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) static_cast<W*>(s.state)[at + v] = last[v];
+      }
+      if (q.nwv > 1) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = end[v];
+      }
+    }
+    __syncthreads();
+  }
+}
+
+template <class E, bool SIG, int V, int L, bool TV>
+__global__ __launch_bounds__(kThreads) void scan_grad_k(ScanArgs s, ScanPlan p) {
+  typedef typename E::T El;
+  typedef typename E::W W;
+  __shared__ ScanLds<W, V> lds;
+  const Place q = place_of(p);
+  const bool back = !s.c.reverse;
+  for (int64_t blk = blockIdx.x; blk < p.tiles; blk += gridDim.x) {
+    const Job j = job_of<V, TV>(p, q, s.c, blk);
+    const int n = seq_len(s, j.b, q.seg == 0 && blockIdx.y == 0), T = (int)s.c.T;
+    const int64_t at = j.b * s.c.D + j.d;
+    W C[V], h0[V];
+    state_before<W, V>(s, p, q, j, blockIdx.y, s.ds, C, lds);
+#pragma unroll
+    for (int v = 0; v < V; ++v) h0[v] = s.h0 && s.dg.data ? static_cast<const W*>(s.h0)[at + v] : (W)0;
+    const int span = q.nseg * L;
+    const int p0 = (int)blockIdx.y * p.ctiles * span + q.seg * L;
+    for (int i = 0; i < p.ctiles; ++i) {
+      const Where w{first_step<L, TV>(p0 + i * span, T, back), n, T, j.d, back, p.vec != 0};
+      Block<E, V, L, TV> g{}, dy{}, y{}, x{};
+      load(g, s.g, j.b, w);
+      load(dy, s.dy, j.b, w);
+      const int before = s.c.reverse ? 1 : -1;   // from a step to the one whose state it starts from
+      if (s.dg.data) {
+        load(y, s.y, j.b, w, before);
+        if (SIG) load(x, s.x, j.b, w);
+      }
+      W a[V], u[V], end[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) { a[v] = (W)1; u[v] = (W)0; }
+#pragma unroll
+      for (int l = 0; l < L; ++l) {
+        const int t = w.t(l, L);
+        const bool on = t >= 0 && t < n;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          W f, r;
+          gate_of<W, SIG>(g.get(l, v), f, r);
+          const W nu = f * (dy.get(l, v) + u[v]);
+          u[v] = on ? nu : u[v];
+          a[v] = on ? a[v] * f : a[v];
+        }
+      }
+      scan_tile<W, V>(q, a, u, C, end, lds.v[i & 1]);
+      Block<E, V, L, TV> og, ox;
+      W c[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) c[v] = fma_w(a[v], C[v], u[v]);
+#pragma unroll
+      for (int l = 0; l < L; ++l) {
+        const int t = w.t(l, L), tp = t + before;
+        const bool on = t >= 0 && t < n;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          W f, r;
+          gate_of<W, SIG>(g.get(l, v), f, r);
+          const W G = dy.get(l, v) + c[v];
+          const W hp = tp >= 0 && tp < n ? y.get(l, v) : h0[v];
+          const El dx = (El)(on ? r * G : (W)0);
+          const El dg = (El)(on ? (SIG ? G * (hp - x.get(l, v)) * (f * r) : G * hp) : (W)0);
+          c[v] = on ? f * G : c[v];
+          if constexpr (TV) { ox.r[0][l] = dx; og.r[0][l] = dg; }
+          else if constexpr (V == 1) { ox.r[l] = dx; og.r[l] = dg; }
+          else { ox.r[l][v] = dx; og.r[l][v] = dg; }
+        }
+      }
+      if (j.live) {
+        if (s.dg.data) store(og, s.dg, j.b, w);
+        if (s.dx.data) store(ox, s.dx, j.b, w);
+        if (i + 1 == p.ctiles && (int)blockIdx.y + 1 == p.chunks && s.state && q.seg == q.nseg - 1) {
+#pragma unroll
+          for (int v = 0; v < V; ++v) static_cast<W*>(s.state)[at + v] = c[v];
+        }
+      }
+      if (q.nwv > 1) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) C[v] = end[v];
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// A few steps (serving: one): a thread has V channels and takes them in turn.
+template <class E, bool SIG, int V>
+__global__ __launch_bounds__(kThreads) void scan_step_k(ScanArgs s) {
+  typedef typename E::T T;
+  typedef typename E::W W;
+  typedef typename VecOf<T, V>::V Vec;
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x, per = s.c.D / V;
+  if (i >= s.c.B * per) return;
+  const int64_t b = i / per, d = i % per * V, at = b * s.c.D + d;
+  const int n = seq_len(s, b, d == 0);
   const T* g = static_cast<const T*>(s.g.data) + b * s.g.stride_b + d;
   const T* x = static_cast<const T*>(s.x.data) + b * s.x.stride_b + d;
   T* y = static_cast<T*>(s.y.data) + b * s.y.stride_b + d;
-  W h = s.h0 ? static_cast<const W*>(s.h0)[c] : (W)0;
+  W h[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) h[v] = s.h0 ? static_cast<const W*>(s.h0)[at + v] : (W)0;
   for (int64_t p = 0; p < s.c.T; ++p) {
     const int64_t t = s.c.reverse ? s.c.T - 1 - p : p;
-    W out = (W)0;
+    Vec out{};
     if (t < n) {
-      W a, r;
-      gate_of<W, SIG>((W)g[t * s.g.stride_t], a, r);
-      h = a * h + r * (W)x[t * s.x.stride_t];
-      out = h;
-    }
-    if (s.y.data) y[t * s.y.stride_t] = (T)out;
-  }
-  if (s.state) static_cast<W*>(s.state)[c] = h;
-}
-
-template <class E, bool SIG>
-__global__ __launch_bounds__(256) void scan_step_grad_k(ScanArgs s) {
-  typedef typename E::T T;
-  typedef typename E::W W;
-  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (c >= s.c.B * s.c.D) return;
-  const int64_t b = c / s.c.D, d = c % s.c.D, n = seq_len(s, b, d == 0);
-  const T* g = static_cast<const T*>(s.g.data) + b * s.g.stride_b + d;
-  const T* x = static_cast<const T*>(s.x.data) + b * s.x.stride_b + d;
-  const T* y = static_cast<const T*>(s.y.data) + b * s.y.stride_b + d;
-  const T* dy = static_cast<const T*>(s.dy.data) + b * s.dy.stride_b + d;
-  T* dg = static_cast<T*>(s.dg.data) + b * s.dg.stride_b + d;
-  T* dx = static_cast<T*>(s.dx.data) + b * s.dx.stride_b + d;
-  const W h0 = s.h0 ? static_cast<const W*>(s.h0)[c] : (W)0;
-  W C = s.ds ? static_cast<const W*>(s.ds)[c] : (W)0;
-  for (int64_t p = s.c.T - 1; p >= 0; --p) {
-    const int64_t t = s.c.reverse ? s.c.T - 1 - p : p, tp = s.c.reverse ? t + 1 : t - 1;
-    W og = (W)0, ox = (W)0;
-    if (t < n) {
-      W a, r;
-      gate_of<W, SIG>((W)g[t * s.g.stride_t], a, r);
-      const W G = (W)dy[t * s.dy.stride_t] + C;
-      ox = r * G;
-      C = a * G;
-      if (s.dg.data) {
-        const W hp = tp >= 0 && tp < n ? (W)y[tp * s.y.stride_t] : h0;
-        og = SIG ? G * (hp - (W)x[t * s.x.stride_t]) * a * r : G * hp;
+      const Vec gv = *reinterpret_cast<const Vec*>(g + t * s.g.stride_t);
+      const Vec xv = *reinterpret_cast<const Vec*>(x + t * s.x.stride_t);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        W a, r;
+        if constexpr (V == 1) {
+          gate_of<W, SIG>((W)gv, a, r);
+          h[v] = fma_w(a, h[v], r * (W)xv);
+          out = (T)h[v];
+        } else {
+          gate_of<W, SIG>((W)gv[v], a, r);
+          h[v] = fma_w(a, h[v], r * (W)xv[v]);
+          out[v] = (T)h[v];
+        }
       }
     }
-    if (s.dg.data) dg[t * s.dg.stride_t] = (T)og;
-    if (s.dx.data) dx[t * s.dx.stride_t] = (T)ox;
+    if (s.y.data) *reinterpret_cast<Vec*>(y + t * s.y.stride_t) = out;
   }
-  if (s.state) static_cast<W*>(s.state)[c] = C;
+  if (s.state) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) static_cast<W*>(s.state)[at + v] = h[v];
+  }
+}
+
+// ---- plans ------------------------------------------------------------------------------------
+constexpr int kStepT = 4;             // up to this many steps, step after step
+constexpr int kSteps = 4;             // L of 16-byte accesses along the channels
+constexpr int kSteps1 = 16;           // L of single ones
+constexpr int kStepsG = 2, kStepsG1 = 8;   // the same of the gradient, which holds four arrays
+constexpr int kStepsT = 8;            // L along time
+constexpr int kWant = 512;            // workgroups that keep HBM busy
+constexpr int64_t kMaxGrid = 1 << 22;
+
+int ceil_log2(int64_t x) {
+  int r = 0;
+  while (((int64_t)1 << r) < x) ++r;
+  return r;
+}
+
+ScanPlan plan_of(const sim_scan& c, bool grad, bool time, bool vec, int V) {
+  ScanPlan p{};
+  p.time = time;
+  p.vec = vec;
+  int64_t total;   // tiles of a sequence, in time
+  if (time) {
+    p.gs = std::min(8, ceil_log2((c.T + kStepsT - 1) / kStepsT));
+    const int rows = kThreads >> p.gs;
+    p.tiles = (c.B + rows - 1) / rows;
+    p.per = 1;
+    total = ((c.T + kStepsT - 1) / kStepsT + (1 << p.gs) - 1) >> p.gs;
+  } else {
+    const int L = grad ? (vec ? kStepsG : kStepsG1) : (vec ? kSteps : kSteps1);
+    const int64_t wide = (c.D + V - 1) / V;   // threads that the channels need
+    p.lx = std::min(ceil_log2(wide), vec ? 3 : 5);
+    // shorter sequences: more channels and fewer segments
+    while (p.lx < 6 && ((int64_t)1 << p.lx) < wide && (int64_t)(kThreads >> p.lx) * L >= 2 * c.T) ++p.lx;
+    const int64_t chans = (int64_t)V << p.lx, span = (int64_t)(kThreads >> p.lx) * L;
+    p.per = (c.D + chans - 1) / chans;
+    p.tiles = c.B * p.per;
+    total = (c.T + span - 1) / span;
+  }
+  if (total < 1) total = 1;
+  int64_t want = p.tiles ? kWant / p.tiles : 1;
+  if (p.tiles > kWant / 3 || total < 4) want = 1;
+  if (want > total) want = total;
+  p.ctiles = (int)((total + want - 1) / want);
+  p.chunks = (int)((total + p.ctiles - 1) / p.ctiles);
+  return p;
+}
+
+int vec_channels(const sim_scan& c) { return c.dtype == SIM_DT_F64 ? 2 : (c.dtype == SIM_DT_F32 ? 4 : 8); }
+size_t plan_bytes(const sim_scan& c, const ScanPlan& p) {
+  if (p.chunks <= 1) return 0;
+  return (size_t)(p.chunks + 1) * 2 * c.B * c.D * (c.dtype == SIM_DT_F64 ? 8 : 4);
+}
+
+template <class E, bool SIG, int V, int L, int LG, bool TV>
+void run(const ScanArgs& a, bool grad, bool vec, hipStream_t st) {
+  const ScanPlan p = plan_of(a.c, grad, TV, vec, V);
+  const dim3 grid((unsigned)std::min<int64_t>(p.tiles, kMaxGrid), (unsigned)p.chunks), block(kThreads);
+  if (p.chunks > 1) {
+    const dim3 runs((unsigned)p.tiles, (unsigned)p.chunks - 1);
+    if (grad) hipLaunchKernelGGL((scan_runs_k<E, SIG, V, LG, TV, true>), runs, block, 0, st, a, p);
+    else hipLaunchKernelGGL((scan_runs_k<E, SIG, V, L, TV, false>), runs, block, 0, st, a, p);
+  }
+  if (grad) hipLaunchKernelGGL((scan_grad_k<E, SIG, V, LG, TV>), grid, block, 0, st, a, p);
+  else hipLaunchKernelGGL((scan_tile_k<E, SIG, V, L, TV>), grid, block, 0, st, a, p);
+}
+
+// whether every array in use lies on 16-byte boundaries wherever a block may start
+bool vec_ok(const ScanArgs& a, bool time) {
+  const int eb = a.c.dtype == SIM_DT_F64 ? 8 : (a.c.dtype == SIM_DT_F32 ? 4 : 2);
+  for (const sim_seq* q : {&a.g, &a.x, &a.y, &a.dy, &a.dg, &a.dx}) {
+    if (!q->data) continue;
+    if (reinterpret_cast<uintptr_t>(q->data) % 16) return false;
+    if (a.c.B > 1 && q->stride_b * eb % 16) return false;
+    if (time ? q->stride_t != 1 && a.c.T > 1 : a.c.T > 1 && q->stride_t * eb % 16) return false;
+  }
+  return time || a.c.D * eb % 16 == 0;
 }
 
 template <class E, bool SIG>
-hipError_t go(const ScanArgs& a, bool grad, hipStream_t st) {
-  const unsigned nb = (unsigned)((a.c.B * a.c.D + 255) / 256);
-  if (grad) hipLaunchKernelGGL((scan_step_grad_k<E, SIG>), dim3(nb), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((scan_step_k<E, SIG>), dim3(nb), dim3(256), 0, st, a);
+hipError_t go(ScanArgs a, bool grad, hipStream_t st) {
+  constexpr int V = 16 / sizeof(typename E::T);
+  // sequences side by side in every array are channels (lengths apart)
+  bool flat = a.c.B > 1 && !a.len;
+  for (const sim_seq* q : {&a.g, &a.x, &a.y, &a.dy, &a.dg, &a.dx})
+    if (q->data && q->stride_b != a.c.D) flat = false;
+  if (flat) {
+    a.c.D *= a.c.B;
+    a.c.B = 1;
+  }
+  bool time = a.c.D == 1 && a.c.T > 1;
+  for (const sim_seq* q : {&a.g, &a.x, &a.y, &a.dy, &a.dg, &a.dx})
+    if (q->data && q->stride_t > 1) time = false;
+  if (!grad && a.c.T <= kStepT) {
+    const bool v = vec_ok(a, false);
+    const int64_t n = a.c.B * (v ? a.c.D / V : a.c.D);
+    const dim3 grid((unsigned)((n + kThreads - 1) / kThreads)), block(kThreads);
+    if (v) hipLaunchKernelGGL((scan_step_k<E, SIG, V>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((scan_step_k<E, SIG, 1>), grid, block, 0, st, a);
+  } else if (time) {
+    run<E, SIG, 1, kStepsT, kStepsT, true>(a, grad, vec_ok(a, true), st);
+  } else if (vec_ok(a, false)) {
+    run<E, SIG, V, kSteps, kStepsG, false>(a, grad, true, st);
+  } else {
+    run<E, SIG, 1, kSteps1, kStepsG1, false>(a, grad, false, st);
+  }
   return hipGetLastError();
 }
 template <class E>
@@ -106,7 +669,19 @@ hipError_t go(const ScanArgs& a, bool grad, hipStream_t st) {
 
 }  // namespace
 
-size_t scan_work_bytes(const sim_scan&, bool) { return 0; }
+size_t scan_work_bytes(const sim_scan& c, bool grad) {
+  if (!grad && c.T <= kStepT) return 0;
+  size_t need = 0;
+  sim_scan flat = c;   // as one sequence of all channels, if the strides allow it
+  flat.D *= c.B;
+  flat.B = 1;
+  for (const sim_scan& s : {c, flat}) {
+    need = std::max(need, plan_bytes(s, plan_of(s, grad, false, true, vec_channels(s))));
+    need = std::max(need, plan_bytes(s, plan_of(s, grad, false, false, 1)));
+    if (s.D == 1) need = std::max(need, plan_bytes(s, plan_of(s, grad, true, true, 1)));
+  }
+  return need;
+}
 
 hipError_t launch_scan(const ScanArgs& a, bool grad, hipStream_t st) {
   switch (a.c.dtype) {

@@ -80,7 +80,7 @@ def test_common_refusals(stub, name):
 
 def test_scan_refusals(stub):
     bad = [("kind", call("gated_scan", dict(kind=2))), ("reverse", call("gated_scan", dict(reverse=2))),
-           (">= 0", call("gated_scan", dict(T=-1))), ("2^31", call("gated_scan", dict(T=1 << 31))),
+           (">= 0", call("gated_scan", dict(T=-1))), ("2^30", call("gated_scan", dict(T=1 << 30))),
            ("2^31", call("gated_scan", dict(B=1 << 20, D=1 << 20))), ("gate is NULL", call("gated_scan", a0=None)),
            ("x is NULL", call("gated_scan", a1=None)), ("negative", call("gated_scan", a1=[P, -1, 16])),
            ("2^62", call("gated_scan", a1=[P, 1 << 61, 16])), ("share memory", call("gated_scan", a4=seq(3, st=15))),
@@ -148,7 +148,7 @@ def test_every_size_launches_within_limits(stub):
                   **{f"a{i}": [P + (i << 33), t * d, d] for i in ((0, 1, 4) if g == 0 else (0, 1, 2, 3, 7, 8))})
              for g, (b, t, d), dt, k in itertools.product(
                  (0, 1), [(1, 1, 1), (64, 1, 2048), (1, 1000, 256), (512, 2047, 1), (8, 2048, 2048), (1, 65536, 512),
-                          (1, 1, 1 << 30), (1 << 20, 3, 7), (1, 1 << 30, 1), (16, 1025, 1536), (1, 300000, 5)], range(4), (0, 1))]
+                          (1, 1, 1 << 30), (1 << 20, 3, 7), (1, (1 << 30) - 1, 1), (16, 1025, 1536), (1, 300000, 5)], range(4), (0, 1))]
     calls += [call("policy_loss", dict(N=n, A=a, dtype=dt, action_type=t), a0=m(1, n, a), a7=m(2, n, a))
               for (n, a), dt, t, m in itertools.product(
                   [(1, 1), (256, 6), (131072, 96), (2048, 50257), (4096, 131072), ((1 << 31) - 1, 3), (1, (1 << 31) - 1)],
