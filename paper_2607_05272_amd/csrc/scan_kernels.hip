@@ -12,13 +12,14 @@
 // Positions p = 0..T-1 are taken in processing order, t = p, or from the end. Padding is the
 // identity (A, X) = (1, 0), so the state passes through it on either side of a sequence.
 #include <algorithm>
+#include <type_traits>
 
 #include "ops_dev.hpp"
 
 namespace bsim {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kLogThreads = 8, kThreads = 1 << kLogThreads, kWaves = kThreads / 64;
 
 __device__ __forceinline__ float fma_w(float a, float b, float c) { return fmaf(a, b, c); }
 __device__ __forceinline__ double fma_w(double a, double b, double c) { return fma(a, b, c); }
@@ -130,14 +131,37 @@ __device__ __forceinline__ void scan_tile(const Place& q, W (&A)[V], W (&X)[V], 
     __syncthreads();
 #pragma unroll
     for (int v = 0; v < V; ++v) total[v] = carry[v];
-    for (int w = 0; w < q.nwv; ++w) {
-      auto row = lds[q.wave - q.wv + w][q.col];
+    W run[kWaves][V][2];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const auto& row = lds[(q.wave - q.wv + w) & (kWaves - 1)][q.col];
+#pragma unroll
+      for (int v = 0; v < V; ++v) { run[w][v][0] = row[v][0]; run[w][v][1] = row[v][1]; }
+    }
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         carry[v] = w == q.wv ? total[v] : carry[v];
-        total[v] = fma_w(row[v][0], total[v], row[v][1]);
+        total[v] = w < q.nwv ? fma_w(run[w][v][0], total[v], run[w][v][1]) : total[v];
       }
     }
+  }
+}
+
+// N values rounded to the element type, 16-bit ones in pairs
+template <class E, int N>
+__device__ __forceinline__ typename VecOf<typename E::T, N>::V round_to(const typename E::W (&w)[N]) {
+  typedef typename E::W W;
+  if constexpr (N == 1) {
+    return (typename E::T)w[0];
+  } else {
+    typedef W Wide __attribute__((ext_vector_type(N)));
+    Wide v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = w[i];
+    typedef typename E::T Narrow __attribute__((ext_vector_type(N)));
+    return __builtin_bit_cast(typename VecOf<typename E::T, N>::V, __builtin_convertvector(v, Narrow));
   }
 }
 
@@ -153,6 +177,10 @@ struct Block {
     else if constexpr (V == 1) return (W)r[l];
     else return (W)r[l][v];
   }
+  __device__ __forceinline__ void set(int l, const W (&o)[V]) {
+    if constexpr (TV) r[0][l] = (T)o[0];
+    else r[l] = round_to<E, V>(o);
+  }
 };
 
 // Where a thread's block lies: steps t0 + l (or t0 + L - 1 - l, back) of its channels.
@@ -164,11 +192,18 @@ struct Where {
   __device__ __forceinline__ int t(int l, int L) const { return back ? t0 + L - 1 - l : t0 + l; }
 };
 
-// Reads steps t + shift; those outside the sequence read some other step of it (or, where it has none,
-// nothing): the caller does not use them.
+// Whether a thread's steps, and those `shift` from them, all lie in the sequence, for every lane of the wave.
+template <int L>
+__device__ __forceinline__ bool whole(const Where& w, int shift = 0) {
+  const int lo = w.t0 + (shift < 0 ? shift : 0), hi = w.t0 + L + (shift > 0 ? shift : 0);
+  return __all(lo >= 0 && hi <= w.n);
+}
+
+// Reads steps t + shift; those outside the sequence (unless it is `whole` there) read some other step of
+// it (or, where it has none, nothing): the caller does not use them.
 template <class E, int V, int L, bool TV>
 __device__ __forceinline__ void load(Block<E, V, L, TV>& blk, const sim_seq& q, int64_t b, const Where& w,
-                                     int shift = 0) {
+                                     bool whole, int shift = 0) {
   typedef typename E::T T;
   typedef typename Block<E, V, L, TV>::Vec Vec;
   const T* p = static_cast<const T*>(q.data) + b * q.stride_b;
@@ -188,6 +223,11 @@ __device__ __forceinline__ void load(Block<E, V, L, TV>& blk, const sim_seq& q, 
 #pragma unroll
       for (int l = 0; l < L; ++l) blk.r[0][l] = o[L - 1 - l];
     }
+  } else if (whole) {
+    const int64_t step = w.back ? -q.stride_t : q.stride_t;
+    p += (int64_t)(w.t(0, L) + shift) * q.stride_t + w.d;
+#pragma unroll
+    for (int l = 0; l < L; ++l) blk.r[l] = *reinterpret_cast<const Vec*>(p + l * step);
   } else if (w.n > 0) {
 #pragma unroll
     for (int l = 0; l < L; ++l) {
@@ -199,7 +239,8 @@ __device__ __forceinline__ void load(Block<E, V, L, TV>& blk, const sim_seq& q, 
 }
 
 template <class E, int V, int L, bool TV>
-__device__ __forceinline__ void store(const Block<E, V, L, TV>& blk, const sim_seq& q, int64_t b, const Where& w) {
+__device__ __forceinline__ void store(const Block<E, V, L, TV>& blk, const sim_seq& q, int64_t b, const Where& w,
+                                      bool whole) {
   typedef typename E::T T;
   typedef typename Block<E, V, L, TV>::Vec Vec;
   T* p = static_cast<T*>(q.data) + b * q.stride_b;
@@ -216,6 +257,11 @@ __device__ __forceinline__ void store(const Block<E, V, L, TV>& blk, const sim_s
       for (int l = 0; l < L; ++l)
         if (w.t0 + l >= 0 && w.t0 + l < w.T) p[(int64_t)(w.t0 + l) * q.stride_t] = o[l];
     }
+  } else if (whole) {
+    const int64_t step = w.back ? -q.stride_t : q.stride_t;
+    p += (int64_t)w.t(0, L) * q.stride_t + w.d;
+#pragma unroll
+    for (int l = 0; l < L; ++l) *reinterpret_cast<Vec*>(p + l * step) = blk.r[l];
   } else {
 #pragma unroll
     for (int l = 0; l < L; ++l) {
@@ -223,6 +269,13 @@ __device__ __forceinline__ void store(const Block<E, V, L, TV>& blk, const sim_s
       if (t >= 0 && t < w.T) *reinterpret_cast<Vec*>(p + (int64_t)t * q.stride_t + w.d) = blk.r[l];
     }
   }
+}
+
+// f(true) or f(false), so that the usual case is compiled without its conditions
+template <class F>
+__device__ __forceinline__ void either(bool c, F f) {
+  if (c) f(std::true_type{});
+  else f(std::false_type{});
 }
 
 // The block of position p: for one channel whose steps are adjacent, blocks start at multiples
@@ -247,7 +300,7 @@ template <int V, bool TV>
 __device__ __forceinline__ Job job_of(const ScanPlan& p, const Place& q, const sim_scan& c, int64_t blk) {
   Job j;
   if (TV) {
-    j.b = (blk << (8 - p.gs)) + (threadIdx.x >> p.gs);
+    j.b = (blk << (kLogThreads - p.gs)) + (threadIdx.x >> p.gs);
     j.d = 0;
     j.live = j.b < c.B;
     if (!j.live) j.b = c.B - 1;
@@ -306,23 +359,26 @@ __global__ __launch_bounds__(kThreads) void scan_runs_k(ScanArgs s, ScanPlan p) 
   const int p0 = ((int)blockIdx.y * q.nseg + q.seg) * p.ctiles * L;
   for (int i = 0; i < p.ctiles; ++i) {
     Where w{first_step<L, TV>(p0 + i * L, T, back), n, T, j.d, back, p.vec != 0};
+    const bool all = whole<L>(w);
     Block<E, V, L, TV> g{}, x{};
-    load(g, s.g, j.b, w);
-    load(x, GRAD ? s.dy : s.x, j.b, w);
+    load(g, s.g, j.b, w, all);
+    load(x, GRAD ? s.dy : s.x, j.b, w, all);
+    either(all, [&](auto ALL) {
 #pragma unroll
-    for (int l = 0; l < L; ++l) {
-      const int t = w.t(l, L);
-      const bool on = t >= 0 && t < n;
+      for (int l = 0; l < L; ++l) {
+        const int t = w.t(l, L);
+        const bool on = ALL || (t >= 0 && t < n);
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        W a, r;
-        gate_of<W, SIG>(g.get(l, v), a, r);
-        // gradient: C = a (dy + C)
-        const W nx = GRAD ? a * (x.get(l, v) + X[v]) : fma_w(a, X[v], r * x.get(l, v));
-        X[v] = on ? nx : X[v];
-        A[v] = on ? A[v] * a : A[v];
+        for (int v = 0; v < V; ++v) {
+          W a, r;
+          gate_of<W, SIG>(g.get(l, v), a, r);
+          // gradient: C = a (dy + C)
+          const W nx = GRAD ? a * (x.get(l, v) + X[v]) : fma_w(a, X[v], r * x.get(l, v));
+          X[v] = on ? nx : X[v];
+          A[v] = on ? A[v] * a : A[v];
+        }
       }
-    }
+    });
   }
   W carry[V], end[V], run[V];
 #pragma unroll
@@ -348,7 +404,6 @@ __global__ __launch_bounds__(kThreads) void scan_runs_k(ScanArgs s, ScanPlan p) 
 
 template <class E, bool SIG, int V, int L, bool TV>
 __global__ __launch_bounds__(kThreads) void scan_tile_k(ScanArgs s, ScanPlan p) {
-  typedef typename E::T El;
   typedef typename E::W W;
   __shared__ ScanLds<W, V> lds;
   const Place q = place_of(p);
@@ -363,60 +418,70 @@ __global__ __launch_bounds__(kThreads) void scan_tile_k(ScanArgs s, ScanPlan p) 
     const int p0 = (int)blockIdx.y * p.ctiles * span + q.seg * L;
     Where w{first_step<L, TV>(p0, T, back), n, T, j.d, back, p.vec != 0};
     Block<E, V, L, TV> g{}, x{};
-    load(g, s.g, j.b, w);
-    load(x, s.x, j.b, w);
+    bool all = whole<L>(w);
+    load(g, s.g, j.b, w, all);
+    load(x, s.x, j.b, w, all);
     for (int i = 0; i < p.ctiles; ++i) {
       // the segment from a state of 0, and its gates' products
       W A[L][V], X[L][V];
+      either(all, [&](auto ALL) {
 #pragma unroll
-      for (int l = 0; l < L; ++l) {
-        const int t = w.t(l, L);
-        const bool on = t >= 0 && t < n;
+        for (int l = 0; l < L; ++l) {
+          const int t = w.t(l, L);
+          const bool on = ALL || (t >= 0 && t < n);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          W a, r;
-          gate_of<W, SIG>(g.get(l, v), a, r);
-          W u = r * x.get(l, v);
-          a = on ? a : (W)1;
-          u = on ? u : (W)0;
-          A[l][v] = l ? A[l - (l > 0)][v] * a : a;
-          X[l][v] = l ? fma_w(a, X[l - (l > 0)][v], u) : u;
+          for (int v = 0; v < V; ++v) {
+            W a, r;
+            gate_of<W, SIG>(g.get(l, v), a, r);
+            W u = r * x.get(l, v);
+            a = on ? a : (W)1;
+            u = on ? u : (W)0;
+            A[l][v] = l ? A[l - (l > 0)][v] * a : a;
+            X[l][v] = l ? fma_w(a, X[l - (l > 0)][v], u) : u;
+          }
         }
-      }
+      });
       const Where now = w;
+      const bool now_all = all;
       if (i + 1 < p.ctiles) {   // the next tile's loads fly during the scan
         w.t0 = first_step<L, TV>(p0 + (i + 1) * span, T, back);
-        load(g, s.g, j.b, w);
-        load(x, s.x, j.b, w);
+        all = whole<L>(w);
+        load(g, s.g, j.b, w, all);
+        load(x, s.x, j.b, w, all);
       }
       W a[V], u[V], end[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) { a[v] = A[L - 1][v]; u[v] = X[L - 1][v]; }
       scan_tile<W, V>(q, a, u, h, end, lds.v[i & 1]);
       Block<E, V, L, TV> y;
-      W last[V];
-      bool ends = false;   // whether the sequence's last step is here
+      W in[V];
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const W in = fma_w(a[v], h[v], u[v]);
-        last[v] = in;
+      for (int v = 0; v < V; ++v) in[v] = fma_w(a[v], h[v], u[v]);
+      either(now_all, [&](auto ALL) {
 #pragma unroll
         for (int l = 0; l < L; ++l) {
           const int t = now.t(l, L);
-          const bool on = t >= 0 && t < n;
-          const W hl = fma_w(A[l][v], in, X[l][v]);
-          if (on && t == (back ? 0 : n - 1)) {
-            ends = true;
-            last[v] = hl;
-          }
-          const El o = (El)(on ? hl : (W)0);
-          if constexpr (TV) y.r[0][l] = o;
-          else if constexpr (V == 1) y.r[l] = o;
-          else y.r[l][v] = o;
+          const bool on = ALL || (t >= 0 && t < n);
+          W o[V];
+#pragma unroll
+          for (int v = 0; v < V; ++v) o[v] = on ? fma_w(A[l][v], in[v], X[l][v]) : (W)0;
+          y.set(l, o);
         }
-      }
-      if (s.y.data && j.live) store(y, s.y, j.b, now);
-      if (s.state && j.live && (ends || (n == 0 && i == 0 && blockIdx.y == 0 && q.seg == 0))) {
+      });
+      if (s.y.data && j.live) store(y, s.y, j.b, now, now_all);
+      // where the sequence's last step is, the state after it, as y has it
+      const int tl = back ? 0 : n - 1;
+      const bool none = n == 0 && i == 0 && blockIdx.y == 0 && q.seg == 0;
+      if (s.state && j.live && (none || (n > 0 && now.t0 <= tl && tl < now.t0 + L))) {
+        W last[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) last[v] = in[v];
+#pragma unroll
+        for (int l = 0; l < L; ++l) {
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+            last[v] = !none && now.t(l, L) == tl ? fma_w(A[l][v], in[v], X[l][v]) : last[v];
+        }
 #pragma unroll
         for (int v = 0; v < V; ++v) static_cast<W*>(s.state)[at + v] = last[v];
       }
@@ -431,7 +496,6 @@ __global__ __launch_bounds__(kThreads) void scan_tile_k(ScanArgs s, ScanPlan p) 
 
 template <class E, bool SIG, int V, int L, bool TV>
 __global__ __launch_bounds__(kThreads) void scan_grad_k(ScanArgs s, ScanPlan p) {
-  typedef typename E::T El;
   typedef typename E::W W;
   __shared__ ScanLds<W, V> lds;
   const Place q = place_of(p);
@@ -449,55 +513,60 @@ __global__ __launch_bounds__(kThreads) void scan_grad_k(ScanArgs s, ScanPlan p) 
     for (int i = 0; i < p.ctiles; ++i) {
       const Where w{first_step<L, TV>(p0 + i * span, T, back), n, T, j.d, back, p.vec != 0};
       Block<E, V, L, TV> g{}, dy{}, y{}, x{};
-      load(g, s.g, j.b, w);
-      load(dy, s.dy, j.b, w);
       const int before = s.c.reverse ? 1 : -1;   // from a step to the one whose state it starts from
+      const bool all = whole<L>(w, before);
+      load(g, s.g, j.b, w, all);
+      load(dy, s.dy, j.b, w, all);
       if (s.dg.data) {
-        load(y, s.y, j.b, w, before);
-        if (SIG) load(x, s.x, j.b, w);
+        load(y, s.y, j.b, w, all, before);
+        if (SIG) load(x, s.x, j.b, w, all);
       }
       W a[V], u[V], end[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) { a[v] = (W)1; u[v] = (W)0; }
+      either(all, [&](auto ALL) {
 #pragma unroll
-      for (int l = 0; l < L; ++l) {
-        const int t = w.t(l, L);
-        const bool on = t >= 0 && t < n;
+        for (int l = 0; l < L; ++l) {
+          const int t = w.t(l, L);
+          const bool on = ALL || (t >= 0 && t < n);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          W f, r;
-          gate_of<W, SIG>(g.get(l, v), f, r);
-          const W nu = f * (dy.get(l, v) + u[v]);
-          u[v] = on ? nu : u[v];
-          a[v] = on ? a[v] * f : a[v];
+          for (int v = 0; v < V; ++v) {
+            W f, r;
+            gate_of<W, SIG>(g.get(l, v), f, r);
+            const W nu = f * (dy.get(l, v) + u[v]);
+            u[v] = on ? nu : u[v];
+            a[v] = on ? a[v] * f : a[v];
+          }
         }
-      }
+      });
       scan_tile<W, V>(q, a, u, C, end, lds.v[i & 1]);
       Block<E, V, L, TV> og, ox;
       W c[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) c[v] = fma_w(a[v], C[v], u[v]);
+      either(all, [&](auto ALL) {
 #pragma unroll
-      for (int l = 0; l < L; ++l) {
-        const int t = w.t(l, L), tp = t + before;
-        const bool on = t >= 0 && t < n;
+        for (int l = 0; l < L; ++l) {
+          const int t = w.t(l, L), tp = t + before;
+          const bool on = ALL || (t >= 0 && t < n), has = ALL || (tp >= 0 && tp < n);
+          W wg[V], wx[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          W f, r;
-          gate_of<W, SIG>(g.get(l, v), f, r);
-          const W G = dy.get(l, v) + c[v];
-          const W hp = tp >= 0 && tp < n ? y.get(l, v) : h0[v];
-          const El dx = (El)(on ? r * G : (W)0);
-          const El dg = (El)(on ? (SIG ? G * (hp - x.get(l, v)) * (f * r) : G * hp) : (W)0);
-          c[v] = on ? f * G : c[v];
-          if constexpr (TV) { ox.r[0][l] = dx; og.r[0][l] = dg; }
-          else if constexpr (V == 1) { ox.r[l] = dx; og.r[l] = dg; }
-          else { ox.r[l][v] = dx; og.r[l][v] = dg; }
+          for (int v = 0; v < V; ++v) {
+            W f, r;
+            gate_of<W, SIG>(g.get(l, v), f, r);
+            const W G = dy.get(l, v) + c[v];
+            const W hp = has ? y.get(l, v) : h0[v];
+            wx[v] = on ? r * G : (W)0;
+            wg[v] = on ? (SIG ? G * (hp - x.get(l, v)) * (f * r) : G * hp) : (W)0;
+            c[v] = on ? f * G : c[v];
+          }
+          ox.set(l, wx);
+          og.set(l, wg);
         }
-      }
+      });
       if (j.live) {
-        if (s.dg.data) store(og, s.dg, j.b, w);
-        if (s.dx.data) store(ox, s.dx, j.b, w);
+        if (s.dg.data) store(og, s.dg, j.b, w, all);
+        if (s.dx.data) store(ox, s.dx, j.b, w, all);
         if (i + 1 == p.ctiles && (int)blockIdx.y + 1 == p.chunks && s.state && q.seg == q.nseg - 1) {
 #pragma unroll
           for (int v = 0; v < V; ++v) static_cast<W*>(s.state)[at + v] = c[v];
@@ -558,10 +627,12 @@ __global__ __launch_bounds__(kThreads) void scan_step_k(ScanArgs s) {
 
 // ---- plans ------------------------------------------------------------------------------------
 constexpr int kStepT = 4;             // up to this many steps, step after step
-constexpr int kSteps = 4;             // L of 16-byte accesses along the channels
-constexpr int kSteps1 = 16;           // L of single ones
-constexpr int kStepsG = 2, kStepsG1 = 8;   // the same of the gradient, which holds four arrays
+constexpr int kChans = 4;             // channels of an access, at most 16 bytes
+constexpr int kHold = 64;             // bytes of an array that a thread holds so: L steps
+constexpr int kHoldG = 16;            // at most so many elements in the gradient, which holds four arrays
+constexpr int kSteps1 = 16, kStepsG1 = 8;   // L of single elements along the channels
 constexpr int kStepsT = 8;            // L along time
+constexpr int kRow = 128;             // bytes of a step that a workgroup takes: a cache line
 constexpr int kWant = 512;            // workgroups that keep HBM busy
 constexpr int64_t kMaxGrid = 1 << 22;
 
@@ -571,21 +642,28 @@ int ceil_log2(int64_t x) {
   return r;
 }
 
-ScanPlan plan_of(const sim_scan& c, bool grad, bool time, bool vec, int V) {
+int elem_bytes(const sim_scan& c) { return c.dtype == SIM_DT_F64 ? 8 : (c.dtype == SIM_DT_F32 ? 4 : 2); }
+constexpr int vec_channels(int eb) { return kChans * eb < 16 ? kChans : 16 / eb; }
+constexpr int vec_steps(int eb, bool grad) {
+  return (grad && kHold / eb > kHoldG ? kHoldG : kHold / eb) / vec_channels(eb);
+}
+
+ScanPlan plan_of(const sim_scan& c, bool grad, bool time, bool vec) {
+  const int eb = elem_bytes(c), V = time || !vec ? 1 : vec_channels(eb);
   ScanPlan p{};
   p.time = time;
   p.vec = vec;
   int64_t total;   // tiles of a sequence, in time
   if (time) {
-    p.gs = std::min(8, ceil_log2((c.T + kStepsT - 1) / kStepsT));
+    p.gs = std::min(kLogThreads, ceil_log2((c.T + kStepsT - 1) / kStepsT));
     const int rows = kThreads >> p.gs;
     p.tiles = (c.B + rows - 1) / rows;
     p.per = 1;
     total = ((c.T + kStepsT - 1) / kStepsT + (1 << p.gs) - 1) >> p.gs;
   } else {
-    const int L = grad ? (vec ? kStepsG : kStepsG1) : (vec ? kSteps : kSteps1);
+    const int L = vec ? vec_steps(eb, grad) : (grad ? kStepsG1 : kSteps1);
     const int64_t wide = (c.D + V - 1) / V;   // threads that the channels need
-    p.lx = std::min(ceil_log2(wide), vec ? 3 : 5);
+    p.lx = std::min(ceil_log2(wide), vec ? ceil_log2(kRow / (V * eb)) : 5);
     // shorter sequences: more channels and fewer segments
     while (p.lx < 6 && ((int64_t)1 << p.lx) < wide && (int64_t)(kThreads >> p.lx) * L >= 2 * c.T) ++p.lx;
     const int64_t chans = (int64_t)V << p.lx, span = (int64_t)(kThreads >> p.lx) * L;
@@ -602,7 +680,6 @@ ScanPlan plan_of(const sim_scan& c, bool grad, bool time, bool vec, int V) {
   return p;
 }
 
-int vec_channels(const sim_scan& c) { return c.dtype == SIM_DT_F64 ? 2 : (c.dtype == SIM_DT_F32 ? 4 : 8); }
 size_t plan_bytes(const sim_scan& c, const ScanPlan& p) {
   if (p.chunks <= 1) return 0;
   return (size_t)(p.chunks + 1) * 2 * c.B * c.D * (c.dtype == SIM_DT_F64 ? 8 : 4);
@@ -610,7 +687,7 @@ size_t plan_bytes(const sim_scan& c, const ScanPlan& p) {
 
 template <class E, bool SIG, int V, int L, int LG, bool TV>
 void run(const ScanArgs& a, bool grad, bool vec, hipStream_t st) {
-  const ScanPlan p = plan_of(a.c, grad, TV, vec, V);
+  const ScanPlan p = plan_of(a.c, grad, TV, vec);
   const dim3 grid((unsigned)std::min<int64_t>(p.tiles, kMaxGrid), (unsigned)p.chunks), block(kThreads);
   if (p.chunks > 1) {
     const dim3 runs((unsigned)p.tiles, (unsigned)p.chunks - 1);
@@ -621,21 +698,21 @@ void run(const ScanArgs& a, bool grad, bool vec, hipStream_t st) {
   else hipLaunchKernelGGL((scan_tile_k<E, SIG, V, L, TV>), grid, block, 0, st, a, p);
 }
 
-// whether every array in use lies on 16-byte boundaries wherever a block may start
+// whether every array in use is aligned to whole accesses wherever a block may start
 bool vec_ok(const ScanArgs& a, bool time) {
-  const int eb = a.c.dtype == SIM_DT_F64 ? 8 : (a.c.dtype == SIM_DT_F32 ? 4 : 2);
+  const int eb = elem_bytes(a.c), n = time ? 16 : vec_channels(eb) * eb;
   for (const sim_seq* q : {&a.g, &a.x, &a.y, &a.dy, &a.dg, &a.dx}) {
     if (!q->data) continue;
-    if (reinterpret_cast<uintptr_t>(q->data) % 16) return false;
-    if (a.c.B > 1 && q->stride_b * eb % 16) return false;
-    if (time ? q->stride_t != 1 && a.c.T > 1 : a.c.T > 1 && q->stride_t * eb % 16) return false;
+    if (reinterpret_cast<uintptr_t>(q->data) % n) return false;
+    if (a.c.B > 1 && q->stride_b * eb % n) return false;
+    if (time ? q->stride_t != 1 && a.c.T > 1 : a.c.T > 1 && q->stride_t * eb % n) return false;
   }
-  return time || a.c.D * eb % 16 == 0;
+  return time || a.c.D * eb % n == 0;
 }
 
 template <class E, bool SIG>
 hipError_t go(ScanArgs a, bool grad, hipStream_t st) {
-  constexpr int V = 16 / sizeof(typename E::T);
+  constexpr int eb = sizeof(typename E::T), V = vec_channels(eb);
   // sequences side by side in every array are channels (lengths apart)
   bool flat = a.c.B > 1 && !a.len;
   for (const sim_seq* q : {&a.g, &a.x, &a.y, &a.dy, &a.dg, &a.dx})
@@ -656,7 +733,7 @@ hipError_t go(ScanArgs a, bool grad, hipStream_t st) {
   } else if (time) {
     run<E, SIG, 1, kStepsT, kStepsT, true>(a, grad, vec_ok(a, true), st);
   } else if (vec_ok(a, false)) {
-    run<E, SIG, V, kSteps, kStepsG, false>(a, grad, true, st);
+    run<E, SIG, V, vec_steps(eb, false), vec_steps(eb, true), false>(a, grad, true, st);
   } else {
     run<E, SIG, 1, kSteps1, kStepsG1, false>(a, grad, false, st);
   }
@@ -676,9 +753,9 @@ size_t scan_work_bytes(const sim_scan& c, bool grad) {
   flat.D *= c.B;
   flat.B = 1;
   for (const sim_scan& s : {c, flat}) {
-    need = std::max(need, plan_bytes(s, plan_of(s, grad, false, true, vec_channels(s))));
-    need = std::max(need, plan_bytes(s, plan_of(s, grad, false, false, 1)));
-    if (s.D == 1) need = std::max(need, plan_bytes(s, plan_of(s, grad, true, true, 1)));
+    need = std::max(need, plan_bytes(s, plan_of(s, grad, false, true)));
+    need = std::max(need, plan_bytes(s, plan_of(s, grad, false, false)));
+    if (s.D == 1) need = std::max(need, plan_bytes(s, plan_of(s, grad, true, true)));
   }
   return need;
 }
