@@ -1,271 +1,895 @@
 // logit_kernels.hip -- losses over the logits of the caller's network, with their gradients: the
 // clipped policy loss with a KL term, and a router's balance loss.
 //
-// Both need a row's softmax first (its maximum m and S = sum exp(l - m)) and then write a gradient
-// per logit, so the logits are read, reduced and written out again: bound by HBM.
+// With x = l - m of a row's maximum m, e = exp(x) and S = sum e, both gradients are p = e / S times an
+// affine function of something known per element, and their terms follow from S and one more sum:
+//   policy   H = log S - sum(e x) / S,   dl_j = p_j (alpha + beta x_j) + delta [j = action]
+//   balance  s = sum(e f) / S,           dl_j = p_j (f_j - s)
+// So a row is read, reduced once and written: bound by HBM as long as it stays in registers in
+// between. An x below -1000 is taken as -1000: its e is 0 either way, and 0 times a finite number
+// is 0, so -inf logits and masked ones need no case of their own. Maxima keep NaN.
+#include <algorithm>
+
 #include "ops_dev.hpp"
 
 namespace bsim {
 namespace {
 
-constexpr int kRows = 4;            // rows per workgroup, one wave each
 constexpr int kMaxBlocks = 2048;    // workgroups of a loss, each with its partial sums
+constexpr float kLowest = -1000.0f;
 
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-  return v;
+__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
+
+// A part of a row: its maximum m, S = sum e and X = sum e x (policy) or sum e f (balance), with x and e
+// against m. A part of nothing has m = -inf, S = X = 0.
+struct Part { float m, S, X; };
+// the same against the maximum m of a larger part
+template <bool BAL>
+__device__ __forceinline__ Part against(const Part& a, float m) {
+  const float d = m == -INFINITY ? 0.0f : max_nan(a.m - m, kLowest), f = exp_of(d);
+  return Part{m, f * a.S, BAL ? f * a.X : f * fmaf(d, a.S, a.X)};
 }
-template <class W>
-__device__ __forceinline__ W wave_sum(W v) {
+// over 1 << lg adjacent lanes, in every lane
+__device__ __forceinline__ float max_lanes(float m, int lg) {
+  for (int o = 1; o < (1 << lg); o <<= 1) m = max_nan(m, __shfl_xor(m, o));
+  return m;
+}
+__device__ __forceinline__ void add_lanes(float& S, float& X, int lg) {
+  for (int o = 1; o < (1 << lg); o <<= 1) {
+    S += __shfl_xor(S, o);
+    X += __shfl_xor(X, o);
+  }
+}
+__device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
   for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
   return v;
 }
 
-// A sample's loss terms and the derivative q of its loss with respect to logp (without weight).
-struct Terms { float pol, kl, q; };
-__device__ __forceinline__ Terms policy_terms(const sim_policy_loss& c, float logp, const float* old,
-                                              const float* ref, double adv64, int64_t n) {
-  const float adv = (float)adv64;
-  Terms r{0.f, 0.f, 0.f};
-  const float rho = old ? expf(logp - old[n]) : 1.0f;
-  const float lo = 1.0f - c.clip, hi = 1.0f + c.clip;
-  const float rc = fminf(fmaxf(rho, lo), hi);
-  const float s1 = rho * adv, s2 = rc * adv;
-  r.pol = s1 <= s2 ? -s1 : -s2;   // NaN if either is: rc alone may have lost it
-  if (!(s1 == s1)) r.pol = s1;
-  const bool slope = s1 <= s2 || (rho > lo && rho < hi) || !(s1 == s1);
-  r.q = slope ? -s1 : 0.0f;
-  if (ref) {
-    const float d = ref[n] - logp, e = expm1f(d);
-    r.kl = e - d;
-    r.q -= c.c_kl * e;
+struct RowOut { float alpha, beta, delta; };
+struct Sums { double a, b, c; };   // a thread's sums over its rows
+
+// ---- the two losses ----------------------------------------------------------------------------
+struct PolicyOp {
+  static constexpr bool kBal = false;
+  typedef PolicyLossArgs Args;
+  struct Row { float w, adv, old, ref; int64_t act; };
+
+  // what the row has besides its logits; false: it is not looked at
+  __device__ static __forceinline__ bool open(const Args& s, int64_t n, Row& r) {
+    r.w = s.w ? s.w[n] : 1.0f / (float)s.c.N;
+    r.act = load_int(s.act, s.c.action_type, n);
+    r.adv = s.c.adv_type == SIM_DT_F64 ? (float)static_cast<const double*>(s.adv)[n]
+                                       : static_cast<const float*>(s.adv)[n];
+    r.old = s.logp_old ? s.logp_old[n] : 0.0f;
+    r.ref = s.logp_ref ? s.logp_ref[n] : 0.0f;
+    return r.w != 0.0f;
   }
+  // the taken action's logit, -inf if it is out of range or forbidden
+  template <class T>
+  __device__ static __forceinline__ float taken(const Args& s, int64_t n, const Row& r) {
+    if (r.act < 0 || r.act >= s.c.A) return -INFINITY;
+    const uint8_t* mk = static_cast<const uint8_t*>(s.mask.data);
+    if (mk && !mk[n * s.mask.stride_n + r.act * s.mask.stride_a]) return -INFINITY;
+    return (float)static_cast<const T*>(s.l.data)[n * s.l.stride_n + r.act * s.l.stride_a];
+  }
+  // the row's terms and gradient; false: it gives nothing. `first`: this thread keeps its sums
+  __device__ static __forceinline__ bool close(const Args& s, int64_t n, const Row& r, const Part& p, float la,
+                                               bool first, Sums& sums, RowOut& o) {
+    if (p.m == -INFINITY) return false;          // no allowed action
+    if (la == -INFINITY) {
+      if (first) atomicOr(s.err, ERR_ACTION);
+      return false;
+    }
+    const float logS = logf(p.S), logp = (la - p.m) - logS, rS = 1.0f / p.S, H = logS - p.X * rS;
+    const float rho = s.logp_old ? expf(logp - r.old) : 1.0f;
+    const float lo = 1.0f - s.c.clip, hi = 1.0f + s.c.clip;
+    const float s1 = rho * r.adv, s2 = fminf(fmaxf(rho, lo), hi) * r.adv;
+    const bool nan = !(s1 == s1);                // the clipped one alone may have lost it
+    const float pol = s1 <= s2 || nan ? -s1 : -s2;
+    float q = s1 <= s2 || nan || (rho > lo && rho < hi) ? -s1 : 0.0f, kl = 0.0f;
+    if (s.logp_ref) {
+      const float d = r.ref - logp, e = expm1f(d);
+      kl = e - d;
+      q -= s.c.c_kl * e;
+    }
+    const float wr = r.w * rS, ch = s.c.c_entropy;
+    o.alpha = ch > 0.0f ? wr * fmaf(ch, H - logS, -q) : -wr * q;
+    o.beta = wr * ch;
+    o.delta = r.w * q;
+    if (first) {
+      sums.a += (double)r.w * pol;
+      sums.b += (double)r.w * kl;
+      sums.c += (double)r.w * H;
+      if (s.logp) s.logp[n] = logp;
+    }
+    return true;
+  }
+  __device__ static __forceinline__ void shut(const Args& s, int64_t n) {   // a row that gives nothing
+    if (s.logp) s.logp[n] = 0.0f;
+  }
+  __device__ static __forceinline__ void finish(const Args& s, const Sums& v) {
+    s.loss[0] = (float)(v.a + (double)s.c.c_kl * v.b - (double)s.c.c_entropy * v.c);
+    s.loss[1] = (float)v.a;
+    s.loss[2] = (float)v.b;
+    s.loss[3] = (float)v.c;
+  }
+};
+
+// f of a target: coef G / W times its share of the live rows' choices, so that a row's term of the
+// loss is s and its gradient p (f - s). Every workgroup holds it in LDS.
+constexpr int kMaxTargets = 4096;
+// Workgroups that count the choices, each into its own row of the work memory.
+constexpr int kCountBlocks = 64, kCountThreads = 512;
+// the work memory: sums [kMaxBlocks][3] fp64, live rows [kCountBlocks], counts [kCountBlocks][G]
+__device__ __forceinline__ uint32_t* live_parts(const BalanceArgs& s) {
+  return reinterpret_cast<uint32_t*>(static_cast<double*>(s.work) + 3 * kMaxBlocks);
+}
+int count_blocks(int64_t N, int k) {
+  const int64_t b = (N * k + kCountThreads * 4 - 1) / (kCountThreads * 4);
+  return (int)(b < 1 ? 1 : (b > kCountBlocks ? kCountBlocks : b));
+}
+
+struct BalanceOp {
+  static constexpr bool kBal = true;
+  typedef BalanceArgs Args;
+  struct Row { int64_t act; };
+  __device__ static __forceinline__ bool open(const Args& s, int64_t n, Row& r) {
+    r.act = -1;
+    return !s.live || s.live[n];
+  }
+  template <class T>
+  __device__ static __forceinline__ float taken(const Args&, int64_t, const Row&) { return 0.0f; }
+  __device__ static __forceinline__ bool close(const Args&, int64_t, const Row&, const Part& p, float, bool first,
+                                               Sums& sums, RowOut& o) {
+    if (p.m == -INFINITY) return false;
+    const float rS = 1.0f / p.S, si = p.X * rS;
+    o.beta = rS;
+    o.alpha = -si * rS;
+    o.delta = 0.0f;
+    if (first) sums.a += (double)si;
+    return true;
+  }
+  __device__ static __forceinline__ void shut(const Args&, int64_t) {}
+  __device__ static __forceinline__ void finish(const Args& s, const Sums& v) { s.loss[0] = (float)v.a; }
+};
+
+// Fills f [G] from the nb counting workgroups' rows and, in one workgroup, the counts.
+__device__ __forceinline__ void fill_targets(const BalanceArgs& s, int nb, float* f) {
+  const int G = s.c.A / s.c.group;
+  const uint32_t* live = live_parts(s);
+  const uint32_t* cnt = live + kCountBlocks;
+  uint32_t W = 0;
+  for (int b = 0; b < nb; ++b) W += live[b];
+  const double unit = W ? (double)s.c.coef * G / ((double)W * W * s.c.k) : 0.0;
+  for (int g = threadIdx.x; g < G; g += blockDim.x) {
+    uint32_t c = 0;
+#pragma unroll 8
+    for (int b = 0; b < nb; ++b) c += cnt[b * G + g];
+    f[g] = (float)(unit * c);
+    if (blockIdx.x == 0) s.counts[g] = c;
+  }
+  __syncthreads();
+}
+__device__ __forceinline__ void fill_targets(const PolicyLossArgs&, int, float*) {}
+__device__ __forceinline__ float target(const BalanceArgs& s, const float* f, int j) {
+  return f[s.c.group == 1 ? (uint32_t)j : (uint32_t)j / (uint32_t)s.c.group];
+}
+__device__ __forceinline__ float target(const PolicyLossArgs&, const float*, int) { return 0.0f; }
+
+__global__ __launch_bounds__(kCountThreads) void balance_count_k(BalanceArgs s) {
+  __shared__ uint32_t hist[kMaxTargets];
+  __shared__ uint32_t live;
+  const int G = s.c.A / s.c.group;
+  for (int g = threadIdx.x; g < G; g += kCountThreads) hist[g] = 0;
+  if (threadIdx.x == 0) live = 0;
+  __syncthreads();
+  uint32_t mine = 0;
+  const uint32_t k = (uint32_t)s.c.k, total = (uint32_t)(s.c.N * s.c.k);   // below 2^31
+  for (uint32_t i = blockIdx.x * kCountThreads + threadIdx.x; i < total; i += gridDim.x * kCountThreads) {
+    const uint32_t n = k == 1 ? i : i / k;
+    if (s.live && !s.live[n]) continue;
+    if (n * k == i) ++mine;
+    const int64_t a = load_int(s.idx, s.c.index_type, i);
+    if (a >= 0 && a < s.c.A) atomicAdd(&hist[(uint32_t)a / (uint32_t)s.c.group], 1u);
+    else if (a != -1) atomicOr(s.err, ERR_ACTION);
+  }
+  if (mine) atomicAdd(&live, mine);
+  __syncthreads();
+  uint32_t* o = live_parts(s);
+  if (threadIdx.x == 0) o[blockIdx.x] = live;
+  for (int g = threadIdx.x; g < G; g += kCountThreads) o[kCountBlocks + blockIdx.x * G + g] = hist[g];
+}
+
+// A workgroup's sums, in a fixed order: to the work memory, or with one workgroup the loss itself.
+// lds: [waves][3]
+template <class OP>
+__device__ __forceinline__ void leave(const typename OP::Args& s, Sums v, double (*lds)[3]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
+  v.a = wave_sum(v.a);
+  if (!OP::kBal) {
+    v.b = wave_sum(v.b);
+    v.c = wave_sum(v.c);
+  }
+  if (lane == 0) { lds[wave][0] = v.a; lds[wave][1] = v.b; lds[wave][2] = v.c; }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    Sums t{0.0, 0.0, 0.0};
+    for (int w = 0; w < nw; ++w) { t.a += lds[w][0]; t.b += lds[w][1]; t.c += lds[w][2]; }
+    if (gridDim.x == 1) {
+      OP::finish(s, t);
+    } else {
+      double* o = static_cast<double*>(s.work) + 3 * blockIdx.x;
+      o[0] = t.a; o[1] = t.b; o[2] = t.c;
+    }
+  }
+}
+template <class OP>
+__global__ __launch_bounds__(256) void loss_finish_k(typename OP::Args s, int nb) {
+  __shared__ double lds[4][3];
+  const double* w = static_cast<const double*>(s.work);
+  Sums v{0.0, 0.0, 0.0};
+#pragma unroll 8
+  for (int b = threadIdx.x; b < nb; b += 256) {
+    v.a += w[3 * b];
+    v.b += w[3 * b + 1];
+    v.c += w[3 * b + 2];
+  }
+  leave<OP>(s, v, lds);
+}
+
+// ---- rows of adjacent logits -----------------------------------------------------------------
+// N elements of a row, at any alignment of the element type
+template <class E, int N>
+struct Chunk {
+  typedef typename E::T T;
+  typedef T Raw __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+  typedef T Val __attribute__((ext_vector_type(N)));
+  typedef float Wide __attribute__((ext_vector_type(N)));
+  Val v;
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (N == 1) v[0] = p[0];
+    else v = __builtin_bit_cast(Val, *reinterpret_cast<const Raw*>(p));
+  }
+  __device__ __forceinline__ float get(int i) const { return (float)v[i]; }
+  // Keeps the compiler from holding the widened elements of one pass for the next one: they would
+  // take twice the registers (and spill) where the chunks just fit.
+  __device__ __forceinline__ void forget() {
+    if constexpr (N * sizeof(T) == 16) {
+      typedef uint32_t Words __attribute__((ext_vector_type(4)));
+      Words w = __builtin_bit_cast(Words, v);
+      asm volatile("" : "+v"(w));
+      v = __builtin_bit_cast(Val, w);
+    }
+  }
+  __device__ __forceinline__ static void store(T* p, const Wide& w) {
+    if constexpr (N == 1) p[0] = (T)w[0];
+    else *reinterpret_cast<Raw*>(p) = __builtin_bit_cast(Raw, __builtin_convertvector(w, Val));
+  }
+};
+// their mask bytes, at any stride
+template <int N>
+struct MaskBytes {
+  uint32_t w[(N + 3) / 4];
+  __device__ __forceinline__ void load(const uint8_t* p, int64_t stride) {
+    if (N > 1 && stride == 1) {
+      __builtin_memcpy(w, p, N);
+    } else {
+#pragma unroll
+      for (int i = 0; i < (N + 3) / 4; ++i) w[i] = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i / 4] |= (uint32_t)p[i * stride] << (8 * (i % 4));
+    }
+  }
+  __device__ __forceinline__ bool open(int i) const { return (w[i / 4] >> (8 * (i % 4))) & 0xffu; }
+};
+
+// Chunk c of a row of A >= N logits starts at j0. The last one ends with the row: its first `skip`
+// elements belong to the chunk before it too (both write the same values there, but only one adds
+// them up). Chunks past the row's end are all skip, and not written.
+template <int N>
+__device__ __forceinline__ void place(int c, int A, int& j0, int& skip) {
+  const int at = c * N;
+  j0 = at < A - N ? at : A - N;
+  skip = at - j0 < N ? at - j0 : N;
+}
+
+// Rows of up to 4 KB: 1 << lg lanes take a row, R chunks each.
+template <class OP, class E, int N, int R>
+__global__ __launch_bounds__(256) void loss_wave_k(typename OP::Args s, int lg, int nb) {
+  typedef typename E::T T;
+  typedef Chunk<E, N> Ch;
+  __shared__ double lds[4][3];
+  __shared__ float f[OP::kBal ? kMaxTargets : 1];
+  fill_targets(s, nb, f);
+  const int A = s.c.A, gl = threadIdx.x & ((1 << lg) - 1), per = 256 >> lg;
+  int j0[R], skip[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) place<N>(gl + (r << lg), A, j0[r], skip[r]);
+  float fj[OP::kBal ? R : 1][OP::kBal ? N : 1];
+  if constexpr (OP::kBal) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) fj[r][i] = target(s, f, j0[r] + i);
+    }
+  }
+  Sums sums{0.0, 0.0, 0.0};
+  for (int64_t n0 = (int64_t)blockIdx.x * per; n0 < s.c.N; n0 += (int64_t)gridDim.x * per) {
+    const int64_t n = n0 + (threadIdx.x >> lg);
+    const bool in = n < s.c.N;
+    typename OP::Row row;
+    bool on = in && OP::open(s, n, row);
+    Ch ch[R];
+    float la = 0.0f;
+    if (on) {
+      const T* l = static_cast<const T*>(s.l.data) + n * s.l.stride_n;
+#pragma unroll
+      for (int r = 0; r < R; ++r) ch[r].load(l + j0[r]);
+      la = OP::template taken<T>(s, n, row);
+    } else {
+#pragma unroll
+      for (int r = 0; r < R; ++r) ch[r].v = typename Ch::Val{};
+    }
+    float x[R][N];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[r][i] = ch[r].get(i);
+    }
+    if constexpr (!OP::kBal) {
+      if (s.mask.data && on) {
+        const uint8_t* mk = static_cast<const uint8_t*>(s.mask.data) + n * s.mask.stride_n;
+        MaskBytes<N> mb[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) mb[r].load(mk + j0[r] * s.mask.stride_a, s.mask.stride_a);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) x[r][i] = mb[r].open(i) ? x[r][i] : -INFINITY;
+        }
+      }
+    }
+    Part p{-INFINITY, 0.0f, 0.0f};
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) p.m = max_nan(p.m, x[r][i]);
+    }
+    p.m = max_lanes(p.m, lg);
+    const float m = p.m == -INFINITY ? 0.0f : p.m;
+    float e[R][N];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        x[r][i] = max_nan(x[r][i] - m, kLowest);
+        e[r][i] = exp_of(x[r][i]);
+        const float add = i >= skip[r] ? e[r][i] : 0.0f;
+        p.S += add;
+        p.X = fmaf(add, OP::kBal ? fj[OP::kBal ? r : 0][OP::kBal ? i : 0] : x[r][i], p.X);
+      }
+    }
+    add_lanes(p.S, p.X, lg);
+    RowOut o{0.0f, 0.0f, 0.0f};
+    on = on && OP::close(s, n, row, p, la, gl == 0, sums, o);
+    if (in && !on && gl == 0) OP::shut(s, n);
+    if (s.grad.data && in) {
+      T* g = static_cast<T*>(s.grad.data) + n * s.grad.stride_n;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        typename Ch::Wide w;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          w[i] = e[r][i] * fmaf(o.beta, OP::kBal ? fj[OP::kBal ? r : 0][OP::kBal ? i : 0] : x[r][i], o.alpha);
+        if constexpr (!OP::kBal) {
+          const int64_t at = row.act - j0[r];
+          if (at >= 0 && at < N) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] += at == i ? o.delta : 0.0f;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = on ? w[i] : 0.0f;
+        if (skip[r] < N) Ch::store(g + j0[r], w);
+      }
+    }
+  }
+  leave<OP>(s, sums, lds);
+}
+
+// A row's part per wave, joined over the workgroup's NW waves; lds: two uses one after the other take
+// different buffers.
+template <bool BAL, int NW>
+__device__ __forceinline__ Part join_waves(Part p, Part* lds) {
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) lds[wave] = p;
+  __syncthreads();
+  const Part q = lds[(threadIdx.x & 63) % NW];   // a lane holds each wave's part
+  constexpr int lg = NW == 4 ? 2 : (NW == 8 ? 3 : 4);
+  Part r = against<BAL>(q, max_lanes(q.m, lg));
+  add_lanes(r.S, r.X, lg);
   return r;
 }
 
-template <class E>
-__global__ __launch_bounds__(64 * kRows) void policy_row_k(PolicyLossArgs s) {
+// Longer rows: a workgroup takes a row and holds it as it was read, R chunks a thread; while a chunk's
+// gradient goes out the same chunk of the workgroup's next row comes in. Places past the row's end hold
+// -inf.
+template <class E, int NT, int R, bool MASK>
+__global__ __launch_bounds__(NT) void policy_block_k(PolicyLossArgs s) {
+  typedef PolicyOp OP;
   typedef typename E::T T;
-  __shared__ double part[kRows][3];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const T* l = static_cast<const T*>(s.l.data);
+  constexpr int N = 16 / sizeof(T), NW = NT / 64;
+  typedef Chunk<E, N> Ch;
+  __shared__ double lds[NW][3];
+  __shared__ Part parts[2][NW];
+  __shared__ float taken[2];
+  const int A = s.c.A;
   T* g = static_cast<T*>(s.grad.data);
-  const uint8_t* mk = static_cast<const uint8_t*>(s.mask.data);
-  double pol = 0.0, kl = 0.0, ent = 0.0;
-  for (int64_t n = (int64_t)blockIdx.x * kRows + wave; n < s.c.N; n += (int64_t)gridDim.x * kRows) {
-    const float w = s.w ? s.w[n] : 1.0f / (float)s.c.N;
-    auto logit = [&](int64_t j) {
-      if (mk && !mk[n * s.mask.stride_n + j * s.mask.stride_a]) return -INFINITY;
-      return (float)l[n * s.l.stride_n + j * s.l.stride_a];
-    };
-    bool on = w != 0.0f;
-    float m = -INFINITY, S = 0.f, X = 0.f, logp = 0.f, logS = 0.f, H = 0.f;
-    Terms tm{0.f, 0.f, 0.f};
-    int64_t act = -1;
-    if (on) {
-      bool some = false;
-      for (int j = lane; j < s.c.A; j += 64) {
-        const float v = logit(j);
-        some = some || !(v == -INFINITY);
-        m = fmaxf(m, v);
-      }
-      on = __ballot(some) != 0ull;
-      m = wave_max(m);
-    }
-    if (on) {
-      act = load_int(s.act, s.c.action_type, n);
-      const bool ok = act >= 0 && act < s.c.A && !(logit(act) == -INFINITY);
-      if (!ok) {
-        if (lane == 0) atomicOr(s.err, ERR_ACTION);
-        on = false;
-      }
-    }
-    if (on) {
-      for (int j = lane; j < s.c.A; j += 64) {
-        const float v = logit(j);
-        const float e = v == -INFINITY ? 0.0f : expf(v - m);
-        S += e;
-        if (e != 0.0f) X += e * (v - m);
-      }
-      S = wave_sum(S);
-      X = wave_sum(X);
-      logS = logf(S);
-      logp = (logit(act) - m) - logS;
-      H = logS - X / S;
-      const double adv = s.c.adv_type == SIM_DT_F64 ? static_cast<const double*>(s.adv)[n]
-                                                    : (double)static_cast<const float*>(s.adv)[n];
-      tm = policy_terms(s.c, logp, s.logp_old, s.logp_ref, adv, n);
-      pol += (double)w * tm.pol;
-      kl += (double)w * tm.kl;
-      ent += (double)w * H;
-    }
-    if (lane == 0 && s.logp) s.logp[n] = logp;
-    if (!g) continue;
-    for (int j = lane; j < s.c.A; j += 64) {
-      float o = 0.0f;
-      if (on) {
-        const float v = logit(j);
-        if (!(v == -INFINITY)) {
-          const float lp = (v - m) - logS, p = expf(lp);
-          o = tm.q * ((j == act ? 1.0f : 0.0f) - p);
-          if (s.c.c_entropy > 0.0f && p > 0.0f) o += s.c.c_entropy * (p * (lp + H));
-          o *= w;
+  Ch ch[R];
+  MaskBytes<N> mb[MASK ? R : 1];
+  const T none = (T)-INFINITY;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) ch[r].v[i] = none;
+  }
+  // chunk r of row n; at: its first element
+  auto fetch = [&](int r, int at, int64_t n) {
+    const T* l = static_cast<const T*>(s.l.data) + n * s.l.stride_n;
+    const uint8_t* mk = nullptr;
+    if constexpr (MASK) mk = static_cast<const uint8_t*>(s.mask.data) + n * s.mask.stride_n;
+    if (at + N <= A) {
+      ch[r].load(l + (uint32_t)at);
+      if constexpr (MASK) mb[r].load(mk + at * s.mask.stride_a, s.mask.stride_a);
+    } else if (at < A) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        ch[r].v[i] = at + i < A ? l[at + i] : none;
+        if constexpr (MASK) {
+          if (i % 4 == 0) mb[r].w[i / 4] = 0;
+          if (at + i < A) mb[r].w[i / 4] |= (uint32_t)mk[(at + i) * s.mask.stride_a] << (8 * (i % 4));
         }
       }
-      g[n * s.grad.stride_n + j * s.grad.stride_a] = (T)o;
+    }
+  };
+  auto value = [&](int r, int i) {
+    const float v = ch[r].get(i);
+    if constexpr (MASK) return mb[r].open(i) ? v : -INFINITY;
+    else return v;
+  };
+  Sums sums{0.0, 0.0, 0.0};
+  OP::Row row, next;
+  bool on = false, on_next = false;
+  const int64_t step = gridDim.x;
+  if (blockIdx.x < s.c.N) on_next = OP::open(s, blockIdx.x, next);
+  if (on_next) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) fetch(r, (threadIdx.x + r * NT) * N, blockIdx.x);
+  }
+  int use = 0;
+  for (int64_t n = blockIdx.x; n < s.c.N; n += step) {
+    row = next;
+    on = on_next;
+    on_next = n + step < s.c.N && OP::open(s, n + step, next);
+    RowOut o{0.0f, 0.0f, 0.0f};
+    float m = 0.0f;
+    if (on) {   // the same in the whole workgroup
+      if (threadIdx.x == 0) taken[use] = OP::template taken<T>(s, n, row);
+      Part p{-INFINITY, 0.0f, 0.0f};
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (r * NT * N < A) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) p.m = max_nan(p.m, value(r, i));
+        }
+      }
+      p.m = max_lanes(p.m, 6);
+      m = p.m == -INFINITY ? 0.0f : p.m;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (r * NT * N < A) {
+          ch[r].forget();
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const float x = max_nan(value(r, i) - m, kLowest), e = exp_of(x);
+            p.S += e;
+            p.X = fmaf(e, x, p.X);
+          }
+        }
+      }
+      add_lanes(p.S, p.X, 6);
+      p = join_waves<false, NW>(p, parts[use]);
+      on = OP::close(s, n, row, p, taken[use], threadIdx.x == 0, sums, o);
+      m = p.m;
+      use ^= 1;   // only a row with a barrier between frees the other buffer
+    }
+    if (!on && threadIdx.x == 0) OP::shut(s, n);
+    int at0 = threadIdx.x * N;
+    asm volatile("" : "+v"(at0));   // the chunks' places are found again, not held from row to row
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int at = at0 + r * NT * N;
+      if (g && at < A) {
+        ch[r].forget();
+        T* out = g + n * s.grad.stride_n;
+        typename Ch::Wide w;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float x = max_nan(value(r, i) - m, kLowest);
+          w[i] = exp_of(x) * fmaf(o.beta, x, o.alpha);
+        }
+        const int64_t hit = row.act - at;
+        if (hit >= 0 && hit < N) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) w[i] += hit == i ? o.delta : 0.0f;
+        }
+        if (!on) w = typename Ch::Wide{};
+        if (at + N <= A) {
+          Ch::store(out + (uint32_t)at, w);
+        } else {
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+            if (at + i < A) out[at + i] = (T)w[i];
+        }
+      }
+      if (on_next) fetch(r, at, n + step);
     }
   }
-  if (lane == 0) { part[wave][0] = pol; part[wave][1] = kl; part[wave][2] = ent; }
-  __syncthreads();
-  if (threadIdx.x < 3) {
-    double v = 0.0;
-    for (int i = 0; i < kRows; ++i) v += part[i][threadIdx.x];
-    static_cast<double*>(s.work)[3 * blockIdx.x + threadIdx.x] = v;
-  }
+  leave<OP>(s, sums, lds);
 }
 
-// the workgroups' sums, in a fixed order
-__global__ __launch_bounds__(64) void policy_finish_k(PolicyLossArgs s, int nb) {
-  const double* w = static_cast<const double*>(s.work);
-  double v[3] = {0.0, 0.0, 0.0};
-  for (int b = threadIdx.x; b < nb; b += 64)
-    for (int i = 0; i < 3; ++i) v[i] += w[3 * b + i];
-  for (int i = 0; i < 3; ++i) v[i] = wave_sum(v[i]);
-  if (threadIdx.x == 0) {
-    s.loss[0] = (float)(v[0] + (double)s.c.c_kl * v[1] - (double)s.c.c_entropy * v[2]);
-    for (int i = 0; i < 3; ++i) s.loss[1 + i] = (float)v[i];
-  }
-}
-
-int loss_blocks(int64_t N) {
-  const int64_t b = (N + kRows - 1) / kRows;
-  return (int)(b < 1 ? 1 : (b > kMaxBlocks ? kMaxBlocks : b));
-}
-
-// ---- balance loss ----------------------------------------------------------------------------
-// work: per-workgroup sums [kMaxBlocks] fp64, then the live rows (one 64-bit integer)
-__device__ __forceinline__ unsigned long long* live_count(const BalanceArgs& s) {
-  return reinterpret_cast<unsigned long long*>(static_cast<double*>(s.work) + kMaxBlocks);
-}
-
-__global__ __launch_bounds__(256) void balance_zero_k(BalanceArgs s, int G) {
-  for (int i = threadIdx.x; i < G; i += 256) s.counts[i] = 0;
-  if (threadIdx.x == 0) *live_count(s) = 0ull;
-}
-
-__global__ __launch_bounds__(256) void balance_count_k(BalanceArgs s) {
-  for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < s.c.N; n += (int64_t)gridDim.x * 256) {
-    if (s.live && !s.live[n]) continue;
-    atomicAdd(live_count(s), 1ull);
-    for (int i = 0; i < s.c.k; ++i) {
-      const int64_t a = load_int(s.idx, s.c.index_type, n * s.c.k + i);
-      if (a >= 0 && a < s.c.A)
-        atomicAdd(reinterpret_cast<unsigned long long*>(s.counts) + a / s.c.group, 1ull);
-      else if (a != -1)
-        atomicOr(s.err, ERR_ACTION);
-    }
-  }
-}
-
-template <class E>
-__global__ __launch_bounds__(64 * kRows) void balance_row_k(BalanceArgs s) {
+// Rows that no workgroup's registers hold: read twice.
+constexpr int kStream = 1024;
+template <class OP, class E>
+__global__ __launch_bounds__(kStream) void loss_stream_k(typename OP::Args s, int nb) {
   typedef typename E::T T;
-  __shared__ double part[kRows];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const T* l = static_cast<const T*>(s.l.data);
+  constexpr int N = 16 / sizeof(T), NW = kStream / 64, U = 4;
+  typedef Chunk<E, N> Ch;
+  __shared__ double lds[NW][3];
+  __shared__ Part parts[2][NW];
+  __shared__ float taken[2];
+  __shared__ float f[OP::kBal ? kMaxTargets : 1];
+  fill_targets(s, nb, f);
+  const int A = s.c.A, whole = A / N;
   T* g = static_cast<T*>(s.grad.data);
-  const double W = (double)*live_count(s);
-  const float scale = W > 0.0 ? (float)((double)s.c.coef * (s.c.A / s.c.group) / W) : 0.0f;
-  const float fk = W > 0.0 ? (float)(1.0 / (W * s.c.k)) : 0.0f;
-  double acc = 0.0;
-  for (int64_t n = (int64_t)blockIdx.x * kRows + wave; n < s.c.N; n += (int64_t)gridDim.x * kRows) {
-    bool on = !s.live || s.live[n];
-    float m = -INFINITY, S = 0.f, X = 0.f;
-    if (on) {
-      bool some = false;
-      for (int j = lane; j < s.c.A; j += 64) {
-        const float v = (float)l[n * s.l.stride_n + j * s.l.stride_a];
-        some = some || !(v == -INFINITY);
-        m = fmaxf(m, v);
-      }
-      on = __ballot(some) != 0ull;
-      m = wave_max(m);
+  Sums sums{0.0, 0.0, 0.0};
+  int use = 0;
+  for (int64_t n = blockIdx.x; n < s.c.N; n += gridDim.x) {
+    typename OP::Row row;
+    bool on = OP::open(s, n, row);
+    const T* l = static_cast<const T*>(s.l.data) + n * s.l.stride_n;
+    const uint8_t* mk = nullptr;
+    int64_t ms = 0;
+    if constexpr (!OP::kBal) {
+      if (s.mask.data) mk = static_cast<const uint8_t*>(s.mask.data) + n * s.mask.stride_n;
+      ms = s.mask.stride_a;
     }
+    auto factor = [&](int j, float x) { return OP::kBal ? target(s, f, j) : x; };
+    RowOut o{0.0f, 0.0f, 0.0f};
+    float m = 0.0f;
     if (on) {
-      for (int j = lane; j < s.c.A; j += 64) {
-        const float v = (float)l[n * s.l.stride_n + j * s.l.stride_a];
-        const float e = v == -INFINITY ? 0.0f : expf(v - m);
-        S += e;
-        X += e * (fk * (float)s.counts[j / s.c.group]);
+      if (threadIdx.x == 0) taken[use] = OP::template taken<T>(s, n, row);
+      Part p{-INFINITY, 0.0f, 0.0f};
+      auto one = [&](int j, float v) {   // an element, against the maximum so far
+        const float M = max_nan(p.m, v);
+        p = against<OP::kBal>(p, M);
+        const float x = M == -INFINITY ? kLowest : max_nan(v - M, kLowest), e = exp_of(x);
+        p.S += e;
+        p.X = fmaf(e, factor(j, x), p.X);
+      };
+      for (int c0 = threadIdx.x; c0 < whole; c0 += U * kStream) {
+        Ch ch[U];
+        MaskBytes<N> mb[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int c = c0 + u * kStream;
+          if (c < whole) {
+            ch[u].load(l + c * N);
+            if (mk) mb[u].load(mk + (int64_t)c * N * ms, ms);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int c = c0 + u * kStream;
+          if (c >= whole) continue;
+          float v[N], M = p.m;
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            v[i] = !mk || mb[u].open(i) ? ch[u].get(i) : -INFINITY;
+            M = max_nan(M, v[i]);
+          }
+          if (M == -INFINITY) continue;
+          p = against<OP::kBal>(p, M);
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const float x = max_nan(v[i] - M, kLowest), e = exp_of(x);
+            p.S += e;
+            p.X = fmaf(e, factor(c * N + i, x), p.X);
+          }
+        }
       }
-      S = wave_sum(S);
-      X = wave_sum(X) / S;
-      acc += (double)X;
+      for (int j = whole * N + threadIdx.x; j < A; j += kStream) one(j, !mk || mk[j * ms] ? (float)l[j] : -INFINITY);
+      const float wm = max_lanes(p.m, 6);
+      p = against<OP::kBal>(p, wm);
+      add_lanes(p.S, p.X, 6);
+      p = join_waves<OP::kBal, NW>(p, parts[use]);
+      on = OP::close(s, n, row, p, taken[use], threadIdx.x == 0, sums, o);
+      m = p.m;
+      use ^= 1;
     }
+    if (!on && threadIdx.x == 0) OP::shut(s, n);
     if (!g) continue;
-    for (int j = lane; j < s.c.A; j += 64) {
-      float o = 0.0f;
-      if (on) {
-        const float v = (float)l[n * s.l.stride_n + j * s.l.stride_a];
-        const float p = v == -INFINITY ? 0.0f : expf(v - m) / S;
-        o = scale * p * (fk * (float)s.counts[j / s.c.group] - X);
+    T* out = g + n * s.grad.stride_n;
+    auto slope = [&](int j, float v) {
+      const float x = max_nan(v - m, kLowest);
+      const float w = exp_of(x) * fmaf(o.beta, factor(j, x), o.alpha);
+      return on ? (row.act == j ? w + o.delta : w) : 0.0f;
+    };
+    for (int c0 = threadIdx.x; c0 < whole; c0 += U * kStream) {
+      Ch ch[U];
+      MaskBytes<N> mb[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = c0 + u * kStream;
+        if (c < whole && on) {
+          ch[u].load(l + c * N);
+          if (mk) mb[u].load(mk + (int64_t)c * N * ms, ms);
+        }
       }
-      g[n * s.grad.stride_n + j * s.grad.stride_a] = (T)o;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = c0 + u * kStream;
+        if (c >= whole) continue;
+        typename Ch::Wide w{};
+        if (on) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) w[i] = slope(c * N + i, !mk || mb[u].open(i) ? ch[u].get(i) : -INFINITY);
+        }
+        Ch::store(out + c * N, w);
+      }
     }
+    for (int j = whole * N + threadIdx.x; j < A; j += kStream)
+      out[j] = (T)(on ? slope(j, !mk || mk[j * ms] ? (float)l[j] : -INFINITY) : 0.0f);
   }
-  if (lane == 0) part[wave] = acc;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    double v = 0.0;
-    for (int i = 0; i < kRows; ++i) v += part[i];
-    static_cast<double*>(s.work)[blockIdx.x] = v;
-  }
+  leave<OP>(s, sums, lds);
 }
 
-__global__ __launch_bounds__(64) void balance_finish_k(BalanceArgs s, int nb) {
-  const double* w = static_cast<const double*>(s.work);
-  double v = 0.0;
-  for (int b = threadIdx.x; b < nb; b += 64) v += w[b];
-  v = wave_sum(v);
-  const double W = (double)*live_count(s);
-  if (threadIdx.x == 0)
-    s.loss[0] = W > 0.0 ? (float)(v * ((double)s.c.coef * (s.c.A / s.c.group) / W)) : 0.0f;
+// ---- logits of adjacent samples: [A][N] --------------------------------------------------------
+// A lane takes a sample; 1 << lw waves share 64 samples, each with up to R of the actions.
+template <class OP, class E, int NT, int R>
+__global__ __launch_bounds__(NT) void loss_cols_k(typename OP::Args s, int lw, int nb) {
+  typedef typename E::T T;
+  __shared__ double lds[NT / 64][3];
+  __shared__ Part parts[2][NT / 64][64];
+  __shared__ float taken[2][64];
+  __shared__ float f[OP::kBal ? kMaxTargets : 1];
+  fill_targets(s, nb, f);
+  const int A = s.c.A, lane = threadIdx.x & 63, W = 1 << lw;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // the same in all of a wave's lanes
+  const int mine = (A - (wave & (W - 1)) + W - 1) >> lw;   // actions of this wave
+  const int wa = wave & (W - 1), grp = wave >> lw, per = (blockDim.x >> 6 >> lw) * 64;
+  Sums sums{0.0, 0.0, 0.0};
+  int use = 0;
+  for (int64_t n0 = (int64_t)blockIdx.x * per; n0 < s.c.N; n0 += (int64_t)gridDim.x * per, use ^= 1) {
+    const int64_t n = n0 + grp * 64 + lane;
+    const bool in = n < s.c.N;
+    typename OP::Row row;
+    bool on = in && OP::open(s, n, row);
+    float x[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) x[i] = -INFINITY;
+    if (on) {
+      const T* l = static_cast<const T*>(s.l.data) + n * s.l.stride_n + wa * s.l.stride_a;
+#pragma unroll
+      for (int i = 0; i < R; ++i, l += s.l.stride_a << lw)
+        if (i < mine) x[i] = (float)*l;
+      if constexpr (!OP::kBal) {
+        if (s.mask.data) {
+          const uint8_t* mk = static_cast<const uint8_t*>(s.mask.data) + n * s.mask.stride_n + wa * s.mask.stride_a;
+          uint8_t open[R];
+#pragma unroll
+          for (int i = 0; i < R; ++i, mk += s.mask.stride_a << lw) open[i] = i < mine ? *mk : 0;
+#pragma unroll
+          for (int i = 0; i < R; ++i) x[i] = open[i] ? x[i] : -INFINITY;
+        }
+      }
+    }
+    float la = 0.0f;
+    // read by the wave that writes it, before it does
+    if (on && (OP::kBal || (row.act & (W - 1)) == wa)) {
+      la = OP::template taken<T>(s, n, row);
+      if (W > 1) taken[use][grp * 64 + lane] = la;
+    }
+    Part p{-INFINITY, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < R; ++i) p.m = max_nan(p.m, x[i]);
+    float m = p.m == -INFINITY ? 0.0f : p.m;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const float d = max_nan(x[i] - m, kLowest), e = exp_of(d);
+      p.S += e;
+      p.X = fmaf(e, OP::kBal ? (i < mine ? target(s, f, wa + (i << lw)) : 0.0f) : d, p.X);
+    }
+    if (W > 1) {
+      parts[use][wave][lane] = p;
+      __syncthreads();
+      float M = p.m;
+      for (int w = 0; w < W; ++w) M = max_nan(M, parts[use][(grp << lw) + w][lane].m);
+      Part t{M, 0.0f, 0.0f};
+      for (int w = 0; w < W; ++w) {
+        const Part q = against<OP::kBal>(parts[use][(grp << lw) + w][lane], M);
+        t.S += q.S;
+        t.X += q.X;
+      }
+      p = t;
+      la = taken[use][grp * 64 + lane];
+      m = p.m == -INFINITY ? 0.0f : p.m;
+    }
+    RowOut o{0.0f, 0.0f, 0.0f};
+    on = on && OP::close(s, n, row, p, la, wa == 0, sums, o);
+    if (in && !on && wa == 0) OP::shut(s, n);
+    if (s.grad.data && in) {
+      T* g = static_cast<T*>(s.grad.data) + n * s.grad.stride_n + wa * s.grad.stride_a;
+#pragma unroll
+      for (int i = 0; i < R; ++i, g += s.grad.stride_a << lw) {
+        if (i < mine) {
+          const int a = wa + (i << lw);
+          const float d = max_nan(x[i] - m, kLowest);
+          float w = exp_of(d) * fmaf(o.beta, OP::kBal ? target(s, f, a) : d, o.alpha);
+          if (!OP::kBal && row.act == a) w += o.delta;
+          *g = (T)(on ? w : 0.0f);
+        }
+      }
+    }
+  }
+  __syncthreads();
+  leave<OP>(s, sums, lds);
+}
+
+// More actions than the waves of a workgroup hold (or rows of any strides): a lane takes a sample and
+// reads it three times.
+template <class OP, class E>
+__global__ __launch_bounds__(64) void loss_lane_k(typename OP::Args s, int nb) {
+  typedef typename E::T T;
+  __shared__ double lds[1][3];
+  __shared__ float f[OP::kBal ? kMaxTargets : 1];
+  fill_targets(s, nb, f);
+  Sums sums{0.0, 0.0, 0.0};
+  for (int64_t n = (int64_t)blockIdx.x * 64 + threadIdx.x; n < s.c.N; n += (int64_t)gridDim.x * 64) {
+    typename OP::Row row;
+    bool on = OP::open(s, n, row);
+    const T* l = static_cast<const T*>(s.l.data) + n * s.l.stride_n;
+    auto logit = [&](int a) {
+      if constexpr (!OP::kBal) {
+        if (s.mask.data &&
+            !static_cast<const uint8_t*>(s.mask.data)[n * s.mask.stride_n + a * s.mask.stride_a]) return -INFINITY;
+      }
+      return (float)l[a * s.l.stride_a];
+    };
+    Part p{-INFINITY, 0.0f, 0.0f};
+    RowOut o{0.0f, 0.0f, 0.0f};
+    if (on) {
+#pragma unroll 8
+      for (int a = 0; a < s.c.A; ++a) p.m = max_nan(p.m, logit(a));
+      const float m = p.m == -INFINITY ? 0.0f : p.m;
+#pragma unroll 8
+      for (int a = 0; a < s.c.A; ++a) {
+        const float x = max_nan(logit(a) - m, kLowest), e = exp_of(x);
+        p.S += e;
+        p.X = fmaf(e, OP::kBal ? target(s, f, a) : x, p.X);
+      }
+      on = OP::close(s, n, row, p, OP::template taken<T>(s, n, row), true, sums, o);
+    }
+    if (!on) OP::shut(s, n);
+    if (s.grad.data) {
+      T* g = static_cast<T*>(s.grad.data) + n * s.grad.stride_n;
+#pragma unroll 8
+      for (int a = 0; a < s.c.A; ++a) {
+        float w = 0.0f;
+        if (on) {
+          const float x = max_nan(logit(a) - p.m, kLowest);
+          w = exp_of(x) * fmaf(o.beta, OP::kBal ? target(s, f, a) : x, o.alpha);
+          if (!OP::kBal && row.act == a) w += o.delta;
+        }
+        g[a * s.grad.stride_a] = (T)w;
+      }
+    }
+  }
+  leave<OP>(s, sums, lds);
+}
+
+// ---- choice of the form -------------------------------------------------------------------------
+int ceil_log2(int64_t x) {
+  int r = 0;
+  while (((int64_t)1 << r) < x) ++r;
+  return r;
+}
+int blocks_for(int64_t N, int per, int most) {
+  const int64_t b = (N + per - 1) / per;
+  return (int)(b < 1 ? 1 : (b > most ? most : b));
+}
+
+// Launches the form for these sizes and strides; the workgroups that left sums.
+template <class OP, class E>
+int launch_rows(const typename OP::Args& a, int nb, hipStream_t st) {
+  constexpr int N = 16 / sizeof(typename E::T);
+  const int A = a.c.A;
+  const int64_t rows = a.c.N;
+  const bool adjacent = (a.l.stride_a == 1 || A == 1) && (!a.grad.data || a.grad.stride_a == 1 || A == 1);
+  if (!adjacent) {
+    // waves that share a sample so that each holds at most 24 of its actions
+    const int lw = ceil_log2((A + 23) / 24);
+    if (lw > 4) {
+      const int g = blocks_for(rows, 64, kMaxBlocks);
+      hipLaunchKernelGGL((loss_lane_k<OP, E>), dim3(g), dim3(64), 0, st, a, nb);
+      return g;
+    }
+    const int threads = lw > 2 ? 64 << lw : 256, per = threads >> lw, g = blocks_for(rows, per, kMaxBlocks);
+    const int need = (A + (1 << lw) - 1) >> lw;
+    const dim3 grid(g), block(threads);
+    if (need <= 8) hipLaunchKernelGGL((loss_cols_k<OP, E, 256, 8>), grid, block, 0, st, a, lw, nb);
+    else if (threads == 256) hipLaunchKernelGGL((loss_cols_k<OP, E, 256, 24>), grid, block, 0, st, a, lw, nb);
+    else hipLaunchKernelGGL((loss_cols_k<OP, E, 1024, 24>), grid, block, 0, st, a, lw, nb);
+    return g;
+  }
+  const int chunks = (A + N - 1) / N;
+  if (A < N || chunks <= 256) {
+    // lanes of a row: enough to hold it in one chunk each, or for the longer ones two or four
+    const int lg = A < N ? ceil_log2(A) : std::min(6, ceil_log2(chunks));
+    const int need = A < N ? 1 : (chunks + (1 << lg) - 1) >> lg;
+    const int g = blocks_for(rows, 256 >> lg, kMaxBlocks);
+    const dim3 grid(g), block(256);
+    if (A < N) hipLaunchKernelGGL((loss_wave_k<OP, E, 1, 1>), grid, block, 0, st, a, lg, nb);
+    else if (need == 1) hipLaunchKernelGGL((loss_wave_k<OP, E, N, 1>), grid, block, 0, st, a, lg, nb);
+    else if (need == 2) hipLaunchKernelGGL((loss_wave_k<OP, E, N, 2>), grid, block, 0, st, a, lg, nb);
+    else hipLaunchKernelGGL((loss_wave_k<OP, E, N, 4>), grid, block, 0, st, a, lg, nb);
+    return g;
+  }
+  if constexpr (!OP::kBal) {
+    auto go = [&](auto kern, int threads, int most) {
+      const int g = blocks_for(rows, 1, most);
+      hipLaunchKernelGGL(kern, dim3(g), dim3(threads), 0, st, a);
+      return g;
+    };
+    if (a.mask.data) {
+      if (chunks <= 1024) return go(policy_block_k<E, 256, 4, true>, 256, 2048);
+      if (chunks <= 4096) return go(policy_block_k<E, 512, 8, true>, 512, 1024);
+      if (chunks <= 8192) return go(policy_block_k<E, 1024, 8, true>, 1024, 512);
+    } else {
+      if (chunks <= 1024) return go(policy_block_k<E, 256, 4, false>, 256, 2048);
+      if (chunks <= 4096) return go(policy_block_k<E, 512, 8, false>, 512, 1024);
+      if (chunks <= 8192) return go(policy_block_k<E, 1024, 8, false>, 1024, 512);
+      if (chunks <= 16384) return go(policy_block_k<E, 1024, 16, false>, 1024, 512);
+    }
+  }
+  const int g = blocks_for(rows, 1, 512);
+  hipLaunchKernelGGL((loss_stream_k<OP, E>), dim3(g), dim3(kStream), 0, st, a, nb);
+  return g;
+}
+template <class OP>
+hipError_t launch_loss(const typename OP::Args& a, int nb, hipStream_t st) {
+  const int g = a.c.dtype == SIM_DT_F32 ? launch_rows<OP, F32>(a, nb, st)
+                : a.c.dtype == SIM_DT_BF16 ? launch_rows<OP, BF16>(a, nb, st) : launch_rows<OP, F16>(a, nb, st);
+  if (g > 1) hipLaunchKernelGGL(loss_finish_k<OP>, dim3(1), dim3(256), 0, st, a, g);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 size_t policy_loss_bytes(const sim_policy_loss&) { return (size_t)kMaxBlocks * 3 * sizeof(double); }
 
-hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st) {
-  const int nb = loss_blocks(a.c.N);
-  const dim3 grid(nb), block(64 * kRows);
-  switch (a.c.dtype) {
-    case SIM_DT_F32: hipLaunchKernelGGL(policy_row_k<F32>, grid, block, 0, st, a); break;
-    case SIM_DT_BF16: hipLaunchKernelGGL(policy_row_k<BF16>, grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL(policy_row_k<F16>, grid, block, 0, st, a); break;
-  }
-  hipLaunchKernelGGL(policy_finish_k, dim3(1), dim3(64), 0, st, a, nb);
-  return hipGetLastError();
+hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st) { return launch_loss<PolicyOp>(a, 0, st); }
+
+size_t balance_bytes(const sim_balance& c) {
+  return (size_t)kMaxBlocks * 3 * sizeof(double) + (size_t)kCountBlocks * (1 + c.A / c.group) * sizeof(uint32_t);
 }
 
-size_t balance_bytes(const sim_balance&) { return (size_t)kMaxBlocks * sizeof(double) + 16; }
-
 hipError_t launch_balance(const BalanceArgs& a, hipStream_t st) {
-  const int nb = loss_blocks(a.c.N), G = a.c.A / a.c.group;
-  const dim3 grid(nb), block(64 * kRows);
-  hipLaunchKernelGGL(balance_zero_k, dim3(1), dim3(256), 0, st, a, G);
-  if (a.c.N > 0)
-    hipLaunchKernelGGL(balance_count_k, dim3((unsigned)((a.c.N + 255) / 256 > 1024 ? 1024 : (a.c.N + 255) / 256)),
-                       dim3(256), 0, st, a);
-  switch (a.c.dtype) {
-    case SIM_DT_F32: hipLaunchKernelGGL(balance_row_k<F32>, grid, block, 0, st, a); break;
-    case SIM_DT_BF16: hipLaunchKernelGGL(balance_row_k<BF16>, grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL(balance_row_k<F16>, grid, block, 0, st, a); break;
-  }
-  hipLaunchKernelGGL(balance_finish_k, dim3(1), dim3(64), 0, st, a, nb);
-  return hipGetLastError();
+  const int nb = count_blocks(a.c.N, a.c.k);
+  hipLaunchKernelGGL(balance_count_k, dim3(nb), dim3(kCountThreads), 0, st, a);
+  return launch_loss<BalanceOp>(a, nb, st);
 }
 
 }  // namespace bsim
