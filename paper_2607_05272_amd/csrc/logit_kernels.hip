@@ -15,11 +15,27 @@
 namespace bsim {
 namespace {
 
-constexpr int kMaxBlocks = 2048;    // workgroups of a loss, each with its partial sums
+constexpr int kMaxBlocks = 4096;    // workgroups of a loss, each with its partial sums
 constexpr float kLowest = -1000.0f;
 
 __device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
+
+__device__ __forceinline__ float log_of(float x) { return __builtin_amdgcn_logf(x) * 0.69314718055994531f; }
+// e^d - 1 and, in `rest`, e^d - 1 - d: both lose all their digits to the subtractions where d is small, so
+// the second is summed as a series up to |d| = 0.35 (its first term left out is d^9/9!, 2e-9 of d^2/2).
+__device__ __forceinline__ float grow(float d, float& rest) {
+  float t = fmaf(d, 1.0f / 40320.0f, 1.0f / 5040.0f);
+  t = fmaf(d, t, 1.0f / 720.0f);
+  t = fmaf(d, t, 1.0f / 120.0f);
+  t = fmaf(d, t, 1.0f / 24.0f);
+  t = fmaf(d, t, 1.0f / 6.0f);
+  t = fmaf(d, t, 0.5f) * (d * d);
+  const float e = exp_of(d) - 1.0f;
+  const bool small = fabsf(d) < 0.35f;
+  rest = small ? t : e - d;
+  return small ? d + t : e;
+}
 
 // A part of a row: its maximum m, S = sum e and X = sum e x (policy) or sum e f (balance), with x and e
 // against m. A part of nothing has m = -inf, S = X = 0.
@@ -82,17 +98,17 @@ struct PolicyOp {
       if (first) atomicOr(s.err, ERR_ACTION);
       return false;
     }
-    const float logS = logf(p.S), logp = (la - p.m) - logS, rS = 1.0f / p.S, H = logS - p.X * rS;
-    const float rho = s.logp_old ? expf(logp - r.old) : 1.0f;
+    const float logS = log_of(p.S), logp = (la - p.m) - logS, rS = __builtin_amdgcn_rcpf(p.S);
+    const float H = fmaf(-p.X, rS, logS);
+    const float rho = s.logp_old ? exp_of(logp - r.old) : 1.0f;
     const float lo = 1.0f - s.c.clip, hi = 1.0f + s.c.clip;
     const float s1 = rho * r.adv, s2 = fminf(fmaxf(rho, lo), hi) * r.adv;
     const bool nan = !(s1 == s1);                // the clipped one alone may have lost it
     const float pol = s1 <= s2 || nan ? -s1 : -s2;
     float q = s1 <= s2 || nan || (rho > lo && rho < hi) ? -s1 : 0.0f, kl = 0.0f;
     if (s.logp_ref) {
-      const float d = r.ref - logp, e = expm1f(d);
-      kl = e - d;
-      q -= s.c.c_kl * e;
+      const float d = r.ref - logp;
+      q -= s.c.c_kl * grow(d, kl);
     }
     const float wr = r.w * rS, ch = s.c.c_entropy;
     o.alpha = ch > 0.0f ? wr * fmaf(ch, H - logS, -q) : -wr * q;
@@ -120,15 +136,22 @@ struct PolicyOp {
 // f of a target: coef G / W times its share of the live rows' choices, so that a row's term of the
 // loss is s and its gradient p (f - s). Every workgroup holds it in LDS.
 constexpr int kMaxTargets = 4096;
-// Workgroups that count the choices, each into its own row of the work memory.
-constexpr int kCountBlocks = 64, kCountThreads = 512;
-// the work memory: sums [kMaxBlocks][3] fp64, live rows [kCountBlocks], counts [kCountBlocks][G]
+// Choices are counted by workgroups that each write a row of counts, which a second launch adds up; few
+// enough of them are counted by every workgroup of the rows itself.
+constexpr int kCountBlocks = 256, kCountThreads = 512, kCountAhead = 4, kCountSelf = 4096;
+// the work memory: sums [kMaxBlocks][3] fp64, f [G], live rows [kCountBlocks], counts [kCountBlocks][G]
+__device__ __forceinline__ float* targets(const BalanceArgs& s) {
+  return reinterpret_cast<float*>(static_cast<double*>(s.work) + 3 * kMaxBlocks);
+}
 __device__ __forceinline__ uint32_t* live_parts(const BalanceArgs& s) {
-  return reinterpret_cast<uint32_t*>(static_cast<double*>(s.work) + 3 * kMaxBlocks);
+  return reinterpret_cast<uint32_t*>(targets(s) + s.c.A / s.c.group);
 }
 int count_blocks(int64_t N, int k) {
-  const int64_t b = (N * k + kCountThreads * 4 - 1) / (kCountThreads * 4);
-  return (int)(b < 1 ? 1 : (b > kCountBlocks ? kCountBlocks : b));
+  if (N * k <= kCountSelf) return 0;
+  return (int)std::min<int64_t>(kCountBlocks, (N * k + kCountThreads * kCountAhead - 1) / (kCountThreads * kCountAhead));
+}
+__device__ __forceinline__ double unit_of(const BalanceArgs& s, uint32_t W) {
+  return W ? (double)s.c.coef * (s.c.A / s.c.group) / ((double)W * W * s.c.k) : 0.0;
 }
 
 struct BalanceOp {
@@ -144,7 +167,7 @@ struct BalanceOp {
   __device__ static __forceinline__ bool close(const Args&, int64_t, const Row&, const Part& p, float, bool first,
                                                Sums& sums, RowOut& o) {
     if (p.m == -INFINITY) return false;
-    const float rS = 1.0f / p.S, si = p.X * rS;
+    const float rS = __builtin_amdgcn_rcpf(p.S), si = p.X * rS;
     o.beta = rS;
     o.alpha = -si * rS;
     o.delta = 0.0f;
@@ -155,28 +178,33 @@ struct BalanceOp {
   __device__ static __forceinline__ void finish(const Args& s, const Sums& v) { s.loss[0] = (float)v.a; }
 };
 
-// Fills f [G] from the nb counting workgroups' rows and, in one workgroup, the counts.
-__device__ __forceinline__ void fill_targets(const BalanceArgs& s, int nb, float* f) {
-  const int G = s.c.A / s.c.group;
-  const uint32_t* live = live_parts(s);
-  const uint32_t* cnt = live + kCountBlocks;
-  uint32_t W = 0;
-  for (int b = 0; b < nb; ++b) W += live[b];
-  const double unit = W ? (double)s.c.coef * G / ((double)W * W * s.c.k) : 0.0;
-  for (int g = threadIdx.x; g < G; g += blockDim.x) {
-    uint32_t c = 0;
-#pragma unroll 8
-    for (int b = 0; b < nb; ++b) c += cnt[b * G + g];
-    f[g] = (float)(unit * c);
-    if (blockIdx.x == 0) s.counts[g] = c;
+// Adds choices first, first + step, ... of the live rows to hist (cleared by the caller) and the live rows
+// to *live; the loads of several choices fly together.
+__device__ __forceinline__ void count_choices(const BalanceArgs& s, uint32_t first, uint32_t step, uint32_t* hist,
+                                              uint32_t* live, bool tell) {
+  const uint32_t k = (uint32_t)s.c.k, total = (uint32_t)(s.c.N * s.c.k);   // below 2^31
+  uint32_t mine = 0;
+  for (uint32_t i0 = first; i0 < total; i0 += kCountAhead * step) {
+    int64_t a[kCountAhead];
+    bool on[kCountAhead];
+#pragma unroll
+    for (int u = 0; u < kCountAhead; ++u) {
+      const uint32_t i = i0 + u * step;
+      on[u] = i < total;
+      a[u] = on[u] ? load_int(s.idx, s.c.index_type, i) : -1;
+      const uint32_t n = k == 1 ? i : i / k;
+      if (on[u] && s.live) on[u] = s.live[n];
+      if (on[u] && n * k == i) ++mine;
+    }
+#pragma unroll
+    for (int u = 0; u < kCountAhead; ++u) {
+      if (!on[u] || a[u] == -1) continue;
+      if (a[u] >= 0 && a[u] < s.c.A) atomicAdd(&hist[s.c.group == 1 ? (uint32_t)a[u] : (uint32_t)a[u] / (uint32_t)s.c.group], 1u);
+      else if (tell) atomicOr(s.err, ERR_ACTION);
+    }
   }
-  __syncthreads();
+  if (mine) atomicAdd(live, mine);
 }
-__device__ __forceinline__ void fill_targets(const PolicyLossArgs&, int, float*) {}
-__device__ __forceinline__ float target(const BalanceArgs& s, const float* f, int j) {
-  return f[s.c.group == 1 ? (uint32_t)j : (uint32_t)j / (uint32_t)s.c.group];
-}
-__device__ __forceinline__ float target(const PolicyLossArgs&, const float*, int) { return 0.0f; }
 
 __global__ __launch_bounds__(kCountThreads) void balance_count_k(BalanceArgs s) {
   __shared__ uint32_t hist[kMaxTargets];
@@ -185,22 +213,75 @@ __global__ __launch_bounds__(kCountThreads) void balance_count_k(BalanceArgs s) 
   for (int g = threadIdx.x; g < G; g += kCountThreads) hist[g] = 0;
   if (threadIdx.x == 0) live = 0;
   __syncthreads();
-  uint32_t mine = 0;
-  const uint32_t k = (uint32_t)s.c.k, total = (uint32_t)(s.c.N * s.c.k);   // below 2^31
-  for (uint32_t i = blockIdx.x * kCountThreads + threadIdx.x; i < total; i += gridDim.x * kCountThreads) {
-    const uint32_t n = k == 1 ? i : i / k;
-    if (s.live && !s.live[n]) continue;
-    if (n * k == i) ++mine;
-    const int64_t a = load_int(s.idx, s.c.index_type, i);
-    if (a >= 0 && a < s.c.A) atomicAdd(&hist[(uint32_t)a / (uint32_t)s.c.group], 1u);
-    else if (a != -1) atomicOr(s.err, ERR_ACTION);
-  }
-  if (mine) atomicAdd(&live, mine);
+  count_choices(s, blockIdx.x * kCountThreads + threadIdx.x, gridDim.x * kCountThreads, hist, &live, true);
   __syncthreads();
   uint32_t* o = live_parts(s);
   if (threadIdx.x == 0) o[blockIdx.x] = live;
   for (int g = threadIdx.x; g < G; g += kCountThreads) o[kCountBlocks + blockIdx.x * G + g] = hist[g];
 }
+
+// 32 targets a workgroup, 8 threads each
+__global__ __launch_bounds__(256) void balance_targets_k(BalanceArgs s, int nb) {
+  __shared__ uint32_t part[8][32], live[4];
+  const int G = s.c.A / s.c.group, g = blockIdx.x * 32 + (threadIdx.x & 31), sl = threadIdx.x >> 5;
+  const uint32_t* lp = live_parts(s);
+  const uint32_t* cnt = lp + kCountBlocks;
+  uint32_t w = threadIdx.x < nb ? lp[threadIdx.x] : 0, c = 0;
+  if (g < G) {
+#pragma unroll 8
+    for (int b = sl; b < nb; b += 8) c += cnt[b * G + g];
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) w += __shfl_xor(w, o);
+  if ((threadIdx.x & 63) == 0) live[threadIdx.x >> 6] = w;
+  part[sl][threadIdx.x & 31] = c;
+  __syncthreads();
+  if (sl == 0 && g < G) {
+    c = 0;
+    for (int i = 0; i < 8; ++i) c += part[i][threadIdx.x];
+    s.counts[g] = c;
+    targets(s)[g] = (float)(unit_of(s, live[0] + live[1] + live[2] + live[3]) * c);
+  }
+}
+static_assert(kCountBlocks <= 256, "a thread per counting workgroup");
+
+// Fills f [G] in LDS: from the launch that added up nb workgroups' counts, by adding them up here where
+// there are few, or (nb = 0) by counting.
+__host__ __device__ bool few_counts(int nb, int G) { return nb * G <= 4096; }
+__device__ __forceinline__ void fill_targets(const BalanceArgs& s, int nb, float* f) {
+  const int G = s.c.A / s.c.group;
+  if (nb && !few_counts(nb, G)) {
+    for (int g = threadIdx.x; g < G; g += blockDim.x) f[g] = targets(s)[g];
+  } else {
+    __shared__ uint32_t live;
+    uint32_t* hist = reinterpret_cast<uint32_t*>(f);
+    for (int g = threadIdx.x; g < G; g += blockDim.x) hist[g] = 0;
+    if (threadIdx.x == 0) live = 0;
+    __syncthreads();
+    if (nb) {
+      const uint32_t* lp = live_parts(s);
+      const uint32_t* cnt = lp + kCountBlocks;
+      for (int b = threadIdx.x; b < nb; b += blockDim.x) atomicAdd(&live, lp[b]);
+#pragma unroll 4
+      for (int i = threadIdx.x; i < nb * G; i += blockDim.x) atomicAdd(&hist[i % G], cnt[i]);
+    } else {
+      count_choices(s, threadIdx.x, blockDim.x, hist, &live, blockIdx.x == 0);
+    }
+    __syncthreads();
+    const double unit = unit_of(s, live);
+    for (int g = threadIdx.x; g < G; g += blockDim.x) {
+      const uint32_t c = hist[g];
+      if (blockIdx.x == 0) s.counts[g] = c;
+      f[g] = (float)(unit * c);
+    }
+  }
+  __syncthreads();
+}
+__device__ __forceinline__ void fill_targets(const PolicyLossArgs&, int, float*) {}
+__device__ __forceinline__ float target(const BalanceArgs& s, const float* f, int j) {
+  return f[s.c.group == 1 ? (uint32_t)j : (uint32_t)j / (uint32_t)s.c.group];
+}
+__device__ __forceinline__ float target(const PolicyLossArgs&, const float*, int) { return 0.0f; }
 
 // A workgroup's sums, in a fixed order: to the work memory, or with one workgroup the loss itself.
 // lds: [waves][3]
@@ -214,24 +295,33 @@ __device__ __forceinline__ void leave(const typename OP::Args& s, Sums v, double
   }
   if (lane == 0) { lds[wave][0] = v.a; lds[wave][1] = v.b; lds[wave][2] = v.c; }
   __syncthreads();
-  if (threadIdx.x == 0) {
+  if (wave == 0) {
     Sums t{0.0, 0.0, 0.0};
-    for (int w = 0; w < nw; ++w) { t.a += lds[w][0]; t.b += lds[w][1]; t.c += lds[w][2]; }
-    if (gridDim.x == 1) {
-      OP::finish(s, t);
-    } else {
-      double* o = static_cast<double*>(s.work) + 3 * blockIdx.x;
-      o[0] = t.a; o[1] = t.b; o[2] = t.c;
+    if (lane < nw) t = Sums{lds[lane][0], lds[lane][1], lds[lane][2]};
+#pragma unroll
+    for (int o = 8; o; o >>= 1) {   // at most 16 waves
+      t.a += __shfl_xor(t.a, o);
+      t.b += __shfl_xor(t.b, o);
+      t.c += __shfl_xor(t.c, o);
+    }
+    if (lane == 0) {
+      if (gridDim.x == 1) {
+        OP::finish(s, t);
+      } else {
+        double* o = static_cast<double*>(s.work) + 3 * blockIdx.x;
+        o[0] = t.a; o[1] = t.b; o[2] = t.c;
+      }
     }
   }
 }
+constexpr int kFinish = 1024;
 template <class OP>
-__global__ __launch_bounds__(256) void loss_finish_k(typename OP::Args s, int nb) {
-  __shared__ double lds[4][3];
+__global__ __launch_bounds__(kFinish) void loss_finish_k(typename OP::Args s, int nb) {
+  __shared__ double lds[kFinish / 64][3];
   const double* w = static_cast<const double*>(s.work);
   Sums v{0.0, 0.0, 0.0};
-#pragma unroll 8
-  for (int b = threadIdx.x; b < nb; b += 256) {
+#pragma unroll 4
+  for (int b = threadIdx.x; b < nb; b += kFinish) {
     v.a += w[3 * b];
     v.b += w[3 * b + 1];
     v.c += w[3 * b + 2];
@@ -403,11 +493,12 @@ __global__ __launch_bounds__(256) void loss_wave_k(typename OP::Args s, int lg, 
 // different buffers.
 template <bool BAL, int NW>
 __device__ __forceinline__ Part join_waves(Part p, Part* lds) {
+  if (NW == 1) return p;
   const int wave = threadIdx.x >> 6;
   if ((threadIdx.x & 63) == 0) lds[wave] = p;
   __syncthreads();
   const Part q = lds[(threadIdx.x & 63) % NW];   // a lane holds each wave's part
-  constexpr int lg = NW == 4 ? 2 : (NW == 8 ? 3 : 4);
+  constexpr int lg = NW == 2 ? 1 : (NW == 4 ? 2 : (NW == 8 ? 3 : 4));
   Part r = against<BAL>(q, max_lanes(q.m, lg));
   add_lanes(r.S, r.X, lg);
   return r;
@@ -476,7 +567,9 @@ __global__ __launch_bounds__(NT) void policy_block_k(PolicyLossArgs s) {
     RowOut o{0.0f, 0.0f, 0.0f};
     float m = 0.0f;
     if (on) {   // the same in the whole workgroup
-      if (threadIdx.x == 0) taken[use] = OP::template taken<T>(s, n, row);
+      float la = 0.0f;   // one wave reads it itself
+      if (NW == 1) la = OP::template taken<T>(s, n, row);
+      else if (threadIdx.x == 0) taken[use] = OP::template taken<T>(s, n, row);
       Part p{-INFINITY, 0.0f, 0.0f};
 #pragma unroll
       for (int r = 0; r < R; ++r) {
@@ -501,7 +594,7 @@ __global__ __launch_bounds__(NT) void policy_block_k(PolicyLossArgs s) {
       }
       add_lanes(p.S, p.X, 6);
       p = join_waves<false, NW>(p, parts[use]);
-      on = OP::close(s, n, row, p, taken[use], threadIdx.x == 0, sums, o);
+      on = OP::close(s, n, row, p, NW == 1 ? la : taken[use], threadIdx.x == 0, sums, o);
       m = p.m;
       use ^= 1;   // only a row with a barrier between frees the other buffer
     }
@@ -811,6 +904,9 @@ int blocks_for(int64_t N, int per, int most) {
   return (int)(b < 1 ? 1 : (b > most ? most : b));
 }
 
+constexpr int kHeld = 16;             // chunks of a row that a thread holds
+constexpr int kFill = 256 * 1024;     // threads that fill the chip while they hold a row (128 registers each)
+
 // Launches the form for these sizes and strides; the workgroups that left sums.
 template <class OP, class E>
 int launch_rows(const typename OP::Args& a, int nb, hipStream_t st) {
@@ -836,8 +932,8 @@ int launch_rows(const typename OP::Args& a, int nb, hipStream_t st) {
   }
   const int chunks = (A + N - 1) / N;
   if (A < N || chunks <= 256) {
-    // lanes of a row: enough to hold it in one chunk each, or for the longer ones two or four
-    const int lg = A < N ? ceil_log2(A) : std::min(6, ceil_log2(chunks));
+    // four chunks a lane: what a row takes besides its elements is shared by the most rows of a wave
+    const int lg = A < N ? ceil_log2(A) : ceil_log2((chunks + 3) / 4);
     const int need = A < N ? 1 : (chunks + (1 << lg) - 1) >> lg;
     const int g = blocks_for(rows, 256 >> lg, kMaxBlocks);
     const dim3 grid(g), block(256);
@@ -848,20 +944,25 @@ int launch_rows(const typename OP::Args& a, int nb, hipStream_t st) {
     return g;
   }
   if constexpr (!OP::kBal) {
-    auto go = [&](auto kern, int threads, int most) {
-      const int g = blocks_for(rows, 1, most);
-      hipLaunchKernelGGL(kern, dim3(g), dim3(threads), 0, st, a);
+    // the fewest threads that hold a row, more where there are too few rows to fill the chip
+    int nt = 64;
+    while (nt < 1024 && (chunks > kHeld * nt || (nt < 512 && rows * nt < kFill && chunks > nt))) nt *= 2;
+    if (chunks <= kHeld * nt && !(a.mask.data && nt == 1024)) {
+      const int g = blocks_for(rows, 1, std::min(kMaxBlocks, kFill / nt));
+      const dim3 grid(g), block(nt);
+      if (a.mask.data) {
+        if (nt == 64) hipLaunchKernelGGL((policy_block_k<E, 64, kHeld, true>), grid, block, 0, st, a);
+        else if (nt == 128) hipLaunchKernelGGL((policy_block_k<E, 128, kHeld, true>), grid, block, 0, st, a);
+        else if (nt == 256) hipLaunchKernelGGL((policy_block_k<E, 256, kHeld, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((policy_block_k<E, 512, kHeld, true>), grid, block, 0, st, a);
+      } else {
+        if (nt == 64) hipLaunchKernelGGL((policy_block_k<E, 64, kHeld, false>), grid, block, 0, st, a);
+        else if (nt == 128) hipLaunchKernelGGL((policy_block_k<E, 128, kHeld, false>), grid, block, 0, st, a);
+        else if (nt == 256) hipLaunchKernelGGL((policy_block_k<E, 256, kHeld, false>), grid, block, 0, st, a);
+        else if (nt == 512) hipLaunchKernelGGL((policy_block_k<E, 512, kHeld, false>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((policy_block_k<E, 1024, kHeld, false>), grid, block, 0, st, a);
+      }
       return g;
-    };
-    if (a.mask.data) {
-      if (chunks <= 1024) return go(policy_block_k<E, 256, 4, true>, 256, 2048);
-      if (chunks <= 4096) return go(policy_block_k<E, 512, 8, true>, 512, 1024);
-      if (chunks <= 8192) return go(policy_block_k<E, 1024, 8, true>, 1024, 512);
-    } else {
-      if (chunks <= 1024) return go(policy_block_k<E, 256, 4, false>, 256, 2048);
-      if (chunks <= 4096) return go(policy_block_k<E, 512, 8, false>, 512, 1024);
-      if (chunks <= 8192) return go(policy_block_k<E, 1024, 8, false>, 1024, 512);
-      if (chunks <= 16384) return go(policy_block_k<E, 1024, 16, false>, 1024, 512);
     }
   }
   const int g = blocks_for(rows, 1, 512);
@@ -872,7 +973,7 @@ template <class OP>
 hipError_t launch_loss(const typename OP::Args& a, int nb, hipStream_t st) {
   const int g = a.c.dtype == SIM_DT_F32 ? launch_rows<OP, F32>(a, nb, st)
                 : a.c.dtype == SIM_DT_BF16 ? launch_rows<OP, BF16>(a, nb, st) : launch_rows<OP, F16>(a, nb, st);
-  if (g > 1) hipLaunchKernelGGL(loss_finish_k<OP>, dim3(1), dim3(256), 0, st, a, g);
+  if (g > 1) hipLaunchKernelGGL(loss_finish_k<OP>, dim3(1), dim3(kFinish), 0, st, a, g);
   return hipGetLastError();
 }
 
@@ -883,12 +984,17 @@ size_t policy_loss_bytes(const sim_policy_loss&) { return (size_t)kMaxBlocks * 3
 hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st) { return launch_loss<PolicyOp>(a, 0, st); }
 
 size_t balance_bytes(const sim_balance& c) {
-  return (size_t)kMaxBlocks * 3 * sizeof(double) + (size_t)kCountBlocks * (1 + c.A / c.group) * sizeof(uint32_t);
+  const size_t G = c.A / c.group;
+  return (size_t)kMaxBlocks * 3 * sizeof(double) + (G + kCountBlocks * (1 + G)) * sizeof(uint32_t);
 }
 
 hipError_t launch_balance(const BalanceArgs& a, hipStream_t st) {
   const int nb = count_blocks(a.c.N, a.c.k);
-  hipLaunchKernelGGL(balance_count_k, dim3(nb), dim3(kCountThreads), 0, st, a);
+  if (nb) {
+    hipLaunchKernelGGL(balance_count_k, dim3(nb), dim3(kCountThreads), 0, st, a);
+    const int G = a.c.A / a.c.group;
+    if (!few_counts(nb, G)) hipLaunchKernelGGL(balance_targets_k, dim3((G + 31) / 32), dim3(256), 0, st, a, nb);
+  }
   return launch_loss<BalanceOp>(a, nb, st);
 }
 
