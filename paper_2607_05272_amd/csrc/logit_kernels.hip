@@ -46,6 +46,30 @@ __device__ __forceinline__ Part against(const Part& a, float m) {
   const float d = m == -INFINITY ? 0.0f : max_nan(a.m - m, kLowest), f = exp_of(d);
   return Part{m, f * a.S, BAL ? f * a.X : f * fmaf(d, a.S, a.X)};
 }
+// Over a wave, in every lane, by DPP moves within the vector unit (a step of a few cycles, where one
+// through LDS takes over a hundred): sums along each row of 16 lanes, then from row to row.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp(float none, float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(none), __float_as_uint(v), CTRL, ROWS, 0xf, false));
+}
+template <class F>
+__device__ __forceinline__ float wave_reduce(float v, F f, bool keep) {
+  // lanes without a source take their own value (keep: maxima) or 0 (sums)
+  v = f(v, dpp<0x111, 0xf>(keep ? v : 0.0f, v));   // row_shr 1, 2, 4, 8
+  v = f(v, dpp<0x112, 0xf>(keep ? v : 0.0f, v));
+  v = f(v, dpp<0x114, 0xf>(keep ? v : 0.0f, v));
+  v = f(v, dpp<0x118, 0xf>(keep ? v : 0.0f, v));
+  v = f(v, dpp<0x142, 0xa>(keep ? v : 0.0f, v));   // row_bcast 15 into rows 1 and 3
+  v = f(v, dpp<0x143, 0xc>(keep ? v : 0.0f, v));   // row_bcast 31 into rows 2 and 3
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
+}
+__device__ __forceinline__ float wave_max(float v) {
+  return wave_reduce(v, [](float a, float b) { return max_nan(a, b); }, true);
+}
+__device__ __forceinline__ float wave_add(float v) {
+  return wave_reduce(v, [](float a, float b) { return a + b; }, false);
+}
+
 // over 1 << lg adjacent lanes, in every lane
 __device__ __forceinline__ float max_lanes(float m, int lg) {
   for (int o = 1; o < (1 << lg); o <<= 1) m = max_nan(m, __shfl_xor(m, o));
@@ -508,7 +532,7 @@ __device__ __forceinline__ Part join_waves(Part p, Part* lds) {
 // gradient goes out the same chunk of the workgroup's next row comes in. Places past the row's end hold
 // -inf.
 template <class E, int NT, int R, bool MASK>
-__global__ __launch_bounds__(NT) void policy_block_k(PolicyLossArgs s) {
+__global__ __launch_bounds__(NT, 4) void policy_block_k(PolicyLossArgs s) {
   typedef PolicyOp OP;
   typedef typename E::T T;
   constexpr int N = 16 / sizeof(T), NW = NT / 64;
@@ -570,29 +594,34 @@ __global__ __launch_bounds__(NT) void policy_block_k(PolicyLossArgs s) {
       float la = 0.0f;   // one wave reads it itself
       if (NW == 1) la = OP::template taken<T>(s, n, row);
       else if (threadIdx.x == 0) taken[use] = OP::template taken<T>(s, n, row);
+      // 16 elements at a time, as they come in, against the thread's maximum so far
+      constexpr int K = 16 / N;
       Part p{-INFINITY, 0.0f, 0.0f};
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        if (r * NT * N < A) {
+      for (int r0 = 0; r0 < R; r0 += K) {
+        if (r0 * NT * N < A) {
+          float M = p.m;
 #pragma unroll
-          for (int i = 0; i < N; ++i) p.m = max_nan(p.m, value(r, i));
-        }
-      }
-      p.m = max_lanes(p.m, 6);
-      m = p.m == -INFINITY ? 0.0f : p.m;
+          for (int r = r0; r < r0 + K; ++r) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        if (r * NT * N < A) {
-          ch[r].forget();
+            for (int i = 0; i < N; ++i) M = max_nan(M, value(r, i));
+          }
+          p = against<false>(p, M);
+          const float from = M == -INFINITY ? 0.0f : M;
 #pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const float x = max_nan(value(r, i) - m, kLowest), e = exp_of(x);
-            p.S += e;
-            p.X = fmaf(e, x, p.X);
+          for (int r = r0; r < r0 + K; ++r) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+              const float x = max_nan(value(r, i) - from, kLowest), e = exp_of(x);
+              p.S += e;
+              p.X = fmaf(e, x, p.X);
+            }
           }
         }
       }
-      add_lanes(p.S, p.X, 6);
+      p = against<false>(p, wave_max(p.m));
+      p.S = wave_add(p.S);
+      p.X = wave_add(p.X);
       p = join_waves<false, NW>(p, parts[use]);
       on = OP::close(s, n, row, p, NW == 1 ? la : taken[use], threadIdx.x == 0, sums, o);
       m = p.m;
@@ -704,9 +733,9 @@ __global__ __launch_bounds__(kStream) void loss_stream_k(typename OP::Args s, in
         }
       }
       for (int j = whole * N + threadIdx.x; j < A; j += kStream) one(j, !mk || mk[j * ms] ? (float)l[j] : -INFINITY);
-      const float wm = max_lanes(p.m, 6);
-      p = against<OP::kBal>(p, wm);
-      add_lanes(p.S, p.X, 6);
+      p = against<OP::kBal>(p, wave_max(p.m));
+      p.S = wave_add(p.S);
+      p.X = wave_add(p.X);
       p = join_waves<OP::kBal, NW>(p, parts[use]);
       on = OP::close(s, n, row, p, taken[use], threadIdx.x == 0, sums, o);
       m = p.m;

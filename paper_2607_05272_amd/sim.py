@@ -5,6 +5,7 @@ into them on the context's stream. Layouts follow the ABI: [T][E] time-major arr
 [F][E] observations.
 """
 import ctypes as C
+import threading
 
 import numpy as np
 import torch
@@ -20,6 +21,11 @@ _FLOAT = {torch.float64: 0, torch.float32: 1, torch.bfloat16: 2, torch.float16: 
 _INT = {torch.uint8: 0, torch.int32: 1, torch.int64: 2}
 
 
+def _a(t):
+    """A tensor's address (None: absent)."""
+    return None if t is None else t.data_ptr()
+
+
 def _seq(t):
     """sim_seq of a [B][T][D] tensor (None: absent)."""
     if t is None:
@@ -27,15 +33,11 @@ def _seq(t):
     sb, st, sd = t.stride()
     if sd != 1 and t.shape[2] > 1:
         raise ValueError("channels (the last dimension) must be adjacent in memory")
-    return L.SimSeq(t.data_ptr(), sb, st)
+    return C.byref(L.SimSeq(t.data_ptr(), sb, st))
 
 
 def _mat(t):
-    return None if t is None else L.SimMat(t.data_ptr(), *t.stride())
-
-
-def _ref(s):
-    return None if s is None else C.byref(s)
+    return None if t is None else C.byref(L.SimMat(t.data_ptr(), *t.stride()))
 
 
 def weights_layout(w):
@@ -176,7 +178,9 @@ class Sim:
         self._index = (self.device.index if self.device.index is not None
                        else torch.cuda.current_device())
         self._device = torch.device("cuda", self._index)
+        self._work = threading.local()
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        self._raw_stream = self.stream.cuda_stream
         self._ctx = C.c_void_p()
         self._keep = []
         with torch.cuda.device(self._device):
@@ -324,37 +328,47 @@ class Sim:
     # -- operators for the caller's own networks -------------------------------------------
     def _check(self, name, t, shape, dtypes):
         """`t` is a tensor on the context's device, of this shape and one of these types."""
-        if t.device.type != "cuda" or t.device.index != self._index:
-            raise ValueError(f"{name} is on {t.device}, the context on cuda:{self._index}")
-        if tuple(t.shape) != tuple(shape):
+        if t.dtype in dtypes and t.shape == shape and t.device == self._device:
+            return
+        if t.device != self._device:
+            raise ValueError(f"{name} is on {t.device}, the context on {self._device}")
+        if t.shape != shape:
             raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-        if t.dtype not in dtypes:
-            raise ValueError(f"{name} is {t.dtype}, expected {' or '.join(map(str, dtypes))}")
-        return t
+        raise ValueError(f"{name} is {t.dtype}, expected {' or '.join(map(str, dtypes))}")
 
     def _flat(self, name, t, shape, dtypes):
-        """As _check, of a tensor that is read as one contiguous array."""
+        """As _check, of a tensor (or None) that is read as one contiguous array."""
         if t is None:
-            return None
+            return
         self._check(name, t, shape, dtypes)
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
-        return t
 
     def _call(self, name, sizes, *args):
-        """An operator's entry point with work memory from torch, ordered after the work of the
-        current stream, and that stream after it, where the context has another one."""
-        need = C.c_size_t()
-        L.check(getattr(self.lib, name + "_work")(C.byref(sizes), C.byref(need)), name)
-        work = torch.empty(need.value, dtype=torch.uint8, device=self._device) if need.value else None
-        now = torch.cuda.current_stream(self._device)
-        other = now.cuda_stream != self.stream.cuda_stream
-        if other:
+        """An operator's entry point with work memory, ordered after the work of the current
+        stream, and that stream after it, where the context has another one. The memory is kept
+        from call to call, per thread, where calls follow one another on the context's stream;
+        a captured call, whose replays do not, gets its own, and so does one from another
+        stream, whose allocations torch orders by that stream."""
+        sizes_p, need = C.byref(sizes), C.c_size_t()
+        L.check(getattr(self.lib, name + "_work")(sizes_p, C.byref(need)), name)
+        work, need = None, need.value
+        same = torch._C._cuda_getCurrentRawStream(self._index) == self._raw_stream
+        if need:
+            work = getattr(self._work, "memory", None)
+            if not same or torch.cuda.is_current_stream_capturing():
+                work = torch.empty(need, dtype=torch.uint8, device=self._device)
+            elif work is None or work.numel() < need:
+                work = self._work.memory = torch.empty(need, dtype=torch.uint8, device=self._device)
+            work = work.data_ptr()
+        if not same:
+            now = torch.cuda.current_stream(self._device)
             self.stream.wait_stream(now)
-        rc = getattr(self.lib, name)(self._ctx, C.byref(sizes), *args, _p(work), need.value)
-        if other:
+        rc = getattr(self.lib, name)(self._ctx, sizes_p, *args, work, need)
+        if not same:
             now.wait_stream(self.stream)
-        L.check(rc, name)
+        if rc:
+            L.check(rc, name)
 
     def gated_scan(self, gate, x, h0=None, lengths=None, kind="linear", reverse=False, y=None,
                    state=None, want_y=True):
@@ -377,13 +391,13 @@ class Sim:
         if y is not None:
             self._check("y", y, (B, T, D), (gate.dtype,))
         elif want_y:
-            y = torch.empty((B, T, D), dtype=gate.dtype, device=self._device)
+            y = gate.new_empty((B, T, D))
         if state is None:
-            state = torch.empty((B, D), dtype=wide, device=self._device)
-        self._flat("state", state, (B, D), (wide,))
+            state = gate.new_empty((B, D), dtype=wide)
+        else:
+            self._flat("state", state, (B, D), (wide,))
         sizes = L.SimScan(_FLOAT[gate.dtype], L.GATE_KINDS[kind], int(reverse), B, T, D)
-        self._call("gated_scan", sizes, _ref(_seq(gate)), _ref(_seq(x)), _p(lengths), _p(h0),
-                   _ref(_seq(y)), _p(state))
+        self._call("gated_scan", sizes, _seq(gate), _seq(x), _a(lengths), _a(h0), _seq(y), _a(state))
         return (None if y is None else y[0], state[0]) if one else (y, state)
 
     def gated_scan_grad(self, gate, x, y, dy, h0=None, dstate=None, lengths=None, kind="linear",
@@ -407,29 +421,30 @@ class Sim:
         self._flat("dstate", dstate, (B, D), (wide,))
         self._flat("lengths", lengths, (B,), (torch.int32,))
         if dgate is None and want_gate:
-            dgate = torch.empty((B, T, D), dtype=gate.dtype, device=self._device)
+            dgate = gate.new_empty((B, T, D))
         if dx is None:
-            dx = torch.empty((B, T, D), dtype=gate.dtype, device=self._device)
+            dx = gate.new_empty((B, T, D))
         if dh0 is None:
-            dh0 = torch.empty((B, D), dtype=wide, device=self._device)
-        self._flat("dh0", dh0, (B, D), (wide,))
+            dh0 = gate.new_empty((B, D), dtype=wide)
+        else:
+            self._flat("dh0", dh0, (B, D), (wide,))
         sizes = L.SimScan(_FLOAT[gate.dtype], L.GATE_KINDS[kind], int(reverse), B, T, D)
-        self._call("gated_scan_grad", sizes, _ref(_seq(gate)), _ref(_seq(x)), _ref(_seq(y)),
-                   _ref(_seq(dy)), _p(lengths), _p(h0), _p(dstate), _ref(_seq(dgate)),
-                   _ref(_seq(dx)), _p(dh0))
+        self._call("gated_scan_grad", sizes, _seq(gate), _seq(x), _seq(y), _seq(dy), _a(lengths),
+                   _a(h0), _a(dstate), _seq(dgate), _seq(dx), _a(dh0))
         if one:
             return None if dgate is None else dgate[0], dx[0], dh0[0]
         return dgate, dx, dh0
 
     def _grad_like(self, logits, grad, want):
         if grad is not None:
-            return self._check("grad", grad, logits.shape, (logits.dtype,))
+            self._check("grad", grad, logits.shape, (logits.dtype,))
+            return grad
         if not want:
             return None
         N, A = logits.shape
         if logits.stride(1) == 1 or A == 1:
-            return torch.empty((N, A), dtype=logits.dtype, device=self._device)
-        return torch.empty((A, N), dtype=logits.dtype, device=self._device).t()
+            return logits.new_empty((N, A))
+        return logits.new_empty((A, N)).t()
 
     def policy_loss(self, logits, actions, adv, logp_old=None, logp_ref=None, weight=None,
                     mask=None, clip=0.2, c_kl=0.0, c_entropy=0.0, grad=None, want_grad=True):
@@ -448,13 +463,12 @@ class Sim:
         if mask is not None:
             self._check("mask", mask, (N, A), (torch.bool, torch.uint8))
         grad = self._grad_like(logits, grad, want_grad)
-        loss = torch.empty(4, dtype=torch.float32, device=self._device)
-        logp = torch.empty(N, dtype=torch.float32, device=self._device)
+        loss = logits.new_empty(4, dtype=torch.float32)
+        logp = logits.new_empty(N, dtype=torch.float32)
         sizes = L.SimPolicyLoss(N, A, _FLOAT[logits.dtype], _INT[actions.dtype], _FLOAT[adv.dtype],
                                 clip, c_kl, c_entropy)
-        self._call("policy_loss", sizes, _ref(_mat(logits)), _ref(_mat(mask)), _p(actions),
-                   _p(weight), _p(logp_old), _p(logp_ref), _p(adv), _ref(_mat(grad)), _p(logp),
-                   _p(loss))
+        self._call("policy_loss", sizes, _mat(logits), _mat(mask), _a(actions), _a(weight),
+                   _a(logp_old), _a(logp_ref), _a(adv), _mat(grad), _a(logp), _a(loss))
         return dict(loss=loss, logp=logp, grad=grad)
 
     def balance_loss(self, logits, index, live=None, group=1, coef=1.0, grad=None, want_grad=True):
@@ -471,11 +485,11 @@ class Sim:
         self._flat("index", index, (N, k), _INT)
         self._flat("live", live, (N,), (torch.bool, torch.uint8))
         grad = self._grad_like(logits, grad, want_grad)
-        counts = torch.empty(max(1, A // max(1, group)), dtype=torch.int64, device=self._device)
-        loss = torch.empty((), dtype=torch.float32, device=self._device)
+        counts = logits.new_empty(max(1, A // max(1, group)), dtype=torch.int64)
+        loss = logits.new_empty((), dtype=torch.float32)
         sizes = L.SimBalance(N, A, k, group, _FLOAT[logits.dtype], _INT[index.dtype], coef)
-        self._call("balance_loss", sizes, _ref(_mat(logits)), _p(index), _p(live), _ref(_mat(grad)),
-                   _p(counts), _p(loss))
+        self._call("balance_loss", sizes, _mat(logits), _a(index), _a(live), _mat(grad), _a(counts),
+                   _a(loss))
         return dict(loss=loss, counts=counts, grad=grad)
 
     def params_from_weights(self, weights):
