@@ -353,6 +353,10 @@ __global__ __launch_bounds__(kFinish) void loss_finish_k(typename OP::Args s, in
   leave<OP>(s, v, lds);
 }
 
+// A value that the compiler finds again in each round of a loop: it would otherwise keep a pointer of its
+// own for every access that depends on it and step them all from round to round, more registers than there are.
+__device__ __forceinline__ void fresh(int64_t& uniform) { asm volatile("" : "+s"(uniform)); }
+
 // ---- rows of adjacent logits -----------------------------------------------------------------
 // N elements of a row, at any alignment of the element type
 template <class E, int N>
@@ -779,92 +783,174 @@ __global__ __launch_bounds__(kStream) void loss_stream_k(typename OP::Args s, in
 }
 
 // ---- logits of adjacent samples: [A][N] --------------------------------------------------------
-// A lane takes a sample; 1 << lw waves share 64 samples, each with up to R of the actions.
-template <class OP, class E, int NT, int R>
-__global__ __launch_bounds__(NT) void loss_cols_k(typename OP::Args s, int lw, int nb) {
+// A lane takes two adjacent samples; W waves share them, each with up to R of their actions, and one
+// thread a sample joins the waves' parts and closes it. GR such groups make a workgroup.
+template <class OP, class E, int W, int GR, int R>
+__global__ __launch_bounds__(64 * W * GR) void loss_cols_k(typename OP::Args s, int nb) {
   typedef typename E::T T;
-  __shared__ double lds[NT / 64][3];
-  __shared__ Part parts[2][NT / 64][64];
-  __shared__ float taken[2][64];
+  typedef T Raw __attribute__((ext_vector_type(2), aligned(sizeof(T))));
+  typedef T Val __attribute__((ext_vector_type(2)));
+  typedef uint8_t Bytes __attribute__((ext_vector_type(2), aligned(1)));
+  struct Closed { float m, alpha, beta, delta; int act; };   // act -2: the sample gives nothing
+  constexpr bool kShare = W > 1;
+  __shared__ double lds[W * GR][3];
+  __shared__ Part parts[kShare ? W * GR : 1][128];
+  __shared__ Closed closed[kShare ? GR : 1][128];
   __shared__ float f[OP::kBal ? kMaxTargets : 1];
   fill_targets(s, nb, f);
-  const int A = s.c.A, lane = threadIdx.x & 63, W = 1 << lw;
+  const int A = s.c.A, lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // the same in all of a wave's lanes
-  const int mine = (A - (wave & (W - 1)) + W - 1) >> lw;   // actions of this wave
-  const int wa = wave & (W - 1), grp = wave >> lw, per = (blockDim.x >> 6 >> lw) * 64;
+  const int wa = wave % W, grp = wave / W, mine = (A - wa + W - 1) / W;
+  const T* l0 = static_cast<const T*>(s.l.data);
+  T* g0 = static_cast<T*>(s.grad.data);
+  const int64_t N = s.c.N, ls = s.l.stride_n, gs = s.grad.stride_n;
   Sums sums{0.0, 0.0, 0.0};
-  int use = 0;
-  for (int64_t n0 = (int64_t)blockIdx.x * per; n0 < s.c.N; n0 += (int64_t)gridDim.x * per, use ^= 1) {
-    const int64_t n = n0 + grp * 64 + lane;
-    const bool in = n < s.c.N;
-    typename OP::Row row;
-    bool on = in && OP::open(s, n, row);
-    float x[R];
+  for (int64_t n0 = (int64_t)blockIdx.x * 128 * GR; n0 < N; n0 += (int64_t)gridDim.x * 128 * GR) {
+    // every lane has both samples, side by side: pairs at a lane's offset from the row's address
+    const bool fits = n0 + 128 * GR <= N && ls == 1 && (!g0 || gs == 1);
+    either(fits, [&](auto ALL) {
+    constexpr bool WHOLE = decltype(ALL)::value;
+    int64_t base = n0 + grp * 128;
+    int64_t la = s.l.stride_a, ma = 0, ga = s.grad.stride_a;
+    if constexpr (!OP::kBal) ma = s.mask.stride_a;
+    fresh(base);
+    fresh(la);
+    fresh(ma);
+    fresh(ga);
+    const int64_t n = base + 2 * lane;
+    const bool in0 = n < N, in1 = n + 1 < N;
+    // what a sample has besides its logits, read ahead of them by the thread that will close it
+    constexpr int OWN = kShare ? 1 : 2;
+    typename OP::Row rows[OWN];
+    bool on[OWN];
+    float taken[OWN];
 #pragma unroll
-    for (int i = 0; i < R; ++i) x[i] = -INFINITY;
-    if (on) {
-      const T* l = static_cast<const T*>(s.l.data) + n * s.l.stride_n + wa * s.l.stride_a;
-#pragma unroll
-      for (int i = 0; i < R; ++i, l += s.l.stride_a << lw)
-        if (i < mine) x[i] = (float)*l;
-      if constexpr (!OP::kBal) {
-        if (s.mask.data) {
-          const uint8_t* mk = static_cast<const uint8_t*>(s.mask.data) + n * s.mask.stride_n + wa * s.mask.stride_a;
-          uint8_t open[R];
-#pragma unroll
-          for (int i = 0; i < R; ++i, mk += s.mask.stride_a << lw) open[i] = i < mine ? *mk : 0;
-#pragma unroll
-          for (int i = 0; i < R; ++i) x[i] = open[i] ? x[i] : -INFINITY;
-        }
-      }
+    for (int v = 0; v < OWN; ++v) {
+      const int64_t t = kShare ? n0 + threadIdx.x : n + v;
+      on[v] = (!kShare || threadIdx.x < 128 * GR) && t < N && OP::open(s, t, rows[v]);
+      taken[v] = on[v] ? OP::template taken<T>(s, t, rows[v]) : 0.0f;
     }
-    float la = 0.0f;
-    // read by the wave that writes it, before it does
-    if (on && (OP::kBal || (row.act & (W - 1)) == wa)) {
-      la = OP::template taken<T>(s, n, row);
-      if (W > 1) taken[use][grp * 64 + lane] = la;
-    }
-    Part p{-INFINITY, 0.0f, 0.0f};
+    float x[R][2];
+    if constexpr (WHOLE) {
+      const T* row = l0 + base + wa * la;
 #pragma unroll
-    for (int i = 0; i < R; ++i) p.m = max_nan(p.m, x[i]);
-    float m = p.m == -INFINITY ? 0.0f : p.m;
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const float d = max_nan(x[i] - m, kLowest), e = exp_of(d);
-      p.S += e;
-      p.X = fmaf(e, OP::kBal ? (i < mine ? target(s, f, wa + (i << lw)) : 0.0f) : d, p.X);
-    }
-    if (W > 1) {
-      parts[use][wave][lane] = p;
-      __syncthreads();
-      float M = p.m;
-      for (int w = 0; w < W; ++w) M = max_nan(M, parts[use][(grp << lw) + w][lane].m);
-      Part t{M, 0.0f, 0.0f};
-      for (int w = 0; w < W; ++w) {
-        const Part q = against<OP::kBal>(parts[use][(grp << lw) + w][lane], M);
-        t.S += q.S;
-        t.X += q.X;
-      }
-      p = t;
-      la = taken[use][grp * 64 + lane];
-      m = p.m == -INFINITY ? 0.0f : p.m;
-    }
-    RowOut o{0.0f, 0.0f, 0.0f};
-    on = on && OP::close(s, n, row, p, la, wa == 0, sums, o);
-    if (in && !on && wa == 0) OP::shut(s, n);
-    if (s.grad.data && in) {
-      T* g = static_cast<T*>(s.grad.data) + n * s.grad.stride_n + wa * s.grad.stride_a;
-#pragma unroll
-      for (int i = 0; i < R; ++i, g += s.grad.stride_a << lw) {
+      for (int i = 0; i < R; ++i, row += W * la) {
+        x[i][0] = x[i][1] = -INFINITY;
         if (i < mine) {
-          const int a = wa + (i << lw);
-          const float d = max_nan(x[i] - m, kLowest);
-          float w = exp_of(d) * fmaf(o.beta, OP::kBal ? target(s, f, a) : d, o.alpha);
-          if (!OP::kBal && row.act == a) w += o.delta;
-          *g = (T)(on ? w : 0.0f);
+          const Raw v = *reinterpret_cast<const Raw*>(row + 2u * lane);
+          x[i][0] = (float)v[0];
+          x[i][1] = (float)v[1];
+        }
+      }
+    } else {
+      const int64_t at[2] = {(in0 ? n : N - 1) * ls, (in1 ? n + 1 : N - 1) * ls};
+      const T* row = l0 + wa * la;
+#pragma unroll
+      for (int i = 0; i < R; ++i, row += W * la) {
+#pragma unroll
+        for (int v = 0; v < 2; ++v) x[i][v] = i < mine ? (float)row[at[v]] : -INFINITY;
+      }
+    }
+    if constexpr (!OP::kBal) {
+      if (s.mask.data) {
+        const int64_t ms = s.mask.stride_n;
+        const uint8_t* row = static_cast<const uint8_t*>(s.mask.data) + wa * ma;
+        if (WHOLE && ms == 1) {
+          Bytes open[R];
+          row += base;
+#pragma unroll
+          for (int i = 0; i < R; ++i, row += W * ma)
+            open[i] = i < mine ? *reinterpret_cast<const Bytes*>(row + 2u * lane) : Bytes{0, 0};
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
+#pragma unroll
+            for (int v = 0; v < 2; ++v) x[i][v] = open[i][v] ? x[i][v] : -INFINITY;
+          }
+        } else {
+          const int64_t at[2] = {(in0 ? n : N - 1) * ms, (in1 ? n + 1 : N - 1) * ms};
+#pragma unroll
+          for (int i = 0; i < R; ++i, row += W * ma) {
+#pragma unroll
+            for (int v = 0; v < 2; ++v) x[i][v] = i < mine && row[at[v]] ? x[i][v] : -INFINITY;
+          }
         }
       }
     }
+    Part p[2];
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+      p[v] = Part{-INFINITY, 0.0f, 0.0f};
+#pragma unroll
+      for (int i = 0; i < R; ++i) p[v].m = max_nan(p[v].m, x[i][v]);
+      const float m = p[v].m == -INFINITY ? 0.0f : p[v].m;
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const float d = max_nan(x[i][v] - m, kLowest), e = exp_of(d);
+        p[v].S += e;
+        p[v].X = fmaf(e, OP::kBal ? (i < mine ? target(s, f, wa + W * i) : 0.0f) : d, p[v].X);
+      }
+    }
+    Closed c[2];
+    auto close = [&](int64_t t, int v, const Part& whole) {
+      RowOut o{0.0f, 0.0f, 0.0f};
+      const bool gives = on[v] && OP::close(s, t, rows[v], whole, taken[v], true, sums, o);
+      if (!gives) OP::shut(s, t);
+      return Closed{whole.m == -INFINITY ? 0.0f : whole.m, o.alpha, o.beta, o.delta, gives ? (int)rows[v].act : -2};
+    };
+    if constexpr (kShare) {
+      static_assert(W >= 2, "a thread for each sample");
+#pragma unroll
+      for (int v = 0; v < 2; ++v) parts[wave][2 * lane + v] = p[v];
+      __syncthreads();
+      const int kg = threadIdx.x / 128, ks = threadIdx.x % 128;
+      if (kg < GR && n0 + threadIdx.x < N) {
+        float M = parts[kg * W][ks].m;
+#pragma unroll
+        for (int w = 1; w < W; ++w) M = max_nan(M, parts[kg * W + w][ks].m);
+        Part whole{M, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+          const Part q = against<OP::kBal>(parts[kg * W + w][ks], M);
+          whole.S += q.S;
+          whole.X += q.X;
+        }
+        closed[kg][ks] = close(n0 + threadIdx.x, 0, whole);
+      }
+      __syncthreads();
+      c[0] = closed[grp][2 * lane];
+      c[1] = closed[grp][2 * lane + 1];
+    } else {
+      c[0] = c[1] = Closed{0.0f, 0.0f, 0.0f, 0.0f, -2};
+      if (in0) c[0] = close(n, 0, p[0]);
+      if (in1) c[1] = close(n + 1, OWN - 1, p[1]);
+    }
+    if (g0) {
+      T* row = g0 + wa * ga;
+      const int64_t at = n * gs;
+#pragma unroll
+      for (int i = 0; i < R; ++i, row += W * ga) {
+        if (i < mine) {
+          const int a = wa + W * i;
+          float w[2];
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            const float d = max_nan(x[i][v] - c[v].m, kLowest);
+            w[v] = exp_of(d) * fmaf(c[v].beta, OP::kBal ? target(s, f, a) : d, c[v].alpha);
+            if (!OP::kBal) w[v] += c[v].act == a ? c[v].delta : 0.0f;
+            w[v] = c[v].act == -2 ? 0.0f : w[v];
+          }
+          if constexpr (WHOLE) {
+            typedef float Two __attribute__((ext_vector_type(2)));
+            *reinterpret_cast<Raw*>(row + base + 2u * lane) =
+                __builtin_bit_cast(Raw, __builtin_convertvector((Two{w[0], w[1]}), Val));
+          } else {
+            if (in0) row[at] = (T)w[0];
+            if (in1) row[at + gs] = (T)w[1];
+          }
+        }
+      }
+    }
+    });
   }
   __syncthreads();
   leave<OP>(s, sums, lds);
@@ -944,19 +1030,22 @@ int launch_rows(const typename OP::Args& a, int nb, hipStream_t st) {
   const int64_t rows = a.c.N;
   const bool adjacent = (a.l.stride_a == 1 || A == 1) && (!a.grad.data || a.grad.stride_a == 1 || A == 1);
   if (!adjacent) {
-    // waves that share a sample so that each holds at most 24 of its actions
-    const int lw = ceil_log2((A + 23) / 24);
-    if (lw > 4) {
+    // waves that share a sample, each with at most 12 of its actions (24 with the most waves)
+    const int lw = ceil_log2((A + 11) / 12), each = 128 * (lw < 2 ? 4 >> lw : 1);
+    if (A > 16 * 24) {
       const int g = blocks_for(rows, 64, kMaxBlocks);
       hipLaunchKernelGGL((loss_lane_k<OP, E>), dim3(g), dim3(64), 0, st, a, nb);
       return g;
     }
-    const int threads = lw > 2 ? 64 << lw : 256, per = threads >> lw, g = blocks_for(rows, per, kMaxBlocks);
-    const int need = (A + (1 << lw) - 1) >> lw;
-    const dim3 grid(g), block(threads);
-    if (need <= 8) hipLaunchKernelGGL((loss_cols_k<OP, E, 256, 8>), grid, block, 0, st, a, lw, nb);
-    else if (threads == 256) hipLaunchKernelGGL((loss_cols_k<OP, E, 256, 24>), grid, block, 0, st, a, lw, nb);
-    else hipLaunchKernelGGL((loss_cols_k<OP, E, 1024, 24>), grid, block, 0, st, a, lw, nb);
+    const int g = blocks_for(rows, each, kMaxBlocks);
+    const dim3 grid(g), block(lw < 2 ? 256 : std::min(1024, 64 << lw));
+    if (A <= 6) hipLaunchKernelGGL((loss_cols_k<OP, E, 1, 4, 6>), grid, block, 0, st, a, nb);
+    else if (lw == 0) hipLaunchKernelGGL((loss_cols_k<OP, E, 1, 4, 12>), grid, block, 0, st, a, nb);
+    else if (lw == 1) hipLaunchKernelGGL((loss_cols_k<OP, E, 2, 2, 12>), grid, block, 0, st, a, nb);
+    else if (lw == 2) hipLaunchKernelGGL((loss_cols_k<OP, E, 4, 1, 12>), grid, block, 0, st, a, nb);
+    else if (lw == 3) hipLaunchKernelGGL((loss_cols_k<OP, E, 8, 1, 12>), grid, block, 0, st, a, nb);
+    else if (lw == 4) hipLaunchKernelGGL((loss_cols_k<OP, E, 16, 1, 12>), grid, block, 0, st, a, nb);
+    else hipLaunchKernelGGL((loss_cols_k<OP, E, 16, 1, 24>), grid, block, 0, st, a, nb);
     return g;
   }
   const int chunks = (A + N - 1) / N;

@@ -1,6 +1,8 @@
 // ops_dev.hpp -- element types of the operators' arrays: loads widened to the type they are
 // computed in, stores rounded once to nearest even.
 #pragma once
+#include <type_traits>
+
 #include "devmath.hpp"
 #include "ops.hpp"
 #include "params.hpp"
@@ -32,6 +34,13 @@ __device__ __forceinline__ int64_t load_int(const void* p, int type, int64_t i) 
   if (type == SIM_IT_U8) return static_cast<const uint8_t*>(p)[i];
   if (type == SIM_IT_I32) return static_cast<const int32_t*>(p)[i];
   return static_cast<const int64_t*>(p)[i];
+}
+
+// f(true) or f(false), so that the usual case is compiled without its conditions
+template <class F>
+__device__ __forceinline__ void either(bool c, F f) {
+  if (c) f(std::true_type{});
+  else f(std::false_type{});
 }
 
 }  // namespace

@@ -12,7 +12,6 @@
 // Positions p = 0..T-1 are taken in processing order, t = p, or from the end. Padding is the
 // identity (A, X) = (1, 0), so the state passes through it on either side of a sequence.
 #include <algorithm>
-#include <type_traits>
 
 #include "ops_dev.hpp"
 
@@ -269,13 +268,6 @@ __device__ __forceinline__ void store(const Block<E, V, L, TV>& blk, const sim_s
       if (t >= 0 && t < w.T) *reinterpret_cast<Vec*>(p + (int64_t)t * q.stride_t + w.d) = blk.r[l];
     }
   }
-}
-
-// f(true) or f(false), so that the usual case is compiled without its conditions
-template <class F>
-__device__ __forceinline__ void either(bool c, F f) {
-  if (c) f(std::true_type{});
-  else f(std::false_type{});
 }
 
 // The block of position p: for one channel whose steps are adjacent, blocks start at multiples
