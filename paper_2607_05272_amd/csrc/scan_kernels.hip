@@ -50,18 +50,31 @@ __device__ __forceinline__ int seq_len(const ScanArgs& s, int64_t b, bool tell) 
 // channel whose steps are adjacent (time = 1): a thread has L adjacent steps, a sequence has
 // 1 << gs threads.
 struct ScanPlan {
-  int time, vec;      // vec: 16-byte accesses
+  int time, vec;      // vec (time = 1): the steps of every array in use are adjacent
   int lx, gs;
   int64_t tiles;      // workgroups side by side
   int64_t per;        // time = 0: channel tiles of a sequence
   int chunks;         // time-wise pieces, each a workgroup that goes over `ctiles` tiles
   int ctiles;
+  int runs;           // tile_of
 };
 
+// N elements, in registers and (at any alignment of the element) in memory
 template <class T, int N>
-struct VecOf { typedef T V __attribute__((ext_vector_type(N), aligned(sizeof(T) * N < 16 ? sizeof(T) * N : 16))); };
+struct VecOf {
+  typedef T V __attribute__((ext_vector_type(N)));
+  typedef T M __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+};
 template <class T>
-struct VecOf<T, 1> { typedef T V; };
+struct VecOf<T, 1> { typedef T V; typedef T M; };
+template <class T, int N>
+__device__ __forceinline__ typename VecOf<T, N>::V read(const T* p) {
+  return __builtin_bit_cast(typename VecOf<T, N>::V, *reinterpret_cast<const typename VecOf<T, N>::M*>(p));
+}
+template <class T, int N>
+__device__ __forceinline__ void write(T* p, typename VecOf<T, N>::V v) {
+  *reinterpret_cast<typename VecOf<T, N>::M*>(p) = __builtin_bit_cast(typename VecOf<T, N>::M, v);
+}
 
 // What a thread is to its tile.
 struct Place {
@@ -186,7 +199,7 @@ struct Block {
 struct Where {
   int t0;        // the first step in memory
   int n, T;      // steps of the sequence, of the arrays
-  int d;         // channel
+  int d, skip;   // first channel, and how many from it are another thread's
   bool back, vec;
   __device__ __forceinline__ int t(int l, int L) const { return back ? t0 + L - 1 - l : t0 + l; }
 };
@@ -208,7 +221,7 @@ __device__ __forceinline__ void load(Block<E, V, L, TV>& blk, const sim_seq& q, 
   const T* p = static_cast<const T*>(q.data) + b * q.stride_b;
   if constexpr (TV) {
     if (w.vec && shift == 0 && w.t0 >= 0 && w.t0 + L <= w.T) {
-      blk.r[0] = *reinterpret_cast<const Vec*>(p + w.t0);
+      blk.r[0] = read<T, L>(p + w.t0);
     } else if (w.n > 0) {
 #pragma unroll
       for (int l = 0; l < L; ++l) {
@@ -226,13 +239,13 @@ __device__ __forceinline__ void load(Block<E, V, L, TV>& blk, const sim_seq& q, 
     const int64_t step = w.back ? -q.stride_t : q.stride_t;
     p += (int64_t)(w.t(0, L) + shift) * q.stride_t + w.d;
 #pragma unroll
-    for (int l = 0; l < L; ++l) blk.r[l] = *reinterpret_cast<const Vec*>(p + l * step);
+    for (int l = 0; l < L; ++l) blk.r[l] = read<T, V>(p + l * step);
   } else if (w.n > 0) {
 #pragma unroll
     for (int l = 0; l < L; ++l) {
       int t = w.t(l, L) + shift;
       t = t < 0 ? 0 : (t >= w.n ? w.n - 1 : t);
-      blk.r[l] = *reinterpret_cast<const Vec*>(p + (int64_t)t * q.stride_t + w.d);
+      blk.r[l] = read<T, V>(p + (int64_t)t * q.stride_t + w.d);
     }
   }
 }
@@ -250,22 +263,25 @@ __device__ __forceinline__ void store(const Block<E, V, L, TV>& blk, const sim_s
       for (int l = 0; l < L; ++l) o[l] = blk.r[0][L - 1 - l];
     }
     if (w.vec && w.t0 >= 0 && w.t0 + L <= w.T) {
-      *reinterpret_cast<Vec*>(p + w.t0) = o;
+      write<T, L>(p + w.t0, o);
     } else {
 #pragma unroll
       for (int l = 0; l < L; ++l)
         if (w.t0 + l >= 0 && w.t0 + l < w.T) p[(int64_t)(w.t0 + l) * q.stride_t] = o[l];
     }
-  } else if (whole) {
-    const int64_t step = w.back ? -q.stride_t : q.stride_t;
-    p += (int64_t)w.t(0, L) * q.stride_t + w.d;
-#pragma unroll
-    for (int l = 0; l < L; ++l) *reinterpret_cast<Vec*>(p + l * step) = blk.r[l];
   } else {
 #pragma unroll
     for (int l = 0; l < L; ++l) {
       const int t = w.t(l, L);
-      if (t >= 0 && t < w.T) *reinterpret_cast<Vec*>(p + (int64_t)t * q.stride_t + w.d) = blk.r[l];
+      if (!whole && (t < 0 || t >= w.T)) continue;
+      T* at = p + (int64_t)t * q.stride_t + w.d;
+      if (w.skip == 0) {
+        write<T, V>(at, blk.r[l]);
+      } else if constexpr (V > 1) {
+#pragma unroll
+        for (int v = 1; v < V; ++v)
+          if (v >= w.skip) at[v] = blk.r[l][v];
+      }
     }
   }
 }
@@ -282,25 +298,36 @@ __device__ __forceinline__ int first_step(int p, int T, bool back) {
 template <class W, int V>
 struct ScanLds { W v[2][kWaves][64][V][2]; };
 
-// What a workgroup's thread is in the whole launch.
+// Workgroups are dealt out to the eight XCDs in turn. Where rows do not start on cache lines, neighbours
+// share lines, so each XCD gets a run of tiles: the one that workgroup i of n takes (fp64 1365 x 26762
+// 284 -> 223 us; rows on lines the other way: fp32 1025 x 16 x 1536 153 in turn, 162 in runs).
+__device__ __forceinline__ int64_t tile_of(const ScanPlan& p, int64_t i) {
+  if (!p.runs) return i;
+  const int64_t each = p.tiles >> 3, rest = p.tiles & 7, x = i & 7;
+  return x * each + (x < rest ? x : rest) + (i >> 3);
+}
+
+// What a workgroup's thread is in the whole launch. The last thread of a row takes the last V channels,
+// the first `skip` of which its neighbour writes; threads past the row (skip = V) write none.
 struct Job {
   int64_t b;
-  int d;
-  bool live;    // it has channels of its own (others read some channel and write none)
+  int d, skip;
+  bool live;
 };
 template <int V, bool TV>
 __device__ __forceinline__ Job job_of(const ScanPlan& p, const Place& q, const sim_scan& c, int64_t blk) {
   Job j;
   if (TV) {
     j.b = (blk << (kLogThreads - p.gs)) + (threadIdx.x >> p.gs);
-    j.d = 0;
+    j.d = j.skip = 0;
     j.live = j.b < c.B;
     if (!j.live) j.b = c.B - 1;
   } else {
     j.b = blk / p.per;
     const int64_t d = (((blk % p.per) << p.lx) + q.col) * V;
     j.live = d < c.D;
-    j.d = (int)(j.live ? d : c.D - V);
+    j.d = (int)(d < c.D - V ? d : c.D - V);
+    j.skip = (int)(d - j.d < V ? d - j.d : V);
   }
   return j;
 }
@@ -324,8 +351,9 @@ __device__ __forceinline__ void state_before(const ScanArgs& s, const ScanPlan& 
     W A[V], X[V], end[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      A[v] = i < chunk ? slot<W>(s, i + 1)[at + v] : (W)1;
-      X[v] = i < chunk ? slot<W>(s, i + 1)[n + at + v] : (W)0;
+      const bool has = i < chunk;
+      A[v] = has ? slot<W>(s, i + 1)[at + v] : (W)1;
+      X[v] = has ? slot<W>(s, i + 1)[n + at + v] : (W)0;
     }
     __syncthreads();
     scan_tile<W, V>(q, A, X, h, end, lds.v[0]);
@@ -342,7 +370,7 @@ __global__ __launch_bounds__(kThreads) void scan_runs_k(ScanArgs s, ScanPlan p) 
   __shared__ ScanLds<W, V> lds;
   const Place q = place_of(p);
   const bool back = GRAD ? !s.c.reverse : s.c.reverse != 0;
-  const Job j = job_of<V, TV>(p, q, s.c, blockIdx.x);
+  const Job j = job_of<V, TV>(p, q, s.c, tile_of(p, blockIdx.x));
   const int n = seq_len(s, j.b, false), T = (int)s.c.T;
   const int64_t at = j.b * s.c.D + j.d, bd = s.c.B * s.c.D;
   W A[V], X[V];
@@ -350,7 +378,7 @@ __global__ __launch_bounds__(kThreads) void scan_runs_k(ScanArgs s, ScanPlan p) 
   for (int v = 0; v < V; ++v) { A[v] = (W)1; X[v] = (W)0; }
   const int p0 = ((int)blockIdx.y * q.nseg + q.seg) * p.ctiles * L;
   for (int i = 0; i < p.ctiles; ++i) {
-    Where w{first_step<L, TV>(p0 + i * L, T, back), n, T, j.d, back, p.vec != 0};
+    Where w{first_step<L, TV>(p0 + i * L, T, back), n, T, j.d, j.skip, back, p.vec != 0};
     const bool all = whole<L>(w);
     Block<E, V, L, TV> g{}, x{};
     load(g, s.g, j.b, w, all);
@@ -387,6 +415,7 @@ __global__ __launch_bounds__(kThreads) void scan_runs_k(ScanArgs s, ScanPlan p) 
     W* o = slot<W>(s, blockIdx.y + 1);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
+      if (v < j.skip) continue;
       o[at + v] = prod[v];
       o[bd + at + v] = end[v];
       if (blockIdx.y == 0) slot<W>(s, 0)[at + v] = first ? static_cast<const W*>(first)[at + v] : (W)0;
@@ -401,14 +430,14 @@ __global__ __launch_bounds__(kThreads) void scan_tile_k(ScanArgs s, ScanPlan p) 
   const Place q = place_of(p);
   const bool back = s.c.reverse != 0;
   for (int64_t blk = blockIdx.x; blk < p.tiles; blk += gridDim.x) {
-    const Job j = job_of<V, TV>(p, q, s.c, blk);
+    const Job j = job_of<V, TV>(p, q, s.c, tile_of(p, blk));
     const int n = seq_len(s, j.b, q.seg == 0 && blockIdx.y == 0), T = (int)s.c.T;
     const int64_t at = j.b * s.c.D + j.d;
     W h[V];
     state_before<W, V>(s, p, q, j, blockIdx.y, s.h0, h, lds);
     const int span = q.nseg * L;
     const int p0 = (int)blockIdx.y * p.ctiles * span + q.seg * L;
-    Where w{first_step<L, TV>(p0, T, back), n, T, j.d, back, p.vec != 0};
+    Where w{first_step<L, TV>(p0, T, back), n, T, j.d, j.skip, back, p.vec != 0};
     Block<E, V, L, TV> g{}, x{};
     bool all = whole<L>(w);
     load(g, s.g, j.b, w, all);
@@ -475,7 +504,8 @@ __global__ __launch_bounds__(kThreads) void scan_tile_k(ScanArgs s, ScanPlan p) 
             last[v] = !none && now.t(l, L) == tl ? fma_w(A[l][v], in[v], X[l][v]) : last[v];
         }
 #pragma unroll
-        for (int v = 0; v < V; ++v) static_cast<W*>(s.state)[at + v] = last[v];
+        for (int v = 0; v < V; ++v)
+          if (v >= j.skip) static_cast<W*>(s.state)[at + v] = last[v];
       }
       if (q.nwv > 1) {
 #pragma unroll
@@ -493,7 +523,7 @@ __global__ __launch_bounds__(kThreads) void scan_grad_k(ScanArgs s, ScanPlan p) 
   const Place q = place_of(p);
   const bool back = !s.c.reverse;
   for (int64_t blk = blockIdx.x; blk < p.tiles; blk += gridDim.x) {
-    const Job j = job_of<V, TV>(p, q, s.c, blk);
+    const Job j = job_of<V, TV>(p, q, s.c, tile_of(p, blk));
     const int n = seq_len(s, j.b, q.seg == 0 && blockIdx.y == 0), T = (int)s.c.T;
     const int64_t at = j.b * s.c.D + j.d;
     W C[V], h0[V];
@@ -503,7 +533,7 @@ __global__ __launch_bounds__(kThreads) void scan_grad_k(ScanArgs s, ScanPlan p) 
     const int span = q.nseg * L;
     const int p0 = (int)blockIdx.y * p.ctiles * span + q.seg * L;
     for (int i = 0; i < p.ctiles; ++i) {
-      const Where w{first_step<L, TV>(p0 + i * span, T, back), n, T, j.d, back, p.vec != 0};
+      const Where w{first_step<L, TV>(p0 + i * span, T, back), n, T, j.d, j.skip, back, p.vec != 0};
       Block<E, V, L, TV> g{}, dy{}, y{}, x{};
       const int before = s.c.reverse ? 1 : -1;   // from a step to the one whose state it starts from
       const bool all = whole<L>(w, before);
@@ -561,7 +591,8 @@ __global__ __launch_bounds__(kThreads) void scan_grad_k(ScanArgs s, ScanPlan p) 
         if (s.dx.data) store(ox, s.dx, j.b, w, all);
         if (i + 1 == p.ctiles && (int)blockIdx.y + 1 == p.chunks && s.state && q.seg == q.nseg - 1) {
 #pragma unroll
-          for (int v = 0; v < V; ++v) static_cast<W*>(s.state)[at + v] = c[v];
+          for (int v = 0; v < V; ++v)
+            if (v >= j.skip) static_cast<W*>(s.state)[at + v] = c[v];
         }
       }
       if (q.nwv > 1) {
@@ -593,8 +624,7 @@ __global__ __launch_bounds__(kThreads) void scan_step_k(ScanArgs s) {
     const int64_t t = s.c.reverse ? s.c.T - 1 - p : p;
     Vec out{};
     if (t < n) {
-      const Vec gv = *reinterpret_cast<const Vec*>(g + t * s.g.stride_t);
-      const Vec xv = *reinterpret_cast<const Vec*>(x + t * s.x.stride_t);
+      const Vec gv = read<T, V>(g + t * s.g.stride_t), xv = read<T, V>(x + t * s.x.stride_t);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         W a, r;
@@ -609,7 +639,7 @@ __global__ __launch_bounds__(kThreads) void scan_step_k(ScanArgs s) {
         }
       }
     }
-    if (s.y.data) *reinterpret_cast<Vec*>(y + t * s.y.stride_t) = out;
+    if (s.y.data) write<T, V>(y + t * s.y.stride_t, out);
   }
   if (s.state) {
 #pragma unroll
@@ -641,7 +671,7 @@ constexpr int vec_steps(int eb, bool grad) {
 }
 
 ScanPlan plan_of(const sim_scan& c, bool grad, bool time, bool vec) {
-  const int eb = elem_bytes(c), V = time || !vec ? 1 : vec_channels(eb);
+  const int eb = elem_bytes(c), V = time || c.D < vec_channels(eb) ? 1 : vec_channels(eb);
   ScanPlan p{};
   p.time = time;
   p.vec = vec;
@@ -653,9 +683,9 @@ ScanPlan plan_of(const sim_scan& c, bool grad, bool time, bool vec) {
     p.per = 1;
     total = ((c.T + kStepsT - 1) / kStepsT + (1 << p.gs) - 1) >> p.gs;
   } else {
-    const int L = vec ? vec_steps(eb, grad) : (grad ? kStepsG1 : kSteps1);
+    const int L = V > 1 ? vec_steps(eb, grad) : (grad ? kStepsG1 : kSteps1);
     const int64_t wide = (c.D + V - 1) / V;   // threads that the channels need
-    p.lx = std::min(ceil_log2(wide), vec ? ceil_log2(kRow / (V * eb)) : 5);
+    p.lx = std::min(ceil_log2(wide), ceil_log2(kRow / (V * eb)));
     // shorter sequences: more channels and fewer segments
     while (p.lx < 6 && ((int64_t)1 << p.lx) < wide && (int64_t)(kThreads >> p.lx) * L >= 2 * c.T) ++p.lx;
     const int64_t chans = (int64_t)V << p.lx, span = (int64_t)(kThreads >> p.lx) * L;
@@ -677,9 +707,20 @@ size_t plan_bytes(const sim_scan& c, const ScanPlan& p) {
   return (size_t)(p.chunks + 1) * 2 * c.B * c.D * (c.dtype == SIM_DT_F64 ? 8 : 4);
 }
 
+// whether every row of every array in use starts on a cache line
+bool on_lines(const ScanArgs& a) {
+  const int eb = elem_bytes(a.c);
+  for (const sim_seq* q : {&a.g, &a.x, &a.y, &a.dy, &a.dg, &a.dx})
+    if (q->data && (reinterpret_cast<uintptr_t>(q->data) % 128 || (a.c.B > 1 && q->stride_b * eb % 128) ||
+                    (a.c.T > 1 && q->stride_t * eb % 128)))
+      return false;
+  return true;
+}
+
 template <class E, bool SIG, int V, int L, int LG, bool TV>
 void run(const ScanArgs& a, bool grad, bool vec, hipStream_t st) {
-  const ScanPlan p = plan_of(a.c, grad, TV, vec);
+  ScanPlan p = plan_of(a.c, grad, TV, vec);
+  p.runs = !TV && !on_lines(a);
   const dim3 grid((unsigned)std::min<int64_t>(p.tiles, kMaxGrid), (unsigned)p.chunks), block(kThreads);
   if (p.chunks > 1) {
     const dim3 runs((unsigned)p.tiles, (unsigned)p.chunks - 1);
@@ -688,18 +729,6 @@ void run(const ScanArgs& a, bool grad, bool vec, hipStream_t st) {
   }
   if (grad) hipLaunchKernelGGL((scan_grad_k<E, SIG, V, LG, TV>), grid, block, 0, st, a, p);
   else hipLaunchKernelGGL((scan_tile_k<E, SIG, V, L, TV>), grid, block, 0, st, a, p);
-}
-
-// whether every array in use is aligned to whole accesses wherever a block may start
-bool vec_ok(const ScanArgs& a, bool time) {
-  const int eb = elem_bytes(a.c), n = time ? 16 : vec_channels(eb) * eb;
-  for (const sim_seq* q : {&a.g, &a.x, &a.y, &a.dy, &a.dg, &a.dx}) {
-    if (!q->data) continue;
-    if (reinterpret_cast<uintptr_t>(q->data) % n) return false;
-    if (a.c.B > 1 && q->stride_b * eb % n) return false;
-    if (time ? q->stride_t != 1 && a.c.T > 1 : a.c.T > 1 && q->stride_t * eb % n) return false;
-  }
-  return time || a.c.D * eb % n == 0;
 }
 
 template <class E, bool SIG>
@@ -713,18 +742,21 @@ hipError_t go(ScanArgs a, bool grad, hipStream_t st) {
     a.c.D *= a.c.B;
     a.c.B = 1;
   }
-  bool time = a.c.D == 1 && a.c.T > 1;
-  for (const sim_seq* q : {&a.g, &a.x, &a.y, &a.dy, &a.dg, &a.dx})
-    if (q->data && q->stride_t > 1) time = false;
+  bool time = a.c.D == 1 && a.c.T > 1, adjacent = true;
+  for (const sim_seq* q : {&a.g, &a.x, &a.y, &a.dy, &a.dg, &a.dx}) {
+    if (!q->data) continue;
+    if (q->stride_t > 1) time = false;
+    if (q->stride_t != 1) adjacent = false;
+  }
   if (!grad && a.c.T <= kStepT) {
-    const bool v = vec_ok(a, false);
+    const bool v = a.c.D % V == 0;
     const int64_t n = a.c.B * (v ? a.c.D / V : a.c.D);
     const dim3 grid((unsigned)((n + kThreads - 1) / kThreads)), block(kThreads);
     if (v) hipLaunchKernelGGL((scan_step_k<E, SIG, V>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((scan_step_k<E, SIG, 1>), grid, block, 0, st, a);
   } else if (time) {
-    run<E, SIG, 1, kStepsT, kStepsT, true>(a, grad, vec_ok(a, true), st);
-  } else if (vec_ok(a, false)) {
+    run<E, SIG, 1, kStepsT, kStepsT, true>(a, grad, adjacent, st);
+  } else if (a.c.D >= V) {
     run<E, SIG, V, vec_steps(eb, false), vec_steps(eb, true), false>(a, grad, true, st);
   } else {
     run<E, SIG, 1, kSteps1, kStepsG1, false>(a, grad, false, st);
@@ -746,7 +778,6 @@ size_t scan_work_bytes(const sim_scan& c, bool grad) {
   flat.B = 1;
   for (const sim_scan& s : {c, flat}) {
     need = std::max(need, plan_bytes(s, plan_of(s, grad, false, true)));
-    need = std::max(need, plan_bytes(s, plan_of(s, grad, false, false)));
     if (s.D == 1) need = std::max(need, plan_bytes(s, plan_of(s, grad, true, true)));
   }
   return need;
