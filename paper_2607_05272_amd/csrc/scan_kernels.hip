@@ -654,8 +654,9 @@ constexpr int kHold = 64;             // bytes of an array that a thread holds s
 constexpr int kHoldG = 16;            // at most so many elements in the gradient, which holds four arrays
 constexpr int kSteps1 = 16, kStepsG1 = 8;   // L of single elements along the channels
 constexpr int kStepsT = 8;            // L along time
-constexpr int kRow = 128;             // bytes of a step that a workgroup takes: a cache line
-constexpr int kWant = 512;            // workgroups that keep HBM busy
+constexpr int kRow = 128;             // a cache line
+constexpr int kEnough = 200;          // workgroups that keep HBM busy
+constexpr int kWant = 512;            // of a sequence split over time
 constexpr int64_t kMaxGrid = 1 << 22;
 
 int ceil_log2(int64_t x) {
@@ -668,6 +669,38 @@ int elem_bytes(const sim_scan& c) { return c.dtype == SIM_DT_F64 ? 8 : (c.dtype 
 constexpr int vec_channels(int eb) { return kChans * eb < 16 ? kChans : 16 / eb; }
 constexpr int vec_steps(int eb, bool grad) {
   return (grad && kHold / eb > kHoldG ? kHoldG : kHold / eb) / vec_channels(eb);
+}
+
+// workgroups side by side if 1 << lx threads share a row
+int64_t tiles_of(const sim_scan& c, int V, int lx) {
+  const int64_t chans = (int64_t)V << lx;
+  return c.B * ((c.D + chans - 1) / chans);
+}
+// How much of a row a workgroup takes: a cache line if that leaves enough workgroups (the gradient, which
+// loads nothing ahead, needs more). With fewer channels narrower pieces, down to 16 bytes, as long as
+// that is enough or the sequence is short; otherwise lines again, and time is split. With many channels
+// wider pieces, whose scans have fewer segments, for the larger types. Us at pieces of 16, 32, 64, 128,
+// 256, 512, 1024 bytes (forward or, t, with the gradient):
+//   fp64 1 x 1000 x 256   6.1   6.8   9.7   9.4   9.7  13   27     fp64 1 x 990 x 1218   14.5 13.5 17.4 17.3 19  19  24
+//   fp64 1 x 2000 x 4000  78    55    42    39    58   60   63     fp64 1 x 1365 x 26752 -    508  283  209  -   182 164
+//   bf16 4 x 500 x 512    6.8   6.7   9.4   12.9  14   19   30     bf16 11 x 3232 x 153  23.8 29.7 26.6 26.6 36  47  47
+//   t fp32 2 x 2000 x 1024  45  38    47    44    46   62  109     t bf16 1 x 8000 x 1024  86 71   66   67   94  188 430
+//   fp32 1 x 1365 x 26752  184 135   114   101    92   94  145     t bf16 8 x 2048 x 2048  249 217 181  221  220 222 211
+int row_threads(const sim_scan& c, bool grad, int V, int L) {
+  const int piece = V * elem_bytes(c), line = ceil_log2(kRow / piece);
+  int lx = line;
+  if (tiles_of(c, V, lx) >= (grad ? 2 * kEnough : kEnough)) {
+    const int widest = grad ? lx : (piece / V == 8 ? lx + 3 : (piece / V == 4 ? lx + 1 : lx));
+    const int64_t enough = piece / V == 8 ? kEnough : 2 * kEnough;
+    while (lx < std::min(widest, 6) && tiles_of(c, V, lx + 1) >= enough) ++lx;
+    return lx;
+  }
+  const int narrowest = ceil_log2(std::max(1, 16 / piece));
+  while (lx > narrowest) {
+    --lx;
+    if (tiles_of(c, V, lx) >= kEnough) return lx;
+  }
+  return (int64_t)(kThreads >> lx) * L * 2 >= c.T ? lx : line;
 }
 
 ScanPlan plan_of(const sim_scan& c, bool grad, bool time, bool vec) {
@@ -685,9 +718,10 @@ ScanPlan plan_of(const sim_scan& c, bool grad, bool time, bool vec) {
   } else {
     const int L = V > 1 ? vec_steps(eb, grad) : (grad ? kStepsG1 : kSteps1);
     const int64_t wide = (c.D + V - 1) / V;   // threads that the channels need
-    p.lx = std::min(ceil_log2(wide), ceil_log2(kRow / (V * eb)));
+    p.lx = std::min(ceil_log2(wide), row_threads(c, grad, V, L));
     // shorter sequences: more channels and fewer segments
-    while (p.lx < 6 && ((int64_t)1 << p.lx) < wide && (int64_t)(kThreads >> p.lx) * L >= 2 * c.T) ++p.lx;
+    while (p.lx < 6 && ((int64_t)1 << p.lx) < wide && (int64_t)(kThreads >> p.lx) * L >= 2 * c.T &&
+           tiles_of(c, V, p.lx) >= 2 * kEnough) ++p.lx;
     const int64_t chans = (int64_t)V << p.lx, span = (int64_t)(kThreads >> p.lx) * L;
     p.per = (c.D + chans - 1) / chans;
     p.tiles = c.B * p.per;
@@ -695,7 +729,7 @@ ScanPlan plan_of(const sim_scan& c, bool grad, bool time, bool vec) {
   }
   if (total < 1) total = 1;
   int64_t want = p.tiles ? kWant / p.tiles : 1;
-  if (p.tiles > kWant / 3 || total < 4) want = 1;
+  if (p.tiles >= kEnough || total < 4) want = 1;
   if (want > total) want = total;
   p.ctiles = (int)((total + want - 1) / want);
   p.chunks = (int)((total + p.ctiles - 1) / p.ctiles);
@@ -720,7 +754,7 @@ bool on_lines(const ScanArgs& a) {
 template <class E, bool SIG, int V, int L, int LG, bool TV>
 void run(const ScanArgs& a, bool grad, bool vec, hipStream_t st) {
   ScanPlan p = plan_of(a.c, grad, TV, vec);
-  p.runs = !TV && !on_lines(a);
+  p.runs = !TV && (!on_lines(a) || (V * elem_bytes(a.c) << p.lx) < kRow);
   const dim3 grid((unsigned)std::min<int64_t>(p.tiles, kMaxGrid), (unsigned)p.chunks), block(kThreads);
   if (p.chunks > 1) {
     const dim3 runs((unsigned)p.tiles, (unsigned)p.chunks - 1);
