@@ -81,9 +81,20 @@ __device__ __forceinline__ void add_lanes(float& S, float& X, int lg) {
     X += __shfl_xor(X, o);
   }
 }
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp(double v) {   // 0 where there is no source
+  const uint64_t u = __double_as_longlong(v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0u, (uint32_t)u, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0u, (uint32_t)(u >> 32), CTRL, ROWS, 0xf, false);
+  return __longlong_as_double((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double wave_sum(double v) {   // in lane 63
+  v += dpp<0x111, 0xf>(v);
+  v += dpp<0x112, 0xf>(v);
+  v += dpp<0x114, 0xf>(v);
+  v += dpp<0x118, 0xf>(v);
+  v += dpp<0x142, 0xa>(v);
+  v += dpp<0x143, 0xc>(v);
   return v;
 }
 
@@ -317,22 +328,19 @@ __device__ __forceinline__ void leave(const typename OP::Args& s, Sums v, double
     v.b = wave_sum(v.b);
     v.c = wave_sum(v.c);
   }
-  if (lane == 0) { lds[wave][0] = v.a; lds[wave][1] = v.b; lds[wave][2] = v.c; }
+  if (lane == 63) { lds[wave][0] = v.a; lds[wave][1] = v.b; lds[wave][2] = v.c; }
   __syncthreads();
   if (wave == 0) {
     Sums t{0.0, 0.0, 0.0};
     if (lane < nw) t = Sums{lds[lane][0], lds[lane][1], lds[lane][2]};
-#pragma unroll
-    for (int o = 8; o; o >>= 1) {   // at most 16 waves
-      t.a += __shfl_xor(t.a, o);
-      t.b += __shfl_xor(t.b, o);
-      t.c += __shfl_xor(t.c, o);
-    }
-    if (lane == 0) {
-      if (gridDim.x == 1) {
+    t.a = wave_sum(t.a);
+    t.b = wave_sum(t.b);
+    t.c = wave_sum(t.c);
+    if (lane == 63) {
+      if (gridDim.x * gridDim.y == 1) {
         OP::finish(s, t);
       } else {
-        double* o = static_cast<double*>(s.work) + 3 * blockIdx.x;
+        double* o = static_cast<double*>(s.work) + 3 * (blockIdx.x * gridDim.y + blockIdx.y);
         o[0] = t.a; o[1] = t.b; o[2] = t.c;
       }
     }
@@ -532,6 +540,15 @@ __device__ __forceinline__ Part join_waves(Part p, Part* lds) {
   return r;
 }
 
+// a thread's part joined over its workgroup
+template <bool BAL, int NW>
+__device__ __forceinline__ Part join_threads(Part p, Part* lds) {
+  p = against<BAL>(p, wave_max(p.m));
+  p.S = wave_add(p.S);
+  p.X = wave_add(p.X);
+  return join_waves<BAL, NW>(p, lds);
+}
+
 // Longer rows: a workgroup takes a row and holds it as it was read, R chunks a thread; while a chunk's
 // gradient goes out the same chunk of the workgroup's next row comes in. Places past the row's end hold
 // -inf.
@@ -623,10 +640,7 @@ __global__ __launch_bounds__(NT, 4) void policy_block_k(PolicyLossArgs s) {
           }
         }
       }
-      p = against<false>(p, wave_max(p.m));
-      p.S = wave_add(p.S);
-      p.X = wave_add(p.X);
-      p = join_waves<false, NW>(p, parts[use]);
+      p = join_threads<false, NW>(p, parts[use]);
       on = OP::close(s, n, row, p, NW == 1 ? la : taken[use], threadIdx.x == 0, sums, o);
       m = p.m;
       use ^= 1;   // only a row with a barrier between frees the other buffer
@@ -666,120 +680,185 @@ __global__ __launch_bounds__(NT, 4) void policy_block_k(PolicyLossArgs s) {
   leave<OP>(s, sums, lds);
 }
 
-// Rows that no workgroup's registers hold: read twice.
+// A run of a row's logits, read where it lies: chunks [c0, c1) and, if `tail`, the elements past the whole
+// chunks, by NT threads.
+template <class OP, class E, int NT>
+struct Run {
+  typedef typename E::T T;
+  static constexpr int N = 16 / sizeof(T), U = 4;
+  typedef Chunk<E, N> Ch;
+  const typename OP::Args& s;
+  const float* f;
+  const T* l;
+  const uint8_t* mk = nullptr;
+  int64_t ms = 0;
+  int c0, c1, whole;
+  bool tail;
+
+  __device__ __forceinline__ Run(const typename OP::Args& s_, const float* f_, int64_t n, int c0_, int c1_, bool tail_)
+      : s(s_), f(f_), l(static_cast<const T*>(s_.l.data) + n * s_.l.stride_n), c0(c0_), c1(c1_), whole(s_.c.A / N), tail(tail_) {
+    if constexpr (!OP::kBal) {
+      if (s.mask.data) mk = static_cast<const uint8_t*>(s.mask.data) + n * s.mask.stride_n;
+      ms = s.mask.stride_a;
+    }
+  }
+  __device__ __forceinline__ float factor(int j, float x) const { return OP::kBal ? target(s, f, j) : x; }
+  __device__ __forceinline__ float logit(int j) const { return !mk || mk[j * ms] ? (float)l[j] : -INFINITY; }
+  __device__ __forceinline__ void fetch(int c, Ch (&ch)[U], MaskBytes<N> (&mb)[U]) const {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (c + u * NT < c1) {
+        ch[u].load(l + (int64_t)(c + u * NT) * N);
+        if (mk) mb[u].load(mk + (int64_t)(c + u * NT) * N * ms, ms);
+      }
+    }
+  }
+  // the thread's part
+  __device__ __forceinline__ Part part() const {
+    Part p{-INFINITY, 0.0f, 0.0f};
+    for (int at = c0 + threadIdx.x; at < c1; at += U * NT) {
+      Ch ch[U];
+      MaskBytes<N> mb[U];
+      fetch(at, ch, mb);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = at + u * NT;
+        if (c >= c1) continue;
+        float v[N], M = p.m;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          v[i] = !mk || mb[u].open(i) ? ch[u].get(i) : -INFINITY;
+          M = max_nan(M, v[i]);
+        }
+        if (M == -INFINITY) continue;
+        p = against<OP::kBal>(p, M);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float x = max_nan(v[i] - M, kLowest), e = exp_of(x);
+          p.S += e;
+          p.X = fmaf(e, factor(c * N + i, x), p.X);
+        }
+      }
+    }
+    for (int j = whole * N + threadIdx.x; tail && j < s.c.A; j += NT) {
+      const float v = logit(j), M = max_nan(p.m, v);
+      if (M == -INFINITY) continue;
+      p = against<OP::kBal>(p, M);
+      const float x = max_nan(v - M, kLowest), e = exp_of(x);
+      p.S += e;
+      p.X = fmaf(e, factor(j, x), p.X);
+    }
+    return p;
+  }
+  // the gradient, 0 if the row is not on
+  __device__ __forceinline__ void slopes(T* out, bool on, float m, const RowOut& o, int64_t act) const {
+    auto slope = [&](int j, float v) {
+      const float x = max_nan(v - m, kLowest), w = exp_of(x) * fmaf(o.beta, factor(j, x), o.alpha);
+      return act == j ? w + o.delta : w;
+    };
+    for (int at = c0 + threadIdx.x; at < c1; at += U * NT) {
+      Ch ch[U];
+      MaskBytes<N> mb[U];
+      if (on) fetch(at, ch, mb);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = at + u * NT;
+        if (c >= c1) continue;
+        typename Ch::Wide w{};
+        if (on) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) w[i] = slope(c * N + i, !mk || mb[u].open(i) ? ch[u].get(i) : -INFINITY);
+        }
+        Ch::store(out + (int64_t)c * N, w);
+      }
+    }
+    for (int j = whole * N + threadIdx.x; tail && j < s.c.A; j += NT) out[j] = (T)(on ? slope(j, logit(j)) : 0.0f);
+  }
+};
+// Rows that no workgroup's registers hold: a workgroup reads a row twice.
 constexpr int kStream = 1024;
 template <class OP, class E>
 __global__ __launch_bounds__(kStream) void loss_stream_k(typename OP::Args s, int nb) {
   typedef typename E::T T;
-  constexpr int N = 16 / sizeof(T), NW = kStream / 64, U = 4;
-  typedef Chunk<E, N> Ch;
+  constexpr int NW = kStream / 64;
   __shared__ double lds[NW][3];
   __shared__ Part parts[2][NW];
   __shared__ float taken[2];
   __shared__ float f[OP::kBal ? kMaxTargets : 1];
   fill_targets(s, nb, f);
-  const int A = s.c.A, whole = A / N;
   T* g = static_cast<T*>(s.grad.data);
   Sums sums{0.0, 0.0, 0.0};
   int use = 0;
   for (int64_t n = blockIdx.x; n < s.c.N; n += gridDim.x) {
     typename OP::Row row;
     bool on = OP::open(s, n, row);
-    const T* l = static_cast<const T*>(s.l.data) + n * s.l.stride_n;
-    const uint8_t* mk = nullptr;
-    int64_t ms = 0;
-    if constexpr (!OP::kBal) {
-      if (s.mask.data) mk = static_cast<const uint8_t*>(s.mask.data) + n * s.mask.stride_n;
-      ms = s.mask.stride_a;
-    }
-    auto factor = [&](int j, float x) { return OP::kBal ? target(s, f, j) : x; };
+    const Run<OP, E, kStream> run(s, f, n, 0, s.c.A / Run<OP, E, kStream>::N, true);
     RowOut o{0.0f, 0.0f, 0.0f};
     float m = 0.0f;
     if (on) {
       if (threadIdx.x == 0) taken[use] = OP::template taken<T>(s, n, row);
-      Part p{-INFINITY, 0.0f, 0.0f};
-      auto one = [&](int j, float v) {   // an element, against the maximum so far
-        const float M = max_nan(p.m, v);
-        p = against<OP::kBal>(p, M);
-        const float x = M == -INFINITY ? kLowest : max_nan(v - M, kLowest), e = exp_of(x);
-        p.S += e;
-        p.X = fmaf(e, factor(j, x), p.X);
-      };
-      for (int c0 = threadIdx.x; c0 < whole; c0 += U * kStream) {
-        Ch ch[U];
-        MaskBytes<N> mb[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int c = c0 + u * kStream;
-          if (c < whole) {
-            ch[u].load(l + c * N);
-            if (mk) mb[u].load(mk + (int64_t)c * N * ms, ms);
-          }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int c = c0 + u * kStream;
-          if (c >= whole) continue;
-          float v[N], M = p.m;
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            v[i] = !mk || mb[u].open(i) ? ch[u].get(i) : -INFINITY;
-            M = max_nan(M, v[i]);
-          }
-          if (M == -INFINITY) continue;
-          p = against<OP::kBal>(p, M);
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const float x = max_nan(v[i] - M, kLowest), e = exp_of(x);
-            p.S += e;
-            p.X = fmaf(e, factor(c * N + i, x), p.X);
-          }
-        }
-      }
-      for (int j = whole * N + threadIdx.x; j < A; j += kStream) one(j, !mk || mk[j * ms] ? (float)l[j] : -INFINITY);
-      p = against<OP::kBal>(p, wave_max(p.m));
-      p.S = wave_add(p.S);
-      p.X = wave_add(p.X);
-      p = join_waves<OP::kBal, NW>(p, parts[use]);
+      const Part p = join_threads<OP::kBal, NW>(run.part(), parts[use]);
       on = OP::close(s, n, row, p, taken[use], threadIdx.x == 0, sums, o);
       m = p.m;
-      use ^= 1;
+      use ^= 1;   // only a row with a barrier between frees the other buffer
     }
     if (!on && threadIdx.x == 0) OP::shut(s, n);
-    if (!g) continue;
-    T* out = g + n * s.grad.stride_n;
-    auto slope = [&](int j, float v) {
-      const float x = max_nan(v - m, kLowest);
-      const float w = exp_of(x) * fmaf(o.beta, factor(j, x), o.alpha);
-      return on ? (row.act == j ? w + o.delta : w) : 0.0f;
-    };
-    for (int c0 = threadIdx.x; c0 < whole; c0 += U * kStream) {
-      Ch ch[U];
-      MaskBytes<N> mb[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int c = c0 + u * kStream;
-        if (c < whole && on) {
-          ch[u].load(l + c * N);
-          if (mk) mb[u].load(mk + (int64_t)c * N * ms, ms);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int c = c0 + u * kStream;
-        if (c >= whole) continue;
-        typename Ch::Wide w{};
-        if (on) {
-#pragma unroll
-          for (int i = 0; i < N; ++i) w[i] = slope(c * N + i, !mk || mb[u].open(i) ? ch[u].get(i) : -INFINITY);
-        }
-        Ch::store(out + c * N, w);
-      }
-    }
-    for (int j = whole * N + threadIdx.x; j < A; j += kStream)
-      out[j] = (T)(on ? slope(j, !mk || mk[j * ms] ? (float)l[j] : -INFINITY) : 0.0f);
+    if (g) run.slopes(g + n * s.grad.stride_n, on, m, o, row.act);
   }
   leave<OP>(s, sums, lds);
+}
+
+// Few long rows: gridDim.y workgroups share each, in two launches. The work memory past the sums holds
+// their parts [N][gridDim.y] and the taken actions' logits [N] (the gradient may overwrite them).
+constexpr int kSplit = 256, kSplitMost = 1024;
+__device__ __forceinline__ Part* split_parts(const PolicyLossArgs& s) {
+  return reinterpret_cast<Part*>(static_cast<double*>(s.work) + 3 * kMaxBlocks);
+}
+template <class E>
+__device__ __forceinline__ Run<PolicyOp, E, kSplit> split_run(const PolicyLossArgs& s) {
+  const int whole = s.c.A / Run<PolicyOp, E, kSplit>::N, k = gridDim.y, i = blockIdx.y;
+  return Run<PolicyOp, E, kSplit>(s, nullptr, blockIdx.x, (int)((int64_t)whole * i / k),
+                                  (int)((int64_t)whole * (i + 1) / k), i + 1 == k);
+}
+template <class E>
+__global__ __launch_bounds__(kSplit) void policy_parts_k(PolicyLossArgs s) {
+  __shared__ Part lds[kSplit / 64];
+  PolicyOp::Row row;
+  if (!PolicyOp::open(s, blockIdx.x, row)) return;   // the same in the whole workgroup
+  float la = 0.0f;
+  if (blockIdx.y == 0 && threadIdx.x == 0) la = PolicyOp::taken<typename E::T>(s, blockIdx.x, row);
+  const Part p = join_threads<false, kSplit / 64>(split_run<E>(s).part(), lds);
+  if (threadIdx.x != 0) return;
+  split_parts(s)[blockIdx.x * gridDim.y + blockIdx.y] = p;
+  if (blockIdx.y == 0) reinterpret_cast<float*>(split_parts(s) + kSplitMost)[blockIdx.x] = la;
+}
+template <class E>
+__global__ __launch_bounds__(kSplit) void policy_slopes_k(PolicyLossArgs s) {
+  typedef typename E::T T;
+  __shared__ double lds[kSplit / 64][3];
+  const int64_t n = blockIdx.x;
+  Sums sums{0.0, 0.0, 0.0};
+  PolicyOp::Row row;
+  bool on = PolicyOp::open(s, n, row);
+  const bool first = blockIdx.y == 0 && threadIdx.x == 0;
+  RowOut o{0.0f, 0.0f, 0.0f};
+  float m = 0.0f;
+  if (on) {
+    const Part* parts = split_parts(s) + n * gridDim.y;
+    float M = -INFINITY;
+    for (int i = 0; i < gridDim.y; ++i) M = max_nan(M, parts[i].m);
+    Part p{M, 0.0f, 0.0f};
+    for (int i = 0; i < gridDim.y; ++i) {
+      const Part q = against<false>(parts[i], M);
+      p.S += q.S;
+      p.X += q.X;
+    }
+    on = PolicyOp::close(s, n, row, p, reinterpret_cast<const float*>(split_parts(s) + kSplitMost)[n], first, sums, o);
+    m = p.m;
+  }
+  if (!on && first) PolicyOp::shut(s, n);
+  if (s.grad.data) split_run<E>(s).slopes(static_cast<T*>(s.grad.data) + n * s.grad.stride_n, on, m, o, row.act);
+  leave<PolicyOp>(s, sums, lds);
 }
 
 // ---- logits of adjacent samples: [A][N] --------------------------------------------------------
@@ -1020,6 +1099,7 @@ int blocks_for(int64_t N, int per, int most) {
 }
 
 constexpr int kHeld = 16;             // chunks of a row that a thread holds
+constexpr int kSplitFrom = 4, kSplitChunks = 4096;   // workgroups that share a row, from which length
 constexpr int kFill = 256 * 1024;     // threads that fill the chip while they hold a row (128 registers each)
 
 // Launches the form for these sizes and strides; the workgroups that left sums.
@@ -1062,6 +1142,16 @@ int launch_rows(const typename OP::Args& a, int nb, hipStream_t st) {
     return g;
   }
   if constexpr (!OP::kBal) {
+    // Few long rows are shared by as many workgroups as fill the chip and have a chunk a thread; the second
+    // launch takes about 3 us (us shared and not, bf16: 16 x 16000 12.0, 11.1; 16 x 50000 14.2, 16.4; 16 x
+    // 150000 15.8, 36.8; 60 x 73246 18.5, 21.3; 100 x 20000 13.8, 12.4; fp32 308 x 27036 by two 26.0, 23.0).
+    const int share = (int)std::min<int64_t>((2 * 256 + rows - 1) / std::max<int64_t>(rows, 1), chunks / kSplit);
+    if (share >= kSplitFrom && chunks >= kSplitChunks && rows * share <= kSplitMost) {
+      const dim3 grid((unsigned)rows, (unsigned)share), block(kSplit);
+      hipLaunchKernelGGL(policy_parts_k<E>, grid, block, 0, st, a);
+      hipLaunchKernelGGL(policy_slopes_k<E>, grid, block, 0, st, a);
+      return (int)rows * share;
+    }
     // the fewest threads that hold a row, more where there are too few rows to fill the chip
     int nt = 64;
     while (nt < 1024 && (chunks > kHeld * nt || (nt < 512 && rows * nt < kFill && chunks > nt))) nt *= 2;
@@ -1097,7 +1187,9 @@ hipError_t launch_loss(const typename OP::Args& a, int nb, hipStream_t st) {
 
 }  // namespace
 
-size_t policy_loss_bytes(const sim_policy_loss&) { return (size_t)kMaxBlocks * 3 * sizeof(double); }
+size_t policy_loss_bytes(const sim_policy_loss&) {
+  return (size_t)kMaxBlocks * 3 * sizeof(double) + kSplitMost * (sizeof(Part) + sizeof(float));
+}
 
 hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st) { return launch_loss<PolicyOp>(a, 0, st); }
 
