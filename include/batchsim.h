@@ -475,7 +475,7 @@ int gated_scan_grad(sim_ctx* ctx, const sim_scan* s, const sim_seq* gate, const 
 
 /* Clipped policy loss with a KL term over logits of any network, and its gradient: the
  * surrogate of ppo_minibatch_grad (Sec. 4.3) without its network.
- *  N, A         samples (below 2^31) and actions
+ *  N, A         samples (below 2^31) and actions (below 2^30)
  *  dtype        of logits and gradient (not SIM_DT_F64)
  *  action_type  SIM_IT_*;  adv_type  SIM_DT_F32 or SIM_DT_F64 (as returns_gae writes them)
  *  clip         in (0, 1); c_kl, c_entropy >= 0                                          */
@@ -505,7 +505,7 @@ int policy_loss(sim_ctx* ctx, const sim_policy_loss* c, const sim_mat* logits, c
 
 /* Balance loss of a router (a policy that sends each request to one of several servers, Sec. 4.1,
  * or each token to k of A experts), its counts and its gradient.
- *  N, A, k      rows (below 2^31), columns, choices per row (N k below 2^31)
+ *  N, A, k      rows (below 2^31), columns (below 2^30), choices per row (N k below 2^31)
  *  group        consecutive columns that count as one target: 1, or 6 for this simulator's
  *               actions (server a/6); divides A, A/group <= 4096
  *  dtype        of logits and gradient (not SIM_DT_F64);  index_type  SIM_IT_*

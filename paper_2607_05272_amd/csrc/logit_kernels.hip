@@ -1146,7 +1146,7 @@ int launch_rows(const typename OP::Args& a, int nb, hipStream_t st) {
     // launch takes about 3 us (us shared and not, bf16: 16 x 16000 12.0, 11.1; 16 x 50000 14.2, 16.4; 16 x
     // 150000 15.8, 36.8; 60 x 73246 18.5, 21.3; 100 x 20000 13.8, 12.4; fp32 308 x 27036 by two 26.0, 23.0).
     const int share = (int)std::min<int64_t>((2 * 256 + rows - 1) / std::max<int64_t>(rows, 1), chunks / kSplit);
-    if (share >= kSplitFrom && chunks >= kSplitChunks && rows * share <= kSplitMost) {
+    if (rows > 0 && share >= kSplitFrom && chunks >= kSplitChunks && rows * share <= kSplitMost) {
       const dim3 grid((unsigned)rows, (unsigned)share), block(kSplit);
       hipLaunchKernelGGL(policy_parts_k<E>, grid, block, 0, st, a);
       hipLaunchKernelGGL(policy_slopes_k<E>, grid, block, 0, st, a);

@@ -50,6 +50,7 @@ bool fits(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t run, int eb) {
 // whether runs of `run` elements at n0 x n1 places share no element: the inner of the two
 // dimensions steps over a run, the outer one over all of the inner
 bool distinct(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t run) {
+  if (!n0 || !n1) return true;
   std::pair<int64_t, int64_t> d[2] = {{s0, n0}, {s1, n1}};
   if (d[1].first < d[0].first) std::swap(d[0], d[1]);
   __int128 span = run;
@@ -135,6 +136,7 @@ int check_policy(const sim_policy_loss* c, const char* who) {
   if (!c) return op_fail(SIM_EINVAL, "%s: sizes are NULL", who);
   if (c->N < 0 || c->N > kMax31) return op_fail(SIM_EINVAL, "%s: N must lie in [0, 2^31)", who);
   if (c->A < 1) return op_fail(SIM_EINVAL, "%s: A must be >= 1", who);
+  if (c->A >= (1 << 30)) return op_fail(SIM_EUNSUPPORTED, "%s: A must stay below 2^30", who);
   if (c->dtype < SIM_DT_F32 || c->dtype > SIM_DT_F16) return op_fail(SIM_EINVAL, "%s: logits of type %d", who, c->dtype);
   if (c->action_type < SIM_IT_U8 || c->action_type > SIM_IT_I64)
     return op_fail(SIM_EINVAL, "%s: unknown action type %d", who, c->action_type);
@@ -150,6 +152,7 @@ int check_balance(const sim_balance* c, const char* who) {
   if (!c) return op_fail(SIM_EINVAL, "%s: sizes are NULL", who);
   if (c->N < 0 || c->N > kMax31) return op_fail(SIM_EINVAL, "%s: N must lie in [0, 2^31)", who);
   if (c->A < 1 || c->k < 1) return op_fail(SIM_EINVAL, "%s: A and k must be >= 1", who);
+  if (c->A >= (1 << 30)) return op_fail(SIM_EUNSUPPORTED, "%s: A must stay below 2^30", who);
   if (c->N * c->k > kMax31) return op_fail(SIM_EUNSUPPORTED, "%s: N*k must stay below 2^31", who);
   if (c->group < 1 || c->A % c->group) return op_fail(SIM_EINVAL, "%s: group must divide A", who);
   if (c->A / c->group > 4096) return op_fail(SIM_EUNSUPPORTED, "%s: at most 4096 targets", who);

@@ -69,8 +69,9 @@ def check(sim, s, c_kl=0.3, c_entropy=0.2, **kw):
 
 SIZES = [(1, 1), (5, 2), (64, 6), (65, 7), (130, 25), (33, 48), (20, 64), (21, 65), (40, 96), (17, 97), (9, 128),
          (9, 130), (12, 255), (6, 256), (6, 512), (7, 515), (5, 1000), (4, 1025), (4, 2048), (4, 2051), (3, 4096),
-         (3, 4099), (3, 8192), (2, 8200), (2, 16391), (2, 33000), (2, 50257), (2, 70001), (1, 131072), (1, 150001),
-         (1, 300001)]
+         (3, 4099), (3, 8192), (3, 8195), (2, 8200), (2, 16391), (2, 33000), (2, 50257), (2, 70001), (1, 131072), (1, 150001),
+         (1, 300001), (40, 40000),
+         (20, 70000)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
@@ -245,6 +246,11 @@ def test_without_gradient_and_without_samples(sim):
     r = sim.policy_loss(e, torch.empty(0, dtype=torch.int64, device="cuda"), torch.empty(0, device="cuda"))
     sim.sync()
     assert (r["loss"] == 0).all() and r["grad"].shape == (0, 48)
+    for A in (1, 700, 5000, 200000):
+        for e in (torch.empty(0, A, device="cuda"), torch.empty(A, 0, device="cuda").t()):
+            r = sim.policy_loss(e, torch.empty(0, dtype=torch.int64, device="cuda"), torch.empty(0, device="cuda"))
+            sim.sync()
+            assert (r["loss"] == 0).all()
 
 
 def test_far_rows(sim):

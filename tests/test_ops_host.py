@@ -104,7 +104,7 @@ def test_scan_refusals(stub):
 
 def test_policy_refusals(stub):
     bad = [("N must", call("policy_loss", dict(N=-1))), ("N must", call("policy_loss", dict(N=1 << 31))),
-           ("A must", call("policy_loss", dict(A=0))), ("type 0", call("policy_loss", dict(dtype=0))),
+           ("A must", call("policy_loss", dict(A=0))), ("A must", call("policy_loss", dict(A=1 << 30))), ("type 0", call("policy_loss", dict(dtype=0))),
            ("action type", call("policy_loss", dict(action_type=3))), ("advantages", call("policy_loss", dict(adv_type=2))),
            ("clip", call("policy_loss", dict(clip=0.0))), ("clip", call("policy_loss", dict(clip=float("nan")))),
            (">= 0", call("policy_loss", dict(c_kl=-1.0))), ("reference", call("policy_loss", a5=None)),
@@ -127,7 +127,7 @@ def test_policy_refusals(stub):
 
 def test_balance_refusals(stub):
     bad = [("N must", call("balance_loss", dict(N=-1))), (">= 1", call("balance_loss", dict(k=0))),
-           (">= 1", call("balance_loss", dict(A=0))), ("N*k", call("balance_loss", dict(N=1 << 30, k=2))),
+           (">= 1", call("balance_loss", dict(A=0))), ("2^30", call("balance_loss", dict(A=1 << 30, group=1 << 20))), ("N*k", call("balance_loss", dict(N=1 << 30, k=2))),
            ("divide", call("balance_loss", dict(group=5))), ("divide", call("balance_loss", dict(group=-6))),
            ("4096", call("balance_loss", dict(A=4097, group=1), a0=mat(1, 4097), a3=mat(2, 4097))),
            ("index type", call("balance_loss", dict(index_type=-1))), ("type 0", call("balance_loss", dict(dtype=0))),
@@ -151,11 +151,12 @@ def test_every_size_launches_within_limits(stub):
                           (1, 1, 1 << 30), (1 << 20, 3, 7), (1, (1 << 30) - 1, 1), (16, 1025, 1536), (1, 300000, 5)], range(4), (0, 1))]
     calls += [call("policy_loss", dict(N=n, A=a, dtype=dt, action_type=t), a0=m(1, n, a), a7=m(2, n, a))
               for (n, a), dt, t, m in itertools.product(
-                  [(1, 1), (256, 6), (131072, 96), (2048, 50257), (4096, 131072), ((1 << 31) - 1, 3), (1, (1 << 31) - 1)],
+                  [(1, 1), (256, 6), (131072, 96), (2048, 50257), (4096, 131072), ((1 << 31) - 1, 3), (1, (1 << 30) - 1), (0, 6), (0, 700), (0, 5000),
+                   (0, 200000)],
                   (1, 2, 3), (0, 2), (lambda i, n, a: mat(i, a, 1), lambda i, n, a: mat(i, 1, n)))]
     calls += [call("balance_loss", dict(N=n, A=a, k=k, group=g, dtype=dt), a0=m(1, n, a), a3=m(2, n, a))
               for (n, a, k, g), dt, m in itertools.product(
-                  [(1, 1, 1, 1), (65536, 48, 1, 6), (131072, 128, 8, 1), ((1 << 30), 4096, 1, 1), (10, 1 << 30, 1, 1 << 20)],
+                  [(1, 1, 1, 1), (65536, 48, 1, 6), (131072, 128, 8, 1), ((1 << 30), 4096, 1, 1), (10, 1023 << 20, 1, 1 << 20), (0, 8, 1, 1)],
                   (1, 2, 3), (lambda i, n, a: mat(i, a, 1), lambda i, n, a: mat(i, 1, n)))]
     for c, (rc, msg, log) in zip(calls, ops_stub.run(stub, calls)):
         assert rc == 0, (c, msg)
