@@ -361,10 +361,6 @@ __global__ __launch_bounds__(kFinish) void loss_finish_k(typename OP::Args s, in
   leave<OP>(s, v, lds);
 }
 
-// A value that the compiler finds again in each round of a loop: it would otherwise keep a pointer of its
-// own for every access that depends on it and step them all from round to round, more registers than there are.
-__device__ __forceinline__ void fresh(int64_t& uniform) { asm volatile("" : "+s"(uniform)); }
-
 // ---- rows of adjacent logits -----------------------------------------------------------------
 // N elements of a row, at any alignment of the element type
 template <class E, int N>
@@ -382,12 +378,7 @@ struct Chunk {
   // Keeps the compiler from holding the widened elements of one pass for the next one: they would
   // take twice the registers (and spill) where the chunks just fit.
   __device__ __forceinline__ void forget() {
-    if constexpr (N * sizeof(T) == 16) {
-      typedef uint32_t Words __attribute__((ext_vector_type(4)));
-      Words w = __builtin_bit_cast(Words, v);
-      asm volatile("" : "+v"(w));
-      v = __builtin_bit_cast(Val, w);
-    }
+    if constexpr (N * sizeof(T) == 16) hide(v);
   }
   __device__ __forceinline__ static void store(T* p, const Wide& w) {
     if constexpr (N == 1) p[0] = (T)w[0];
@@ -647,7 +638,7 @@ __global__ __launch_bounds__(NT, 4) void policy_block_k(PolicyLossArgs s) {
     }
     if (!on && threadIdx.x == 0) OP::shut(s, n);
     int at0 = threadIdx.x * N;
-    asm volatile("" : "+v"(at0));   // the chunks' places are found again, not held from row to row
+    fresh(at0);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int at = at0 + r * NT * N;

@@ -36,6 +36,24 @@ __device__ __forceinline__ int64_t load_int(const void* p, int type, int64_t i) 
   return static_cast<const int64_t*>(p)[i];
 }
 
+// A value that the compiler finds again in each round of a loop: it would otherwise keep a pointer of its
+// own for every access that depends on it and step them all from round to round, more registers than there
+// are. The first is the same in all lanes of a wave.
+__device__ __forceinline__ void fresh(int64_t& uniform) { asm volatile("" : "+s"(uniform)); }
+__device__ __forceinline__ void fresh(int& v) { asm volatile("" : "+v"(v)); }
+
+// A value in registers that the compiler no longer knows, so that what was computed from it before is not
+// held for a later use.
+template <class V>
+__device__ __forceinline__ void hide(V& v) {
+  if constexpr (sizeof(V) == 8 || sizeof(V) == 16 || sizeof(V) == 32) {
+    typedef uint32_t Words __attribute__((ext_vector_type(sizeof(V) / 4)));
+    Words w = __builtin_bit_cast(Words, v);
+    asm volatile("" : "+v"(w));
+    v = __builtin_bit_cast(V, w);
+  }
+}
+
 // f(true) or f(false), so that the usual case is compiled without its conditions
 template <class F>
 __device__ __forceinline__ void either(bool c, F f) {
