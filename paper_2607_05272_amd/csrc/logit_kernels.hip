@@ -50,7 +50,8 @@ __device__ __forceinline__ Part against(const Part& a, float m) {
 // through LDS takes over a hundred): sums along each row of 16 lanes, then from row to row.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ float dpp(float none, float v) {
-  return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(none), __float_as_uint(v), CTRL, ROWS, 0xf, false));
+  return __uint_as_float(
+      __builtin_amdgcn_update_dpp(__float_as_uint(none), __float_as_uint(v), CTRL, ROWS, 0xf, false));
 }
 template <class F>
 __device__ __forceinline__ float wave_reduce(float v, F f, bool keep) {
@@ -183,7 +184,8 @@ __device__ __forceinline__ uint32_t* live_parts(const BalanceArgs& s) {
 }
 int count_blocks(int64_t N, int k) {
   if (N * k <= kCountSelf) return 0;
-  return (int)std::min<int64_t>(kCountBlocks, (N * k + kCountThreads * kCountAhead - 1) / (kCountThreads * kCountAhead));
+  constexpr int each = kCountThreads * kCountAhead;
+  return (int)std::min<int64_t>(kCountBlocks, (N * k + each - 1) / each);
 }
 __device__ __forceinline__ double unit_of(const BalanceArgs& s, uint32_t W) {
   return W ? (double)s.c.coef * (s.c.A / s.c.group) / ((double)W * W * s.c.k) : 0.0;
@@ -234,7 +236,8 @@ __device__ __forceinline__ void count_choices(const BalanceArgs& s, uint32_t fir
 #pragma unroll
     for (int u = 0; u < kCountAhead; ++u) {
       if (!on[u] || a[u] == -1) continue;
-      if (a[u] >= 0 && a[u] < s.c.A) atomicAdd(&hist[s.c.group == 1 ? (uint32_t)a[u] : (uint32_t)a[u] / (uint32_t)s.c.group], 1u);
+      if (a[u] >= 0 && a[u] < s.c.A)
+        atomicAdd(&hist[s.c.group == 1 ? (uint32_t)a[u] : (uint32_t)a[u] / (uint32_t)s.c.group], 1u);
       else if (tell) atomicOr(s.err, ERR_ACTION);
     }
   }
@@ -687,7 +690,8 @@ struct Run {
   bool tail;
 
   __device__ __forceinline__ Run(const typename OP::Args& s_, const float* f_, int64_t n, int c0_, int c1_, bool tail_)
-      : s(s_), f(f_), l(static_cast<const T*>(s_.l.data) + n * s_.l.stride_n), c0(c0_), c1(c1_), whole(s_.c.A / N), tail(tail_) {
+      : s(s_), f(f_), l(static_cast<const T*>(s_.l.data) + n * s_.l.stride_n), c0(c0_), c1(c1_),
+        whole(s_.c.A / N), tail(tail_) {
     if constexpr (!OP::kBal) {
       if (s.mask.data) mk = static_cast<const uint8_t*>(s.mask.data) + n * s.mask.stride_n;
       ms = s.mask.stride_a;
@@ -863,6 +867,9 @@ __global__ __launch_bounds__(64 * W * GR) void loss_cols_k(typename OP::Args s, 
   typedef uint8_t Bytes __attribute__((ext_vector_type(2), aligned(1)));
   struct Closed { float m, alpha, beta, delta; int act; };   // act -2: the sample gives nothing
   constexpr bool kShare = W > 1;
+  // parts joined at once: two, or they and 24 logits spill (policy 40000 x 300 columns 40 -> 35 us); with 12
+  // all of them (balance 30000 x 162 22.3 us, two at a time 23.2)
+  constexpr int kJoin = R > 12 ? 2 : W;
   __shared__ double lds[W * GR][3];
   __shared__ Part parts[kShare ? W * GR : 1][128];
   __shared__ Closed closed[kShare ? GR : 1][128];
@@ -975,10 +982,10 @@ __global__ __launch_bounds__(64 * W * GR) void loss_cols_k(typename OP::Args s, 
       const int kg = threadIdx.x / 128, ks = threadIdx.x % 128;
       if (kg < GR && n0 + threadIdx.x < N) {
         float M = parts[kg * W][ks].m;
-#pragma unroll
+#pragma unroll kJoin
         for (int w = 1; w < W; ++w) M = max_nan(M, parts[kg * W + w][ks].m);
         Part whole{M, 0.0f, 0.0f};
-#pragma unroll
+#pragma unroll kJoin
         for (int w = 0; w < W; ++w) {
           const Part q = against<OP::kBal>(parts[kg * W + w][ks], M);
           whole.S += q.S;
