@@ -1033,55 +1033,103 @@ __global__ __launch_bounds__(64 * W * GR) void loss_cols_k(typename OP::Args s, 
   leave<OP>(s, sums, lds);
 }
 
-// More actions than the waves of a workgroup hold (or rows of any strides): a lane takes a sample and
-// reads it three times.
+// More actions than the waves of a workgroup hold: a lane takes a sample, kLaneWaves waves share its actions
+// and read them twice.
+constexpr int kLaneWaves = 16;
 template <class OP, class E>
-__global__ __launch_bounds__(64) void loss_lane_k(typename OP::Args s, int nb) {
+__global__ __launch_bounds__(64 * kLaneWaves) void loss_lane_k(typename OP::Args s, int nb) {
   typedef typename E::T T;
-  __shared__ double lds[1][3];
+  constexpr int U = 8;   // loads that fly together
+  struct Closed { float m, alpha, beta, delta; int64_t act; bool on; };
+  __shared__ double lds[kLaneWaves][3];
+  __shared__ Part parts[kLaneWaves][64];
+  __shared__ Closed closed[64];
   __shared__ float f[OP::kBal ? kMaxTargets : 1];
   fill_targets(s, nb, f);
+  const int A = s.c.A, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // the same in all of a wave's lanes
   Sums sums{0.0, 0.0, 0.0};
-  for (int64_t n = (int64_t)blockIdx.x * 64 + threadIdx.x; n < s.c.N; n += (int64_t)gridDim.x * 64) {
-    typename OP::Row row;
-    bool on = OP::open(s, n, row);
+  for (int64_t n0 = (int64_t)blockIdx.x * 64; n0 < s.c.N; n0 += (int64_t)gridDim.x * 64) {
+    const bool in = n0 + lane < s.c.N;
+    const int64_t n = in ? n0 + lane : s.c.N - 1;
     const T* l = static_cast<const T*>(s.l.data) + n * s.l.stride_n;
-    auto logit = [&](int a) {
-      if constexpr (!OP::kBal) {
-        if (s.mask.data &&
-            !static_cast<const uint8_t*>(s.mask.data)[n * s.mask.stride_n + a * s.mask.stride_a]) return -INFINITY;
+    // logits a0, a0 + kLaneWaves, ...: those past the last one and masked ones are -inf
+    auto read = [&](int a0, float (&v)[U]) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int a = a0 + u * kLaneWaves;
+        v[u] = a < A ? (float)l[a * s.l.stride_a] : -INFINITY;
       }
-      return (float)l[a * s.l.stride_a];
+      if constexpr (!OP::kBal) {
+        if (s.mask.data) {
+          const uint8_t* mk = static_cast<const uint8_t*>(s.mask.data) + n * s.mask.stride_n;
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const int a = a0 + u * kLaneWaves;
+            if (a < A && !mk[a * s.mask.stride_a]) v[u] = -INFINITY;
+          }
+        }
+      }
     };
     Part p{-INFINITY, 0.0f, 0.0f};
-    RowOut o{0.0f, 0.0f, 0.0f};
-    if (on) {
-#pragma unroll 8
-      for (int a = 0; a < s.c.A; ++a) p.m = max_nan(p.m, logit(a));
-      const float m = p.m == -INFINITY ? 0.0f : p.m;
-#pragma unroll 8
-      for (int a = 0; a < s.c.A; ++a) {
-        const float x = max_nan(logit(a) - m, kLowest), e = exp_of(x);
+    for (int a0 = wave; a0 < A; a0 += U * kLaneWaves) {
+      float v[U], M = p.m;
+      read(a0, v);
+#pragma unroll
+      for (int u = 0; u < U; ++u) M = max_nan(M, v[u]);
+      p = against<OP::kBal>(p, M);
+      const float m = M == -INFINITY ? 0.0f : M;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int a = a0 + u * kLaneWaves;
+        const float x = max_nan(v[u] - m, kLowest), e = exp_of(x);
         p.S += e;
-        p.X = fmaf(e, OP::kBal ? target(s, f, a) : x, p.X);
+        p.X = fmaf(e, OP::kBal ? (a < A ? target(s, f, a) : 0.0f) : x, p.X);
       }
-      on = OP::close(s, n, row, p, OP::template taken<T>(s, n, row), true, sums, o);
     }
-    if (!on) OP::shut(s, n);
-    if (s.grad.data) {
-      T* g = static_cast<T*>(s.grad.data) + n * s.grad.stride_n;
-#pragma unroll 8
-      for (int a = 0; a < s.c.A; ++a) {
-        float w = 0.0f;
-        if (on) {
-          const float x = max_nan(logit(a) - p.m, kLowest);
-          w = exp_of(x) * fmaf(o.beta, OP::kBal ? target(s, f, a) : x, o.alpha);
-          if (!OP::kBal && row.act == a) w += o.delta;
+    parts[wave][lane] = p;
+    __syncthreads();
+    if (wave == 0) {
+      Closed c{0.0f, 0.0f, 0.0f, 0.0f, -1, false};
+      typename OP::Row row;
+      if (in && OP::open(s, n, row)) {
+        float M = parts[0][lane].m;
+#pragma unroll 4
+        for (int w = 1; w < kLaneWaves; ++w) M = max_nan(M, parts[w][lane].m);
+        Part whole{M, 0.0f, 0.0f};
+#pragma unroll 4
+        for (int w = 0; w < kLaneWaves; ++w) {
+          const Part q = against<OP::kBal>(parts[w][lane], M);
+          whole.S += q.S;
+          whole.X += q.X;
         }
-        g[a * s.grad.stride_a] = (T)w;
+        RowOut o{0.0f, 0.0f, 0.0f};
+        c.on = OP::close(s, n, row, whole, OP::template taken<T>(s, n, row), true, sums, o);
+        c = Closed{M, o.alpha, o.beta, o.delta, (int64_t)row.act, c.on};
+      }
+      if (in && !c.on) OP::shut(s, n);
+      closed[lane] = c;
+    }
+    __syncthreads();
+    if (s.grad.data && in) {
+      const Closed c = closed[lane];
+      T* g = static_cast<T*>(s.grad.data) + n * s.grad.stride_n;
+      for (int a0 = wave; a0 < A; a0 += U * kLaneWaves) {
+        float v[U];
+        read(a0, v);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int a = a0 + u * kLaneWaves;
+          if (a >= A) continue;
+          const float x = max_nan(v[u] - c.m, kLowest);
+          float w = exp_of(x) * fmaf(c.beta, OP::kBal ? target(s, f, a) : x, c.alpha);
+          if (!OP::kBal && c.act == a) w += c.delta;
+          g[a * s.grad.stride_a] = (T)(c.on ? w : 0.0f);
+        }
       }
     }
   }
+  __syncthreads();
   leave<OP>(s, sums, lds);
 }
 
@@ -1112,7 +1160,7 @@ int launch_rows(const typename OP::Args& a, int nb, hipStream_t st) {
     const int lw = ceil_log2((A + 11) / 12), each = 128 * (lw < 2 ? 4 >> lw : 1);
     if (A > 16 * 24) {
       const int g = blocks_for(rows, 64, kMaxBlocks);
-      hipLaunchKernelGGL((loss_lane_k<OP, E>), dim3(g), dim3(64), 0, st, a, nb);
+      hipLaunchKernelGGL((loss_lane_k<OP, E>), dim3(g), dim3(64 * kLaneWaves), 0, st, a, nb);
       return g;
     }
     const int g = blocks_for(rows, each, kMaxBlocks);
