@@ -1148,6 +1148,10 @@ constexpr int kHeld = 16;             // chunks of a row that a thread holds
 constexpr int kSplitFrom = 4, kSplitChunks = 4096;   // workgroups that share a row, from which length
 constexpr int kFill = 256 * 1024;     // threads that fill the chip while they hold a row (128 registers each)
 
+// samples whose 193 to 384 actions are held
+template <class OP>
+constexpr int64_t kHold24 = OP::kBal ? 65536 : 32768;
+
 // Launches the form for these sizes and strides; the workgroups that left sums.
 template <class OP, class E>
 int launch_rows(const typename OP::Args& a, int nb, hipStream_t st) {
@@ -1156,9 +1160,12 @@ int launch_rows(const typename OP::Args& a, int nb, hipStream_t st) {
   const int64_t rows = a.c.N;
   const bool adjacent = (a.l.stride_a == 1 || A == 1) && (!a.grad.data || a.grad.stride_a == 1 || A == 1);
   if (!adjacent) {
-    // waves that share a sample, each with at most 12 of its actions (24 with the most waves)
+    // Waves that share a sample, each with at most 12 of its actions, or 24 with the most waves and samples:
+    // they leave little room beside them, which reading the samples twice does (us held and read twice, fp32:
+    // policy 2000 x 200 16.5, 11.6; 40000 x 380 42.3, 41.3, masked 68, 83; 100000 x 200 63, 73; with 12 8000 x
+    // 160 11.5, 12.5; balance 2000 x 200 23.6, 15.7; 40000 x 380 61, 49; 100000 x 200 50, 67).
     const int lw = ceil_log2((A + 11) / 12), each = 128 * (lw < 2 ? 4 >> lw : 1);
-    if (A > 16 * 24) {
+    if (A > 16 * 24 || (A > 16 * 12 && rows < kHold24<OP>)) {
       const int g = blocks_for(rows, 64, kMaxBlocks);
       hipLaunchKernelGGL((loss_lane_k<OP, E>), dim3(g), dim3(64 * kLaneWaves), 0, st, a, nb);
       return g;

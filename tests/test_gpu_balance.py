@@ -65,6 +65,13 @@ def test_many_rows(sim, N, A, k, group):
         check(sim, l, idx, live, group, cols=cols)
 
 
+@pytest.mark.parametrize("N,A,group", [(70001, 200, 1), (400, 200, 8), (400, 720, 6), (300000, 7, 1)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_columns_held_and_read_twice(sim, N, A, group, dtype):
+    l, idx, live = inputs(N, A, 2, TYPES[dtype], 5)
+    check(sim, l, idx, live, group, cols=True)
+
+
 def test_wide_groups(sim):
     l, idx, live = inputs(6, 9000, 3, torch.bfloat16, 4)
     check(sim, l, idx, live, group=3)

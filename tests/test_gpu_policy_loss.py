@@ -96,6 +96,12 @@ def test_many_rows(sim, N, A, cols):
     check(sim, inputs(N, A, torch.float32, 5, True), cols=cols)
 
 
+@pytest.mark.parametrize("N,A", [(33001, 255), (32767, 193), (40001, 384), (70001, 385)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_columns_held_and_read_twice(sim, N, A, dtype):
+    check(sim, inputs(N, A, TYPES[dtype], 6, True), cols=True)
+
+
 @pytest.mark.parametrize("A", [6, 300, 5000])
 @pytest.mark.parametrize("without", ["old", "ref", "weight", "entropy", "kl"])
 def test_absent_terms(sim, A, without):
