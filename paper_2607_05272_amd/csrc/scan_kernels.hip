@@ -374,7 +374,10 @@ __device__ __forceinline__ void state_before(const ScanArgs& s, const ScanPlan& 
   __syncthreads();
 }
 
-// A chunk's run: each thread takes a contiguous part of it, then one scan.
+// A chunk's run: each thread takes a contiguous part of it, then one scan. Its inputs are read again by the
+// launch after it, the price of splitting a sequence: 13 passes over an array in a training step instead of
+// 9, which fills a chip that 8 workgroups would leave empty (bf16 1 x 65536 x 512: 38 us, 3.5 TB/s; gradient
+// 29 us, 4.6 TB/s).
 template <class E, bool SIG, int V, int L, bool TV, bool GRAD>
 __global__ __launch_bounds__(kThreads) void scan_runs_k(ScanArgs s, ScanPlan p) {
   typedef typename E::W W;
@@ -434,6 +437,12 @@ __global__ __launch_bounds__(kThreads) void scan_runs_k(ScanArgs s, ScanPlan p) 
   }
 }
 
+// The recurrence: a segment's products and states stay in registers (64 of them) between the pass from 0 and
+// the one that adds the state before it; the next tile's loads fly under the scan. Bound by HBM with many
+// workgroups (fp32 16 x 1025 x 1536 62 us, 4.8 TB/s; fp64 1 x 4000 x 8192 157 us, 5.0; one channel, fp32
+// 4096 x 4096 38 us, 5.3), by the latency of a tile (loads, scan, barrier) with the one a CU that 2048 bf16
+// channels of 8 sequences make: 61 us, 3.3 TB/s. Splitting those over time instead reads twice (88 us for
+// as many elements); two tiles ahead, 512 threads or wider pieces of a row are slower (62, 58, 75).
 template <class E, bool SIG, int V, int L, bool TV>
 __global__ __launch_bounds__(kThreads) void scan_tile_k(ScanArgs s, ScanPlan p) {
   typedef typename E::W W;
@@ -528,6 +537,12 @@ __global__ __launch_bounds__(kThreads) void scan_tile_k(ScanArgs s, ScanPlan p) 
   }
 }
 
+// The gradient, against the order of the states: C, what later steps ask of a state, goes through the same
+// scan (C = a (dy + C)), and a second pass over the raw elements, kept in registers, makes dg and dx. It
+// computes the gates twice: keeping them takes 30 registers and a third of the waves (bf16 16 x 1024 x 4096
+// step 317 us, 305 so). Bound by HBM: fp32 16 x 1025 x 1536 83 us for five arrays, 6.1 TB/s with what the
+// cache still holds; bf16 1 x 65536 x 512 110 us for six, 3.7 TB/s in chunks. The next tile's loads under the
+// scan help unaligned rows by 5% and cost aligned ones as much (187 against 181 us): not done.
 template <class E, bool SIG, int V, int L, bool TV>
 __global__ __launch_bounds__(kThreads) void scan_grad_k(ScanArgs s, ScanPlan p) {
   typedef typename E::W W;
@@ -619,7 +634,8 @@ __global__ __launch_bounds__(kThreads) void scan_grad_k(ScanArgs s, ScanPlan p) 
   }
 }
 
-// A few steps (serving: one): a thread has V channels and takes them in turn.
+// A few steps (serving: one): a thread has V channels and takes them in turn; bound by the launch (bf16
+// 64 x 1 x 2048 2.3 us), and from about 1000 workgroups on by HBM (512 x 1 x 8192 11.7 us, 5.0 TB/s).
 template <class E, bool SIG, int V>
 __global__ __launch_bounds__(kThreads) void scan_step_k(ScanArgs s) {
   typedef typename E::T T;
