@@ -381,7 +381,7 @@ class Sim:
         one = gate.dim() == 2
         if one:
             gate, x, y = gate[None], x[None], None if y is None else y[None]
-            h0, state = (None if s is None else s.reshape(1, -1) for s in (h0, state))
+            h0, state = (None if s is None else s.view(1, -1) for s in (h0, state))
         B, T, D = gate.shape
         wide = torch.float64 if gate.dtype == torch.float64 else torch.float32
         self._check("gate", gate, (B, T, D), _FLOAT)
@@ -410,7 +410,7 @@ class Sim:
         if one:
             gate, x, y, dy, dgate, dx = (None if t is None else t[None]
                                          for t in (gate, x, y, dy, dgate, dx))
-            h0, dstate, dh0 = (None if s is None else s.reshape(1, -1) for s in (h0, dstate, dh0))
+            h0, dstate, dh0 = (None if s is None else s.view(1, -1) for s in (h0, dstate, dh0))
         B, T, D = gate.shape
         wide = torch.float64 if gate.dtype == torch.float64 else torch.float32
         self._check("gate", gate, (B, T, D), _FLOAT)

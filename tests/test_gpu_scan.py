@@ -230,6 +230,20 @@ def test_refusals(sim):
     sim.sync()
 
 
+def test_state_of_one_sequence_is_never_a_copy(sim):
+    """A state that the caller hands over is written itself, or refused."""
+    g, x = torch.rand(2, 9, 6, device="cuda").unbind()
+    state = torch.zeros(6, device="cuda")
+    _, s = sim.gated_scan(g, x, state, state=state)
+    sim.sync()
+    assert s.data_ptr() == state.data_ptr() and state.abs().max() > 0
+    for apart in (torch.zeros(12, device="cuda")[::2], torch.zeros(3, 2, device="cuda").t()):
+        with pytest.raises((ValueError, RuntimeError)):
+            sim.gated_scan(g, x, state=apart)
+        with pytest.raises((ValueError, RuntimeError)):
+            sim.gated_scan_grad(g, x, x, x, dh0=apart)
+
+
 def test_far_offsets(sim):
     """Two sequences more than 2^31 elements apart, in every array."""
     B, T, D, far = 2, 70, 40, (1 << 31) + 24
