@@ -865,11 +865,23 @@ __global__ __launch_bounds__(kSplit) void policy_slopes_k(PolicyLossArgs s) {
   leave<PolicyOp>(s, sums, lds);
 }
 
+// The place of a workgroup among all: in turn, or each XCD with a run of neighbours, where a wave's piece of a
+// row is 512 bytes (us in turn and so, masked: fp32 131072 x 96 34.7, 33.0; 131072 x 72 30.7, 28.8; 66904 x 72
+// 24.5, 23.7; pieces of 256, bf16 131072 x 72 28.8, 29.1; one workgroup a CU, fp32 40000 x 160 21.8, 24.5).
+template <bool RUNS>
+__device__ __forceinline__ int64_t first_of() {
+  if constexpr (RUNS) {
+    const uint32_t each = gridDim.x >> 3, rest = gridDim.x & 7, xcd = blockIdx.x & 7;
+    return xcd * each + (xcd < rest ? xcd : rest) + (blockIdx.x >> 3);
+  }
+  return blockIdx.x;
+}
+
 // ---- logits of adjacent samples: [A][N] --------------------------------------------------------
 // A lane takes two adjacent samples; W waves share them, each with up to R of their actions, and one
 // thread a sample joins the waves' parts and closes it. GR such groups make a workgroup. Bound by HBM and the
-// two barriers (policy fp32 131072 x 96 masked 31 us, 3.7 TB/s; without 27; balance 65536 x 48 11.4 us): more
-// waves with 6 actions each hold fewer loads (43 us for 35), fewer registers for more waves spill (40).
+// two barriers (policy fp32 131072 x 96 masked 30 us, 3.9 TB/s; balance 65536 x 48 11.4 us): more waves with 6
+// actions each hold fewer loads (43 us for 35, with the sum's launch), fewer registers for more waves spill (40).
 template <class OP, class E, int W, int GR, int R>
 __global__ __launch_bounds__(64 * W * GR) void loss_cols_k(typename OP::Args s, int nb) {
   typedef typename E::T T;
@@ -893,7 +905,7 @@ __global__ __launch_bounds__(64 * W * GR) void loss_cols_k(typename OP::Args s, 
   T* g0 = static_cast<T*>(s.grad.data);
   const int64_t N = s.c.N, ls = s.l.stride_n, gs = s.grad.stride_n;
   Sums sums{0.0, 0.0, 0.0};
-  for (int64_t n0 = (int64_t)blockIdx.x * 128 * GR; n0 < N; n0 += (int64_t)gridDim.x * 128 * GR) {
+  for (int64_t n0 = first_of<sizeof(T) == 4 && W <= 8>() * 128 * GR; n0 < N; n0 += (int64_t)gridDim.x * 128 * GR) {
     // every lane has both samples, side by side: pairs at a lane's offset from the row's address
     const bool fits = n0 + 128 * GR <= N && ls == 1 && (!g0 || gs == 1);
     either(fits, [&](auto ALL) {
