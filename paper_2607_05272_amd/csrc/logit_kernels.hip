@@ -187,8 +187,13 @@ int count_blocks(int64_t N, int k) {
   constexpr int each = kCountThreads * kCountAhead;
   return (int)std::min<int64_t>(kCountBlocks, (N * k + each - 1) / each);
 }
-__device__ __forceinline__ double unit_of(const BalanceArgs& s, uint32_t W) {
-  return W ? (double)s.c.coef * (s.c.A / s.c.group) / ((double)W * W * s.c.k) : 0.0;
+// A target's factor f_g coef G / W, less that of an even share, coef / W: only differences of the factors
+// matter to the gradient, and near balance (or with one target) those of the factors themselves would be
+// rounding. The loss gets the even share back at its end.
+__device__ __forceinline__ float target_of(const BalanceArgs& s, uint32_t W, uint32_t count) {
+  if (W == 0) return 0.0f;
+  const double G = s.c.A / s.c.group, all = (double)W * s.c.k;
+  return (float)((double)s.c.coef / W * ((double)count * G - all) / all);
 }
 
 struct BalanceOp {
@@ -203,16 +208,22 @@ struct BalanceOp {
   __device__ static __forceinline__ float taken(const Args&, int64_t, const Row&) { return 0.0f; }
   __device__ static __forceinline__ bool close(const Args&, int64_t, const Row&, const Part& p, float, bool first,
                                                Sums& sums, RowOut& o) {
+    if (first) sums.c += 1.0;   // live rows, and those that have a probability
     if (p.m == -INFINITY) return false;
     const float rS = __builtin_amdgcn_rcpf(p.S), si = p.X * rS;
     o.beta = rS;
     o.alpha = -si * rS;
     o.delta = 0.0f;
-    if (first) sums.a += (double)si;
+    if (first) {
+      sums.a += (double)si;
+      sums.b += 1.0;
+    }
     return true;
   }
   __device__ static __forceinline__ void shut(const Args&, int64_t) {}
-  __device__ static __forceinline__ void finish(const Args& s, const Sums& v) { s.loss[0] = (float)v.a; }
+  __device__ static __forceinline__ void finish(const Args& s, const Sums& v) {
+    s.loss[0] = v.c > 0.0 ? (float)(v.a + (double)s.c.coef * v.b / v.c) : 0.0f;
+  }
 };
 
 // Adds choices first, first + step, ... of the live rows to hist (cleared by the caller) and the live rows
@@ -281,7 +292,7 @@ __global__ __launch_bounds__(256) void balance_targets_k(BalanceArgs s, int nb) 
     c = 0;
     for (int i = 0; i < 8; ++i) c += part[i][threadIdx.x];
     s.counts[g] = c;
-    targets(s)[g] = (float)(unit_of(s, live[0] + live[1] + live[2] + live[3]) * c);
+    targets(s)[g] = target_of(s, live[0] + live[1] + live[2] + live[3], c);
   }
 }
 static_assert(kCountBlocks <= 256, "a thread per counting workgroup");
@@ -309,11 +320,10 @@ __device__ __forceinline__ void fill_targets(const BalanceArgs& s, int nb, float
       count_choices(s, threadIdx.x, blockDim.x, hist, &live, blockIdx.x == 0);
     }
     __syncthreads();
-    const double unit = unit_of(s, live);
     for (int g = threadIdx.x; g < G; g += blockDim.x) {
       const uint32_t c = hist[g];
       if (blockIdx.x == 0) s.counts[g] = c;
-      f[g] = (float)(unit * c);
+      f[g] = target_of(s, live, c);
     }
   }
   __syncthreads();
@@ -330,10 +340,8 @@ template <class OP>
 __device__ __forceinline__ void leave(const typename OP::Args& s, Sums v, double (*lds)[3]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
   v.a = wave_sum(v.a);
-  if (!OP::kBal) {
-    v.b = wave_sum(v.b);
-    v.c = wave_sum(v.c);
-  }
+  v.b = wave_sum(v.b);
+  v.c = wave_sum(v.c);
   if (lane == 63) { lds[wave][0] = v.a; lds[wave][1] = v.b; lds[wave][2] = v.c; }
   __syncthreads();
   if (wave == 0) {

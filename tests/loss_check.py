@@ -73,8 +73,15 @@ def check_balance(got, want, z, live, group, coef, dtype):
         logS = -np.log(P[n].max())
         eS, eP = softmax_errors(A, x, P[n], logS)
         si = (f * P[n]).sum()
-        dsi = (P[n] * f * eP).sum() + si * (eS + (20 + A / 64 + min(A, 96)) * U)
-        tg[n] = abs(coef) * G / W * P[n] * (np.abs(f - si) * (eP + 8 * U) + 2 * U * f + 2 * U * si + dsi)
+        # the kernel works on f' = f - 1/G, rounded once, and si' = sum p f': |f'| takes f's place in every
+        # rounding, and si - 1/G that of si
+        fc = np.abs(f - 1.0 / G)
+        sc = (fc * P[n]).sum()
+        dsi = (P[n] * fc * eP).sum() + sc * (eS + (20 + A / 64 + min(A, 96)) * U)
+        # the oracle's own fp64: f - si from a sum of A products, each step off by at most 2^-53 of f or si;
+        # where f is even their difference is nothing but that
+        o64 = (A + 8) * 2.0 ** -53 * (f + si)
+        tg[n] = abs(coef) * G / W * P[n] * (np.abs(f - si) * (eP + 8 * U) + 2 * U * fc + 2 * U * sc + dsi + o64)
         tl += abs(coef) * G / W * dsi
     near(got["grad"].double().cpu().numpy(), want["grad"], tg + rounding(want["grad"], dtype), "grad")
     assert np.array_equal(got["counts"].cpu().numpy(), want["counts"]), "counts"
