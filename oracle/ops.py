@@ -114,14 +114,14 @@ def policy_loss(logits, actions, adv, logp_old=None, logp_ref=None, weight=None,
         if logp_ref is not None:
             d = float(logp_ref[n]) - lp
             kl = np.expm1(d) - d
-            q -= c_kl * np.expm1(d)
+            q -= c_kl * np.expm1(d) if c_kl else 0.0
         g = -q * p
         g[a] += q
         g += c_entropy * p * (lsf + H)
         grad[n], logp[n] = w[n] * g, lp
         loss += w[n] * np.array([term, kl, H])
         parts[n] = dict(p=p, ls=lsf, H=H, q=q, rho=rho, x=np.where(ok, z[n] - m, 0.0), term=term)
-    total = loss[0] + c_kl * loss[1] - c_entropy * loss[2]
+    total = loss[0] + (c_kl * loss[1] if c_kl else 0.0) - (c_entropy * loss[2] if c_entropy else 0.0)
     return dict(loss=np.concatenate([[total], loss]), logp=logp, grad=grad, parts=parts, bad=bad)
 
 

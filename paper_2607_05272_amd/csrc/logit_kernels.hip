@@ -143,8 +143,8 @@ struct PolicyOp {
     const float pol = s1 <= s2 || nan ? -s1 : -s2;
     float q = s1 <= s2 || nan || (rho > lo && rho < hi) ? -s1 : 0.0f, kl = 0.0f;
     if (s.logp_ref) {
-      const float d = r.ref - logp;
-      q -= s.c.c_kl * grow(d, kl);
+      const float slope = grow(r.ref - logp, kl);
+      if (s.c.c_kl > 0.0f) q -= s.c.c_kl * slope;   // 0 times an infinite slope is not 0
     }
     const float wr = r.w * rS, ch = s.c.c_entropy;
     o.alpha = ch > 0.0f ? wr * fmaf(ch, H - logS, -q) : -wr * q;
@@ -162,7 +162,9 @@ struct PolicyOp {
     if (s.logp) s.logp[n] = 0.0f;
   }
   __device__ static __forceinline__ void finish(const Args& s, const Sums& v) {
-    s.loss[0] = (float)(v.a + (double)s.c.c_kl * v.b - (double)s.c.c_entropy * v.c);
+    // a term without a coefficient is told apart, but is no part of the loss, infinite or not
+    s.loss[0] = (float)(v.a + (s.c.c_kl > 0.0f ? (double)s.c.c_kl * v.b : 0.0) -
+                        (s.c.c_entropy > 0.0f ? (double)s.c.c_entropy * v.c : 0.0));
     s.loss[1] = (float)v.a;
     s.loss[2] = (float)v.b;
     s.loss[3] = (float)v.c;

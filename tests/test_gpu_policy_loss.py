@@ -327,3 +327,20 @@ def test_graphs(sim):
             torch.cuda.synchronize()
             for w, o in zip(want, got):
                 assert all(torch.equal(w[k], o[k]) for k in w)
+
+
+@pytest.mark.parametrize("N,A,cols", [(20, 6, False), (20, 6, True), (15, 48, True), (9, 300, False), (70, 600, True),
+                                      (6, 5000, False), (3, 9000, False), (2, 140001, False), (2, 300001, False)])
+@pytest.mark.parametrize("ref", [-float("inf"), 120.0, 1000.0, float("nan")])
+def test_a_reference_without_its_coefficient_tells_the_kl_term_alone(sim, N, A, cols, ref):
+    """c_kl = 0 with a reference that forbids the action, lies far above its probability or is NaN: the
+    KL term is infinite, huge or NaN, all else that of a call without a reference."""
+    s = inputs(N, A, torch.float32, 10, True, padded=False)
+    want = run(sim, dict(s, ref=None), c_kl=0.0, cols=cols)
+    s["ref"][0] = ref
+    got = run(sim, s, c_kl=0.0, cols=cols)
+    assert torch.isfinite(want["loss"]).all() and torch.isfinite(want["grad"]).all()
+    assert all(torch.equal(got[k], want[k]) for k in ("logp", "grad"))
+    assert torch.equal(got["loss"][[0, 1, 3]], want["loss"][[0, 1, 3]])
+    kl = got["loss"][2].item()
+    assert kl > 1e40 or kl == float("inf") or kl != kl

@@ -103,3 +103,17 @@ def test_balance_gradient(group, k):
     # every target equally often and equally likely: the loss's value is coef
     even = np.tile(np.arange(A), (A, 1)).T[:, :1]
     np.testing.assert_allclose(ops.balance_loss(np.zeros((A, A)), even, coef=0.7)["loss"], 0.7)
+
+
+def test_a_reference_without_its_coefficient_tells_the_kl_term_alone():
+    """c_kl = 0 with a reference that forbids an action (-inf) or is far above it: the KL term is infinite or
+    huge, loss, policy term and gradient are those of a call without a reference."""
+    r = np.random.default_rng(5)
+    z, adv, act = r.normal(size=(4, 5)), r.normal(size=4), np.array([0, 1, 2, 3])
+    for ref in (np.array([-np.inf, -1.0, 0.0, -2.0]), np.array([1000.0, -1.0, 0.0, -2.0])):
+        with np.errstate(over="ignore"):
+            got = ops.policy_loss(z, act, adv, logp_ref=ref, c_entropy=0.1)
+        want = ops.policy_loss(z, act, adv, c_entropy=0.1)
+        assert got["loss"][2] == np.inf
+        np.testing.assert_array_equal(got["loss"][[0, 1, 3]], want["loss"][[0, 1, 3]])
+        np.testing.assert_array_equal(got["grad"], want["grad"])
