@@ -1113,13 +1113,26 @@ __global__ __launch_bounds__(64 * kLaneWaves) void loss_lane_k(typename OP::Args
       for (int u = 0; u < U; ++u) M = max_nan(M, v[u]);
       p = against<OP::kBal>(p, M);
       const float m = M == -INFINITY ? 0.0f : M;
+      // a round's terms are added up among themselves: a lane's sums take A / 128 additions one after
+      // another, as few as the other forms'
+      float e[U], ex[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int a = a0 + u * kLaneWaves;
-        const float x = max_nan(v[u] - m, kLowest), e = exp_of(x);
-        p.S += e;
-        p.X = fmaf(e, OP::kBal ? (a < A ? target(s, f, a) : 0.0f) : x, p.X);
+        const float x = max_nan(v[u] - m, kLowest);
+        e[u] = exp_of(x);
+        ex[u] = e[u] * (OP::kBal ? (a < A ? target(s, f, a) : 0.0f) : x);
       }
+#pragma unroll
+      for (int h = U / 2; h; h /= 2) {
+#pragma unroll
+        for (int u = 0; u < h; ++u) {
+          e[u] += e[u + h];
+          ex[u] += ex[u + h];
+        }
+      }
+      p.S += e[0];
+      p.X += ex[0];
     }
     parts[wave][lane] = p;
     __syncthreads();

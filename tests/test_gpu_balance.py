@@ -192,3 +192,12 @@ def test_graphs(sim):
             torch.cuda.synchronize()
             for w, o in zip(want, got):
                 assert all(torch.equal(w[k], o[k]) for k in w)
+
+
+@pytest.mark.parametrize("A,cols", [(10000, True), (48000, True), (48000, False)])
+def test_many_small_probabilities(sim, A, cols):
+    """Sixteen logits of 0, then thousands whose exponential is 0.9 half steps of fp32 at 1: a sum that takes
+    them one after another loses them all (48000 columns: 1.6e-4 of the sum)."""
+    l = torch.full((3, A), 24 * -np.log(2.0) + np.log(0.9))
+    l[:, :16] = 0.0
+    check(sim, l, torch.tensor([[0], [17], [3]]), None, group=16, cols=cols)

@@ -344,3 +344,14 @@ def test_a_reference_without_its_coefficient_tells_the_kl_term_alone(sim, N, A, 
     assert torch.equal(got["loss"][[0, 1, 3]], want["loss"][[0, 1, 3]])
     kl = got["loss"][2].item()
     assert kl > 1e40 or kl == float("inf") or kl != kl
+
+
+@pytest.mark.parametrize("A,cols", [(10007, True), (50000, True), (10007, False), (50000, False), (300000, False)])
+def test_many_small_probabilities(sim, A, cols):
+    """Sixteen logits of 0, then thousands whose exponential is 0.9 half steps of fp32 at 1: a sum that takes
+    them one after another loses them all (50000 columns: 1.7e-4 of the sum, the bound is 5e-5)."""
+    l = torch.full((3, A), 24 * -np.log(2.0) + np.log(0.9))
+    l[:, :16] = 0.0
+    s = dict(logits=l, actions=torch.tensor([0, 5, A - 1]), mask=None, weight=None, old=None, ref=None,
+             adv=torch.tensor([1.0, -2.0, 0.5]))
+    check(sim, s, 0.0, 0.2, cols=cols)
