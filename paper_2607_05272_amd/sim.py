@@ -360,12 +360,11 @@ class Sim:
                 work = torch.empty(need, dtype=torch.uint8, device=self._device)
             elif work is None or work.numel() < need:
                 work = self._work.memory = torch.empty(need, dtype=torch.uint8, device=self._device)
-            work = work.data_ptr()
         if not same:
             now = torch.cuda.current_stream(self._device)
             self.stream.wait_stream(now)
-        rc = getattr(self.lib, name)(self._ctx, sizes_p, *args, work, need)
-        if not same:
+        rc = getattr(self.lib, name)(self._ctx, sizes_p, *args, _a(work), need)
+        if not same:   # `work` is held until here: what it is given to next comes after the call
             now.wait_stream(self.stream)
         if rc:
             L.check(rc, name)
