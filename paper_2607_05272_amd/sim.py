@@ -349,14 +349,16 @@ class Sim:
         stream, and that stream after it, where the context has another one. The memory is kept
         from call to call, per thread, where calls follow one another on the context's stream;
         a captured call, whose replays do not, gets its own, and so does one from another
-        stream, whose allocations torch orders by that stream."""
+        stream, whose allocations torch orders by that stream, or made while another device is the
+        current one, whose capture alone torch tells of."""
         sizes_p, need = C.byref(sizes), C.c_size_t()
         L.check(getattr(self.lib, name + "_work")(sizes_p, C.byref(need)), name)
         work, need = None, need.value
         same = torch._C._cuda_getCurrentRawStream(self._index) == self._raw_stream
         if need:
             work = getattr(self._work, "memory", None)
-            if not same or torch.cuda.is_current_stream_capturing():
+            if (not same or torch.cuda.current_device() != self._index
+                    or torch.cuda.is_current_stream_capturing()):
                 work = torch.empty(need, dtype=torch.uint8, device=self._device)
             elif work is None or work.numel() < need:
                 work = self._work.memory = torch.empty(need, dtype=torch.uint8, device=self._device)

@@ -94,3 +94,14 @@ def test_captured_calls_have_memory_of_their_own(world):
     assert c.at != kept and any(c.held)
     world.capturing = set()
     assert world.call().at == kept
+
+
+def test_another_current_device_takes_memory_of_its_own(world):
+    """Whether the context's stream is being captured can be asked only of the current device's: a call made
+    while that is another one does not use the memory that eager calls share."""
+    kept = world.call().at
+    world.capturing, world.device = {0}, 1
+    c = world.call()
+    assert c.at != kept and any(c.held)
+    world.capturing, world.device = set(), 0
+    assert world.call().at == kept
