@@ -451,9 +451,14 @@ typedef struct sim_scan {
  * state updated in place). y may be NULL (only the state is wanted). d_len [B] int32 (NULL: all
  * T): steps t >= d_len[b] are padding, whatever they hold: they leave the state as it is and
  * their y is 0; a length outside [0, T] latches SIM_ESTATE and is taken as the nearer bound.
- * Long sequences of few channels are split over time, so results differ from a step-by-step
- * sum by rounding; the products of the gates over any run of steps must then be finite in the
- * state's type (always so for |gate| <= 1).                                              */
+ * Up to T = 4 steps are taken one after another. With more, and in the gradient whatever T, a
+ * sequence is cut into runs of steps whose gates are multiplied up and joined, runs of any length up
+ * to the whole sequence: results differ from a step-by-step sum by rounding, and the product of the
+ * gates over any run of steps must be finite in the state's type (an infinite one makes NaN of a state
+ * of 0, also where every state is finite). What reaches a state through a run whose product is below
+ * the type's smallest number (fp32 2^-149) is lost, also where later gates above 1 would make it large
+ * again. With |gate| <= 1, as the factors of sigmoid gates are, products are finite and what is lost
+ * is below 2^-149 of the state that it comes from.                                        */
 int gated_scan_work(const sim_scan* s, size_t* bytes);
 int gated_scan(sim_ctx* ctx, const sim_scan* s, const sim_seq* gate, const sim_seq* x,
                const int32_t* d_len, const void* d_h0, const sim_seq* y, void* d_state,
@@ -464,9 +469,10 @@ int gated_scan(sim_ctx* ctx, const sim_scan* s, const sim_seq* gate, const sim_s
  * C = dstate at first and h' the state before a step (y of the step before it as stored, or h0):
  *   G_t = dy_t + C;  linear:  dx_t = G_t,          dgate_t = G_t h',                 C = gate_t G_t
  *                    sigmoid: dx_t = (1 - f) G_t,  dgate_t = G_t (h' - x_t) f (1 - f),  C = f G_t
- * and dh0 = C at the end. Padding gets 0. x is read for SIM_GATE_SIGMOID only, y only if dgate
- * is wanted (either may be NULL otherwise). The gradient of a broadcast input is the sum over
- * the dimension it is broadcast along of what is written here, which is left to the caller. */
+ * and dh0 = C at the end. Padding gets 0. The gates' products must be finite as above, with any T.
+ * x is read for SIM_GATE_SIGMOID only, y only if dgate is wanted (either may be NULL otherwise).
+ * The gradient of a broadcast input is the sum over the dimension it is broadcast along of what is
+ * written here, which is left to the caller.                                              */
 int gated_scan_grad_work(const sim_scan* s, size_t* bytes);
 int gated_scan_grad(sim_ctx* ctx, const sim_scan* s, const sim_seq* gate, const sim_seq* x,
                     const sim_seq* y, const sim_seq* dy, const int32_t* d_len, const void* d_h0,

@@ -7,7 +7,9 @@
 // segments, a thread each: it scans its segment from 0 in registers, the segments' (A, X) are
 // scanned across the workgroup, and each thread then adds A_l times the state that its segment starts
 // from. Each element is read once and written once; a multiplication and an addition per element
-// (and a sigmoid): bound by HBM.
+// (and a sigmoid): bound by HBM. The price is that the products A must stay in the type's range, which with
+// |gate| <= 1 they do, or fall to 0 where what they carry no longer counts (an infinite one times a state
+// of 0 is NaN).
 //
 // Positions p = 0..T-1 are taken in processing order, t = p, or from the end. Padding is the
 // identity (A, X) = (1, 0), so the state passes through it on either side of a sequence.

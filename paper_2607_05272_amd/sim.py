@@ -378,7 +378,9 @@ class Sim:
         h0 [B][D] (fp64 for fp64 inputs, otherwise fp32; default 0), backwards in t with
         `reverse`. lengths [B] int32: later steps are padding. Returns (y, state): the state
         after each step, in the inputs' type (None unless want_y), and the last state, which
-        may be written over h0 (state=h0)."""
+        may be written over h0 (state=h0). With more than 4 steps the gates of runs of steps are
+        multiplied up: linear gates beyond 1 need products over any run that stay finite in the
+        state's type (gated_scan in batchsim.h)."""
         one = gate.dim() == 2
         if one:
             gate, x, y = gate[None], x[None], None if y is None else y[None]
@@ -406,7 +408,8 @@ class Sim:
         """Gradient of gated_scan: gate, x, y (its output), dy [B][T][D] or [T][D], dstate [B][D]
         the gradient of its last state. Returns (dgate, dx, dh0) of the inputs' full shapes (sum
         over the dimensions that an input was broadcast along); with want_gate=False dgate is
-        None and y (and x) may be."""
+        None and y (and x) may be. Products of gates must be finite as for gated_scan, with any
+        number of steps."""
         one = gate.dim() == 2
         if one:
             gate, x, y, dy, dgate, dx = (None if t is None else t[None]

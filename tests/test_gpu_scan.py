@@ -320,3 +320,31 @@ def test_two_contexts_at_once(sim):
                 outs.append(other.gated_scan(d["gate"], d["x"], d["h0"])[0])
         torch.cuda.synchronize()
         assert all(torch.equal(o, want) for o in outs)
+
+
+@pytest.mark.parametrize("dtype", ["f64", "f32", "bf16"])
+@pytest.mark.parametrize("B,T,D", [(3, 90, 40), (2, 700, 24), (1, 6000, 8), (4, 900, 1), (2, 257, 3)])
+def test_gates_beyond_one(sim, B, T, D, dtype):
+    """Gates of either sign from 1/g to g whose product over any run stays finite, g^T = 2^60."""
+    g = 2.0 ** (60 / T)
+    for reverse in (False, True):
+        d = sc.inputs(B, T, D, sc.TYPES[dtype], "linear", T + D, lengths=True, device="cuda")
+        r = torch.rand(B, T, D, generator=torch.Generator().manual_seed(T), dtype=torch.float64).cuda() * 2 - 1
+        grow = torch.rand(B, 1, D, generator=torch.Generator().manual_seed(D)).cuda() < 0.3   # all the time
+        d["gate"] = (g ** torch.where(grow, r.abs(), r) * r.sign()).to(sc.TYPES[dtype])
+        if dtype == "bf16":     # rounded gates are 1 for long sequences, and at most 2^120 together
+            assert d["gate"].double().abs().log2().clamp(min=0).sum(1).max() < 120
+        both(sim, d, "linear", reverse)
+
+
+@pytest.mark.parametrize("dtype", ["f64", "f32"])
+def test_few_steps_are_taken_one_after_another(sim, dtype):
+    """Up to four steps the products of the gates may pass the type's range."""
+    dt = sc.TYPES[dtype]
+    big = 1e200 if dtype == "f64" else 1e30
+    gate = torch.full((2, 4, 5), big, dtype=dt, device="cuda")
+    x = torch.zeros(2, 4, 5, dtype=dt, device="cuda")
+    x[1, 2] = 3.0
+    y, h = sim.gated_scan(gate, x)
+    sim.sync()
+    assert (h[0] == 0).all() and torch.equal(h[1], 3.0 * gate[0, 0]) and torch.equal(y[:, 3], h)
