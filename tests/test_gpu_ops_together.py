@@ -219,3 +219,66 @@ def test_many_sequences(bs, B, T, D):
         assert ((dg[:, t].double() - torch.where(on, G * prev[t], 0.0)).abs() <= (u + sc.unit(torch.float32) * 2 * M) * prev[t].abs()).all()
         C, m = torch.where(on, gate[:, t].double() * G, C), torch.where(on, gate[:, t].double().abs() * M, m)
     assert ((dh0.double() - C).abs() <= sc.unit(torch.float32) * (3 * T + 66) * m + 1e-45).all()
+
+
+def policy_rows(l, act, adv, w, mask, c):
+    """Rows [n][A] at rho = 1 and without a KL term, in fp64: grad, logp and loss_check's bounds of both."""
+    A, U = l.shape[1], lc.U
+    z = l.double() if mask is None else l.double().masked_fill(~mask, -torch.inf)
+    x = z - z.amax(1, keepdim=True)
+    logS = x.exp().sum(1, keepdim=True).log()
+    ls = x - logS
+    p = ls.exp()
+    x, ls = (v.masked_fill(p == 0, 0.0) for v in (x, ls))
+    H = -(p * ls).sum(1, keepdim=True)
+    hot = torch.zeros_like(p).scatter_(1, act[:, None], 1.0)
+    w, q = w.double()[:, None], -adv.double()[:, None]
+    grad = w * (q * (hot - p) + c * p * (ls + H))
+    logp = ls.gather(1, act[:, None]) * (w != 0)
+    adds = A / 64 + min(A, 96) + 16
+    eS = U * (p * (3 * x.abs() + 4)).sum(1, keepdim=True) + U * adds
+    eP = eS + U * (4 * x.abs() + 4 * logS.abs() + 8)
+    eL = eS + U * (x.abs() + ls.abs() + 3 * logS.abs() + 1)
+    mx, mxx = (p * x.abs()).sum(1, keepdim=True), (p * x * x).sum(1, keepdim=True)
+    eH = eS * (1 + 2 * mx) + U * (3 * mxx + adds * mx + 4 * logS.abs() + 4)
+    dq = q.abs() * 6 * U   # rho = 1 as it stands, clipped bounds and products: 4, and 2 as there
+    tol = w * (dq * (hot + p) + q.abs() * p * eP + q.abs() * 3 * U * (hot + p)
+               + c * p * ((ls.abs() + H) * (eP + 6 * U) + eL + eH))
+    tol = tol + torch.finfo(l.dtype).eps / 2 * grad.abs() + torch.finfo(l.dtype).smallest_normal * torch.finfo(l.dtype).eps
+    return grad, logp[:, 0], tol, (eL.gather(1, act[:, None])[:, 0] + U * logp[:, 0].abs())
+
+
+@pytest.mark.parametrize("N,A,dtype,cols,masked", [
+    (300000, 6, "f32", False, False), (20000, 1000, "bf16", False, False), (20000, 1000, "f32", False, True),
+    (5000, 2100, "bf16", False, True), (1300, 20000, "bf16", False, False), (1200, 20000, "bf16", False, True),
+    (700, 50257, "bf16", False, False), (300, 131072, "bf16", False, False), (600, 70001, "f32", False, False),
+    (20, 90001, "bf16", False, True), (2200000, 6, "f32", True, True), (1060000, 13, "f32", True, False), (530000, 40, "f32", True, True),
+    (530000, 90, "f32", True, False), (600001, 40, "f16", True, False), (530000, 90, "bf16", True, True),
+    (530000, 190, "f32", True, False), (270000, 400, "bf16", True, True)])
+def test_every_row(bs, N, A, dtype, cols, masked):
+    """More rows than workgroups take at once: every row's gradient and log-probability against the closed
+    form in fp64. A tenth of the rows is padding."""
+    dt = sc.TYPES[dtype]
+    g = torch.Generator(device="cuda").manual_seed(N + A)
+    l = (torch.randn((A, N) if cols else (N, A), generator=g, device="cuda", dtype=dt) * 2)
+    l = l.t() if cols else l
+    act = torch.randint(0, A, (N,), generator=g, device="cuda")
+    mask = None
+    if masked:
+        mask = torch.rand((A, N) if cols else (N, A), generator=g, device="cuda") > 0.3
+        mask = mask.t() if cols else mask
+        mask.scatter_(1, act[:, None], True)
+    w = (torch.rand(N, generator=g, device="cuda") > 0.1).float() * torch.rand(N, generator=g, device="cuda") / N
+    w = w * (65536.0 if dtype == "f16" else 1.0)
+    adv = torch.randn(N, generator=g, device="cuda")
+    with bs.Sim(preset("C1"), n_envs=1) as sim:
+        r = sim.policy_loss(l, act, adv, weight=w, mask=mask, c_entropy=0.1)
+        sim.sync()
+    rows = max(1, (1 << 24) // A)
+    for i in range(0, N, rows):
+        at = slice(i, min(N, i + rows))
+        grad, logp, tol, tl = policy_rows(l[at], act[at], adv[at], w[at], None if mask is None else mask[at], 0.1)
+        off = ~((r["grad"][at].double() - grad).abs() <= tol)
+        assert not off.any(), (i + off.any(1).nonzero()[0].item(), int(off.sum()))
+        off = ~((r["logp"][at].double() - logp).abs() <= tl)
+        assert not off.any(), (i + off.nonzero()[0].item(), int(off.sum()))

@@ -348,3 +348,24 @@ def test_few_steps_are_taken_one_after_another(sim, dtype):
     y, h = sim.gated_scan(gate, x)
     sim.sync()
     assert (h[0] == 0).all() and torch.equal(h[1], 3.0 * gate[0, 0]) and torch.equal(y[:, 3], h)
+
+
+@pytest.mark.parametrize("dtype", ["f64", "f32", "bf16"])
+@pytest.mark.parametrize("B,T,D", [(5, 300, 1), (40, 70, 1), (3, 130, 3), (4, 90, 24), (2, 6000, 4), (300, 9, 8), (7, 5, 1)])
+def test_time_major_sequences(sim, B, T, D, dtype):
+    """Every array time-major, outputs too: without lengths the sequences' channels lie side by side and are
+    taken as one sequence's, with them they are not; either gives the batch-major results to rounding."""
+    dt = sc.TYPES[dtype]
+    for reverse, lengths, kind in ((False, False, "sigmoid"), (True, False, "linear"), (True, True, "sigmoid")):
+        d = sc.inputs(B, T, D, dt, kind, B + T, h0=not reverse, lengths=lengths, device="cuda")
+        for k in ("gate", "x", "dy"):
+            d[k] = d[k].transpose(0, 1).contiguous().transpose(0, 1)
+        big = torch.full((5, T, B, D), 77.0, dtype=dt, device="cuda")
+        y, dg, dx = (big[i].transpose(0, 1) for i in (1, 2, 3))
+        got, h = sim.gated_scan(d["gate"], d["x"], d["h0"], d["lengths"], kind, reverse, y=y)
+        _, _, dh0 = sim.gated_scan_grad(d["gate"], d["x"], y, d["dy"], d["h0"], d["dstate"], d["lengths"], kind,
+                                        reverse, dgate=dg, dx=dx)
+        sim.sync()
+        assert got is y and (big[0] == 77).all() and (big[4] == 77).all()
+        sc.check_forward(d, y, h, kind, reverse)
+        sc.check_grad(d, y, dg, dx, dh0, kind, reverse)
