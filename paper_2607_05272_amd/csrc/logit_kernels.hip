@@ -431,7 +431,7 @@ __device__ __forceinline__ void place(int c, int A, int& j0, int& skip) {
 
 // Rows of up to 4 KB: 1 << lg lanes take a row, R chunks each; joined by lane moves, without a barrier. Bound
 // by HBM (policy fp32 65536 x 512 51 us, 5.3 TB/s), short rows by what each row takes besides its elements
-// (bf16 131072 x 128 22 us, 3.2 TB/s; balance 16.7 us for the same).
+// (bf16 131072 x 128 22 us, 3.2 TB/s; balance 17 us for the same).
 template <class OP, class E, int N, int R>
 __global__ __launch_bounds__(256) void loss_wave_k(typename OP::Args s, int lg, int nb) {
   typedef typename E::T T;
@@ -561,8 +561,8 @@ __device__ __forceinline__ Part join_threads(Part p, Part* lds) {
 
 // Longer rows: a workgroup takes a row and holds it as it was read, R chunks a thread; while a chunk's
 // gradient goes out the same chunk of the workgroup's next row comes in. Places past the row's end hold
-// -inf. One read and one write: bf16 4096 x 131072 466 us, 4.6 TB/s; of odd length, off the cache lines, 2048 x
-// 50257 107 us, 3.9 TB/s. A row's chain (loads, two joins, gradient) is hidden by the other workgroups of the
+// -inf. One read and one write: bf16 4096 x 131072 492 us, 4.4 TB/s; of odd length, off the cache lines, 2048 x
+// 50257 106 us, 3.9 TB/s. A row's chain (loads, two joins, gradient) is hidden by the other workgroups of the
 // CU alone, 4 waves per SIMD of 128 registers; 8 chunks a thread instead of 16 are slower.
 template <class E, int NT, int R, bool MASK>
 __global__ __launch_bounds__(NT, 4) void policy_block_k(PolicyLossArgs s) {
@@ -788,8 +788,9 @@ struct Run {
     for (int j = whole * N + threadIdx.x; tail && j < s.c.A; j += NT) out[j] = (T)(on ? slope(j, logit(j)) : 0.0f);
   }
 };
-// Rows that no workgroup's registers hold: a workgroup reads a row twice (bf16 512 x 300000 195 us, 4.7 TB/s
-// counting both reads).
+// Rows that no workgroup's registers hold: a workgroup reads a row twice (bf16 512 x 300000 197 us, 4.7 TB/s
+// counting both reads). Masked rows of more than 8192 chunks and all of more than 16384 come here (bf16 65536 and
+// 131072 logits, fp32 half as many) but for few rows: a mask's bytes take as many registers again.
 constexpr int kStream = 1024;
 template <class OP, class E>
 __global__ __launch_bounds__(kStream) void loss_stream_k(typename OP::Args s, int nb) {
@@ -878,6 +879,10 @@ __global__ __launch_bounds__(kSplit) void policy_slopes_k(PolicyLossArgs s) {
 // The place of a workgroup among all: in turn, or each XCD with a run of neighbours, where a wave's piece of a
 // row is 512 bytes (us in turn and so, masked: fp32 131072 x 96 34.7, 33.0; 131072 x 72 30.7, 28.8; 66904 x 72
 // 24.5, 23.7; pieces of 256, bf16 131072 x 72 28.8, 29.1; one workgroup a CU, fp32 40000 x 160 21.8, 24.5).
+// Over fp32 samples and actions, both losses: 0.99 to 1.08 of the other way's speed with up to 12 actions and
+// around 131072 samples (balance 131072 x 24 22.7, 21.0; policy 131072 x 12 10.4, 9.7), 0.92 to 1.01 with few
+// samples of more actions (65536 x 24 8.5, 9.2; 16384 x 72 8.3, 8.7), 0.93 to 1.05 with 262144 (x 72 masked 56.6,
+// 60.8; balance x 24 26.8, 25.4).
 template <bool RUNS>
 __device__ __forceinline__ int64_t first_of() {
   if constexpr (RUNS) {
@@ -1068,7 +1073,7 @@ __global__ __launch_bounds__(64 * W * GR) void loss_cols_k(typename OP::Args s, 
 
 // More actions than the waves of a workgroup hold: a lane takes a sample, kLaneWaves waves share its actions
 // and read them twice (policy fp32 65536 x 500 81 us, 4.9 TB/s counting both reads; balance 87; few samples of
-// many actions leave most of the chip empty: bf16 2048 x 50257 2.5 ms, by rows 107 us).
+// many actions leave most of the chip empty: bf16 2048 x 50257 2.5 ms, by rows 106 us).
 constexpr int kLaneWaves = 16;
 template <class OP, class E>
 __global__ __launch_bounds__(64 * kLaneWaves) void loss_lane_k(typename OP::Args s, int nb) {

@@ -441,8 +441,9 @@ __global__ __launch_bounds__(kThreads) void scan_runs_k(ScanArgs s, ScanPlan p) 
 
 // The recurrence: a segment's products and states stay in registers (64 of them) between the pass from 0 and
 // the one that adds the state before it; the next tile's loads fly under the scan. Bound by HBM with many
-// workgroups (fp32 16 x 1025 x 1536 62 us, 4.8 TB/s; fp64 1 x 4000 x 8192 157 us, 5.0; one channel, fp32
-// 4096 x 4096 38 us, 5.3), by the latency of a tile (loads, scan, barrier) with the one a CU that 2048 bf16
+// workgroups (fp32 16 x 1025 x 1536 72 us, 4.2 TB/s; fp64 1 x 4000 x 8192 157 us, 5.0; one channel, fp32
+// 4096 x 4096 38 us, 5.3; with half of the steps padding, which is not read but goes through the scan, the first
+// 63 us, 3.3 TB/s), by the latency of a tile (loads, scan, barrier) with the one a CU that 2048 bf16
 // channels of 8 sequences make: 61 us, 3.3 TB/s. Splitting those over time instead reads twice (88 us for
 // as many elements); two tiles ahead, 512 threads or wider pieces of a row are slower (62, 58, 75).
 template <class E, bool SIG, int V, int L, bool TV>
@@ -542,8 +543,8 @@ __global__ __launch_bounds__(kThreads) void scan_tile_k(ScanArgs s, ScanPlan p) 
 // The gradient, against the order of the states: C, what later steps ask of a state, goes through the same
 // scan (C = a (dy + C)), and a second pass over the raw elements, kept in registers, makes dg and dx. It
 // computes the gates twice: keeping them takes 30 registers and a third of the waves (bf16 16 x 1024 x 4096
-// step 317 us, 305 so). Bound by HBM: fp32 16 x 1025 x 1536 83 us for five arrays, 6.1 TB/s with what the
-// cache still holds; bf16 1 x 65536 x 512 110 us for six, 3.7 TB/s in chunks. The next tile's loads under the
+// step 317 us, 305 so). Bound by HBM: fp32 16 x 1025 x 1536 119 us for five arrays, 4.2 TB/s (half of
+// the steps padding 96 us, 3.7); bf16 1 x 65536 x 512 111 us for six, 3.6 TB/s in chunks. The next tile's loads under the
 // scan help unaligned rows by 5% and cost aligned ones as much (187 against 181 us): not done.
 template <class E, bool SIG, int V, int L, bool TV>
 __global__ __launch_bounds__(kThreads) void scan_grad_k(ScanArgs s, ScanPlan p) {

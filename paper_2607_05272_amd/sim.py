@@ -326,6 +326,8 @@ class Sim:
         return grads, loss, idx
 
     # -- operators for the caller's own networks -------------------------------------------
+    # They work on the tensors' memory and are no part of torch's autograd: results do not require
+    # gradients, and a gradient is computed where its function is called.
     def _check(self, name, t, shape, dtypes):
         """`t` is a tensor on the context's device, of this shape and one of these types."""
         if t.dtype in dtypes and t.shape == shape and t.device == self._device:
@@ -457,7 +459,7 @@ class Sim:
         int64, adv [N] fp32 or fp64, logp_old, logp_ref, weight [N] fp32 (0: padding; default
         1/N), mask [N][A] bool or uint8 (0 forbids). Returns dict(loss [4] fp32: total, policy, KL and
         entropy terms; logp [N]; grad [N][A] in the logits' type, which may be the logits
-        themselves: grad=logits)."""
+        themselves: grad=logits). Few samples of more than 384 actions are much faster as rows."""
         N, A = logits.shape
         self._check("logits", logits, (N, A), (torch.float32, torch.bfloat16, torch.float16))
         self._flat("actions", actions, (N,), _INT)
