@@ -502,7 +502,8 @@ typedef struct sim_policy_loss {
  * mask [N][A] bytes (NULL: all allowed; any strides, stride_n = 0 to share a row): 0 forbids
  * an action, whatever its logit holds, and so does a logit of -inf. d_weight [N] (NULL:
  * 1/N each): samples of weight 0 are not looked at. d_logp_old NULL: logp itself (the first step
- * after a rollout: rho = 1). d_logp_ref may be NULL if c_kl = 0. Outputs: grad dL/dlogits (may be
+ * after a rollout: rho = 1). d_logp_ref may be NULL if c_kl = 0; then it gives d_loss[2] alone,
+ * and no part of L or grad, infinite or not. Outputs: grad dL/dlogits (may be
  * NULL, or the logits themselves: same pointer and strides), d_logp [N] (may be NULL), d_loss [4]
  * fp32: L and its policy, KL and entropy terms (sums of w times each, without the c's; summed in
  * fp64). A sample of weight 0, or with no allowed action, gives nothing: gradient 0, logp 0. So
