@@ -402,8 +402,8 @@ int sim_update(sim_ctx* ctx, const sim_update_cfg* cfg, void* d_weights, float* 
                const double* d_ret, double* d_losses);
 
 /* Operators for policies that the caller's own network computes (a sequence model, a router, an
- * action set of any size): the recurrence, the policy loss and a router's balance loss, each
- * with its gradient. They use a context for its stream, its device and its error flags only,
+ * action set of any size): the recurrence, linear attention, the policy loss, a router's balance
+ * loss and log-probabilities, each with its gradient, and the step of matrices. They use a context for its stream, its device and its error flags only,
  * whatever its configuration; the sizes are their own. Common to them:
  *   - Work memory is the caller's: the *_work calls (no device work) give the bytes, 16-byte
  *     aligned memory; nothing need be in it, and calls that may overlap (two streams, two
@@ -415,8 +415,8 @@ int sim_update(sim_ctx* ctx, const sim_update_cfg* cfg, void* d_weights, float* 
  *     output must not share memory (SIM_EINVAL). Outputs may not overlap inputs but where
  *     stated. Every array must be aligned to its element. Sizes of 0 are allowed.
  *   - Sums run in a fixed order: repeated calls return the same bits.
- *   - While tracing (sim_set_timing) the recurrence counts as SIM_KC_GAE, the losses as
- *     SIM_KC_PPO.                                                                          */
+ *   - While tracing (sim_set_timing) the recurrence and linear attention count as SIM_KC_GAE, the
+ *     others as SIM_KC_PPO.                                                                */
 enum { SIM_DT_F64 = 0, SIM_DT_F32 = 1, SIM_DT_BF16 = 2, SIM_DT_F16 = 3 };
 enum { SIM_IT_U8 = 0, SIM_IT_I32 = 1, SIM_IT_I64 = 2 };
 enum { SIM_GATE_LINEAR = 0, SIM_GATE_SIGMOID = 1 };
@@ -540,6 +540,118 @@ int balance_loss(sim_ctx* ctx, const sim_balance* c, const sim_mat* logits, cons
                  const uint8_t* d_live, const sim_mat* grad, int64_t* d_counts, float* d_loss,
                  void* d_work, size_t work_bytes);
 
+/* ---- a sequence layer, log-probabilities and updates of the caller's own network ------------
+ * Linear attention with a decay for each head: a state that is a matrix, beside gated_scan's vector.
+ * An array over sequences, steps, heads and channels: element (b, t, h, d) at b*stride_b +
+ * t*stride_t + h*stride_h + d.                                                             */
+typedef struct sim_heads {
+  void* data;
+  int64_t stride_b, stride_t, stride_h;
+} sim_heads;
+
+/*  B, T    sequences, steps (below 2^30)
+ *  H, Hk   heads of q and y, heads of k and v: Hk divides H, and heads [i H/Hk, (i+1) H/Hk) share
+ *          the keys and values i (B H below 2^24, B T H below 2^40)
+ *  Dk, Dv  channels of q and k, of v and y: 1 to 256 each
+ *  dtype   of q, k, v, y and their gradients (not SIM_DT_F64); states are fp32
+ *  scale   finite                                                                         */
+typedef struct sim_linear_attn {
+  int64_t B, T;
+  int32_t H, Hk, Dk, Dv, dtype;
+  float scale;
+} sim_linear_attn;
+
+/* Per sequence b and head h, from S = d_s0[b][h] ([B][H][Dk][Dv] contiguous fp32, NULL: 0), with l =
+ * d_decay[h] (fp32, in [0, 1]):
+ *   S = l S + k_t v_t^T,   y_t = scale S^T q_t,     t = 0, 1, ..
+ * d_state [B][H][Dk][Dv] (NULL: not wanted) receives S after the last step and may be d_s0 itself
+ * (serving: T = 1, the state updated in place). y may be NULL (only the state is wanted). d_len [B]
+ * int32 (NULL: all T): steps t >= d_len[b] are padding, whatever they hold: they leave S as it is and
+ * their y is 0; a length outside [0, T] latches SIM_ESTATE and is taken as the nearer bound, and so
+ * does a decay outside [0, 1] (NaN as 0).
+ * Up to T = 16 steps are taken one after another. With more, a run of steps is taken at once: the
+ * products q_t k_s, weighted by l^(t-s), and the state between runs are held in fp32 and multiplied as
+ * bf16 parts that add up to them (two for 16-bit types, 16 bits of the value; three for fp32, all 24), so
+ * they must be finite in fp32, and results differ from a step-by-step sum by rounding. */
+int linear_attn_work(const sim_linear_attn* s, size_t* bytes);
+int linear_attn(sim_ctx* ctx, const sim_linear_attn* s, const sim_heads* q, const sim_heads* k,
+                const sim_heads* v, const float* d_decay, const int32_t* d_len, const float* d_s0,
+                const sim_heads* y, float* d_state, void* d_work, size_t work_bytes);
+
+/* Its gradient: from dy and d_dstate [B][H][Dk][Dv] (gradient of the last state, NULL: 0) those of q, k,
+ * v and s0 (each may be NULL; d_ds0 may be d_dstate). With G the gradient of S after a step,
+ *   G_t = scale q_t dy_t^T + l G_{t+1} (after the last step + dstate),
+ *   dq_t = scale S_t dy_t,  dk_t = sum over the heads that share it of G_t v_t,  dv_t = .. of G_t^T k_t
+ * and ds0 = l G_0. The decays are constants of the layer and get no gradient. Padding gets 0. The
+ * states are formed again from q, k and v: nothing is kept of the forward call.               */
+int linear_attn_grad_work(const sim_linear_attn* s, size_t* bytes);
+int linear_attn_grad(sim_ctx* ctx, const sim_linear_attn* s, const sim_heads* q, const sim_heads* k,
+                     const sim_heads* v, const float* d_decay, const sim_heads* dy,
+                     const int32_t* d_len, const float* d_s0, const float* d_dstate,
+                     const sim_heads* dq, const sim_heads* dk, const sim_heads* dv, float* d_ds0,
+                     void* d_work, size_t work_bytes);
+
+/* Log-probabilities of given tokens (actions) over the logits of any network, the entropy and the
+ * likeliest columns: what policy_loss takes as d_logp_old and d_logp_ref, and what is told of a choice.
+ *  N, A        rows (below 2^31), columns (below 2^30)
+ *  top         alternatives per row, 0 to 64
+ *  dtype       of logits and gradient (not SIM_DT_F64);  token_type  SIM_IT_*             */
+typedef struct sim_logprobs {
+  int64_t N;
+  int32_t A, top, dtype, token_type;
+} sim_logprobs;
+
+/* With p the softmax of a row's logits over its allowed columns (mask [N][A] bytes as for policy_loss,
+ * NULL: all; a logit of -inf is forbidden too): d_logp [N] = log p of the given token (-inf if it is
+ * forbidden), d_entropy [N] = -sum p log p, d_top_index [N][top] int64 the columns of the largest logits,
+ * largest first and of equal ones the lowest column first (a NaN counts as the largest), and d_top_logp
+ * [N][top] their log p. Where a row allows fewer than top columns the rest is -1 and -inf. Each output may be
+ * NULL; d_tokens may be NULL if d_logp is. A token of -1 (not with SIM_IT_U8) is none: its logp is 0; any
+ * other outside [0, A) latches SIM_ESTATE and is taken as none. Rows with d_live [N] bytes (NULL: all) 0
+ * are not looked at; they, and rows that allow no column, give nothing: logp 0, entropy 0, no
+ * alternatives. Alternatives are best had of rows of adjacent columns, or of up to 384 columns.  */
+int token_logprobs_work(const sim_logprobs* c, size_t* bytes);
+int token_logprobs(sim_ctx* ctx, const sim_logprobs* c, const sim_mat* logits, const sim_mat* mask,
+                   const void* d_tokens, const uint8_t* d_live, float* d_logp, float* d_entropy,
+                   int64_t* d_top_index, float* d_top_logp, void* d_work, size_t work_bytes);
+
+/* The gradient over the logits of sum_n (d_dlogp[n] logp_n + d_dentropy[n] H_n) (either may be NULL: 0):
+ *   dl_j = dlogp (1[j = token] - p_j) - dentropy p_j (log p_j + H)
+ * Forbidden columns, and rows that give nothing, get 0; of a row whose token is none or forbidden only the
+ * entropy's part is left. grad may be the logits themselves (same pointer and strides). top is not looked at. */
+int token_logprobs_grad_work(const sim_logprobs* c, size_t* bytes);
+int token_logprobs_grad(sim_ctx* ctx, const sim_logprobs* c, const sim_mat* logits, const sim_mat* mask,
+                        const void* d_tokens, const uint8_t* d_live, const float* d_dlogp,
+                        const float* d_dentropy, const sim_mat* grad, void* d_work, size_t work_bytes);
+
+/* Matrices: element (i, r, c) at i*stride_i + r*stride_r + c*stride_c. */
+typedef struct sim_mats {
+  void* data;
+  int64_t stride_i, stride_r, stride_c;
+} sim_mats;
+
+/* An update orthogonalised by Newton-Schulz products, for the matrices of a network beside adam_update's
+ * step: a polynomial that takes the singular values of U / |U| towards 1 and leaves the singular vectors.
+ *  n, M, N   matrices, rows and columns (up to 65536 each, n below 2^16)
+ *  steps     0 to 32;  dtype  of U and the result (not SIM_DT_F64)
+ *  a, b, c   the polynomial's coefficients;  eps >= 0;  scale  of the result             */
+typedef struct sim_ortho {
+  int64_t n, M, N;
+  int32_t steps, dtype;
+  float a, b, c, eps, scale;
+} sim_ortho;
+
+/* X = U / (|U|_F + eps), then `steps` times, with A = X X^T (X^T X for M > N, which comes to the same),
+ *   X = a X + (b A + c A A) X
+ * and out = scale X. The norm is summed in fp64, sums of products in fp32; between products X, A and
+ * b A + c A A are held as fp16 parts of the value times 2^10: one (11 bits) for bf16, whose own rounding is
+ * coarser, two (22 bits) otherwise. So singular values, and A's and the polynomial's, must stay below 60 (with
+ * the usual coefficients they stay below 4). U and out may have any strides and be the same memory; a matrix
+ * of zeros gives zeros, one that holds an infinity or NaN gives NaN.                         */
+int orthogonalize_work(const sim_ortho* c, size_t* bytes);
+int orthogonalize(sim_ctx* ctx, const sim_ortho* c, const sim_mats* update, const sim_mats* out,
+                  void* d_work, size_t work_bytes);
+
 /* Per-environment counters [2][SIM_NCNT][E] int64 and sums [2][SIM_NSUM][E] fp64 into
  * device buffers (either may be NULL).                                                  */
 int sim_counters(sim_ctx* ctx, int64_t* d_cnt, double* d_sum);
@@ -592,10 +704,11 @@ enum sim_kernel_class {
   SIM_KC_POLICY = 0,  /* policy MLP + sampler */
   SIM_KC_STEP = 1,    /* learned system, one tick */
   SIM_KC_STATIC = 2,  /* static shadow system, one tick */
-  SIM_KC_GAE = 3,     /* returns / GAE, gated_scan, gated_scan_grad */
+  SIM_KC_GAE = 3,     /* returns / GAE, gated_scan, linear_attn and their gradients */
   SIM_KC_RESET = 4,   /* reset */
   SIM_KC_OTHER = 5,   /* weight repack / init, observation packing, counters, totals */
-  SIM_KC_PPO = 6,     /* policy update: minibatch gradients, Adam, policy_loss, balance_loss */
+  SIM_KC_PPO = 6,     /* policy update: minibatch gradients, Adam, policy_loss, balance_loss,
+                         token_logprobs and its gradient, orthogonalize */
   SIM_KC_ROLLOUT = 7, /* fused rollout: every tick's policy and learned tick in one launch */
   SIM_KC_COUNT = 8
 };

@@ -5,6 +5,9 @@ gated_scan        h = g_t h + x_t, or h = f h + (1 - f) x_t with f = 1/(1 + exp(
 gated_scan_grad   its gradient, from the stored y
 policy_loss       the clipped policy loss with a KL term over logits, and its gradient
 balance_loss      a router's balance loss, its counts and its gradient
+linear_attn       S = decay S + k v^T, y = scale S^T q, and linear_attn_grad
+token_logprobs    log-probabilities, entropies, alternatives, and token_logprobs_grad
+orthogonalize     Newton-Schulz products of an update
 """
 import numpy as np
 
@@ -166,3 +169,99 @@ def grad_majorants(gate, dy, dstate, lengths, kind, reverse):
         E[on, t] = M[on, t] + e[on]
         m[on], e[on] = a * M[on, t], a * E[on, t] + a * M[on, t]
     return M, E, m, e
+
+
+def linear_attn(q, k, v, decay, s0=None, lengths=None, scale=1.0):
+    """y [B][T][H][Dv] and the last state [B][H][Dk][Dv]: S = decay S + k_t v_t^T, y_t = scale S^T q_t."""
+    B, T, H, Dk = q.shape
+    g, Dv = H // k.shape[2], v.shape[3]
+    n = np.full(B, T) if lengths is None else np.asarray(lengths)
+    S = np.zeros((B, H, Dk, Dv)) if s0 is None else np.array(s0, np.float64)
+    y = np.zeros((B, T, H, Dv))
+    for t in range(T):
+        on = t < n
+        kt, vt = (np.repeat(x[on, t].astype(np.float64), g, axis=1) for x in (k, v))
+        S[on] = decay[:, None, None] * S[on] + kt[..., :, None] * vt[..., None, :]
+        y[on, t] = scale * (q[on, t].astype(np.float64)[..., None, :] @ S[on])[..., 0, :]
+    return y, S
+
+
+def linear_attn_grad(q, k, v, decay, dy, s0=None, dstate=None, lengths=None, scale=1.0):
+    """dq, dk, dv, ds0 of linear_attn, from the states of every step."""
+    B, T, H, Dk = q.shape
+    Hk, Dv = v.shape[2:]
+    g = H // Hk
+    n = np.full(B, T) if lengths is None else np.asarray(lengths)
+    S = np.zeros((B, H, Dk, Dv)) if s0 is None else np.array(s0, np.float64)
+    G = np.zeros((B, H, Dk, Dv)) if dstate is None else np.array(dstate, np.float64)
+    dq, dk, dv = (np.zeros(x.shape) for x in (q, k, v))
+    l = decay[:, None, None]
+    for t in range(T):
+        on = t < n
+        kt, vt = (np.repeat(x[on, t].astype(np.float64), g, axis=1) for x in (k, v))
+        S[on] = l * S[on] + kt[..., :, None] * vt[..., None, :]
+        dq[on, t] = scale * (S[on] @ dy[on, t].astype(np.float64)[..., None])[..., 0]
+    for t in range(T - 1, -1, -1):
+        on = t < n
+        kt, vt = (np.repeat(x[on, t].astype(np.float64), g, axis=1) for x in (k, v))
+        qt, dt = q[on, t].astype(np.float64), dy[on, t].astype(np.float64)
+        Gt = G[on] + scale * qt[..., :, None] * dt[..., None, :]
+        dk[on, t] = (Gt @ vt[..., None])[..., 0].reshape(-1, Hk, g, Dk).sum(2)
+        dv[on, t] = (kt[..., None, :] @ Gt)[..., 0, :].reshape(-1, Hk, g, Dv).sum(2)
+        G[on] = l * Gt
+    return dq, dk, dv, G
+
+
+def token_logprobs(logits, tokens=None, mask=None, live=None, top=0):
+    """Dict: logp, entropy [N], top_index, top_logp [N][top], and ls, p [N][A] of the rows that give anything."""
+    N, A = logits.shape
+    r = dict(logp=np.zeros(N), entropy=np.zeros(N), top_index=np.full((N, top), -1), top_logp=np.full((N, top), -np.inf),
+             ls=[None] * N, p=[None] * N)
+    for n in range(N):
+        z = logits[n].astype(np.float64)
+        if mask is not None:
+            z = np.where(mask[n], z, -np.inf)
+        if (live is not None and not live[n]) or not (z > -np.inf).any():
+            continue
+        x = z - z.max()
+        ls = x - np.log(np.exp(x).sum())
+        p = np.exp(ls)
+        r["ls"][n], r["p"][n] = ls, p
+        r["entropy"][n] = -(p[p > 0] * ls[p > 0]).sum()
+        if tokens is not None and 0 <= tokens[n] < A:
+            r["logp"][n] = ls[tokens[n]]
+        order = [j for j in sorted(range(A), key=lambda j: (-z[j], j)) if z[j] > -np.inf][:top]
+        r["top_index"][n, :len(order)] = order
+        r["top_logp"][n, :len(order)] = ls[order]
+    return r
+
+
+def token_logprobs_grad(logits, tokens, dlogp, dentropy, mask=None, live=None):
+    """The gradient of sum(dlogp logp + dentropy H); rows whose token is none or forbidden keep H's part."""
+    r = token_logprobs(logits, tokens, mask, live)
+    d = np.zeros(logits.shape)
+    for n in range(len(logits)):
+        ls, p = r["ls"][n], r["p"][n]
+        if p is None:
+            continue
+        a = -1 if tokens is None else int(tokens[n])
+        g = float(dlogp[n]) if dlogp is not None and 0 <= a < len(p) and ls[a] > -np.inf else 0.0
+        h = 0.0 if dentropy is None else float(dentropy[n])
+        d[n] = -p * (g + h * (np.where(p > 0, ls, 0.0) + r["entropy"][n]))
+        if g:
+            d[n, a] += g
+    return d
+
+
+def orthogonalize(u, steps=5, coeffs=(3.4445, -4.7750, 2.0315), eps=1e-7, scale=1.0):
+    """One matrix [M][N]; and every X on the way, with the shorter side as rows."""
+    a, b, c = coeffs
+    x = np.asarray(u, np.float64)
+    x = x.T if x.shape[0] > x.shape[1] else x
+    x = x / (np.sqrt((x * x).sum()) + eps)
+    way = [x]
+    for _ in range(steps):
+        A = x @ x.T
+        x = a * x + (b * A + c * A @ A) @ x
+        way.append(x)
+    return scale * (x.T if u.shape[0] > u.shape[1] else x), way

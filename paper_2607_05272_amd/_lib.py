@@ -26,7 +26,9 @@ SYMBOLS = ("sim_last_error", "sim_abi_version", "sim_create", "sim_destroy", "si
            "sim_get_state", "sim_set_state", "sim_device_primitive", "sim_policy_hidden", "sim_set_graphs", "sim_graph_stats",
            "ppo_minibatch_grad_noalloc", "sim_set_fused_rollout", "gated_scan_work", "gated_scan",
            "gated_scan_grad_work", "gated_scan_grad", "policy_loss_work", "policy_loss",
-           "balance_loss_work", "balance_loss")
+           "balance_loss_work", "balance_loss", "linear_attn_work", "linear_attn",
+           "linear_attn_grad_work", "linear_attn_grad", "token_logprobs_work", "token_logprobs",
+           "token_logprobs_grad_work", "token_logprobs_grad", "orthogonalize_work", "orthogonalize")
 ALGO_PPO, ALGO_REINFORCE = 0, 1
 KERNEL_CLASSES = ("policy", "step", "static", "gae", "reset", "other", "ppo", "rollout")
 FUSE_OFF, FUSE_AUTO, FUSE_ON = 0, 1, 2
@@ -106,6 +108,32 @@ class SimBalance(C.Structure):
                 ("dtype", C.c_int32), ("index_type", C.c_int32), ("coef", C.c_float)]
 
 
+class SimHeads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_b", C.c_int64), ("stride_t", C.c_int64),
+                ("stride_h", C.c_int64)]
+
+
+class SimLinearAttn(C.Structure):
+    _fields_ = [("B", C.c_int64), ("T", C.c_int64), ("H", C.c_int32), ("Hk", C.c_int32),
+                ("Dk", C.c_int32), ("Dv", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float)]
+
+
+class SimLogprobs(C.Structure):
+    _fields_ = [("N", C.c_int64), ("A", C.c_int32), ("top", C.c_int32), ("dtype", C.c_int32),
+                ("token_type", C.c_int32)]
+
+
+class SimMats(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_i", C.c_int64), ("stride_r", C.c_int64),
+                ("stride_c", C.c_int64)]
+
+
+class SimOrtho(C.Structure):
+    _fields_ = [("n", C.c_int64), ("M", C.c_int64), ("N", C.c_int64), ("steps", C.c_int32),
+                ("dtype", C.c_int32), ("a", C.c_float), ("b", C.c_float), ("c", C.c_float),
+                ("eps", C.c_float), ("scale", C.c_float)]
+
+
 class SimTotals(C.Structure):
     _fields_ = [("cnt", (C.c_int64 * NCNT) * 2), ("sum", (C.c_double * NSUM) * 2)]
 
@@ -160,6 +188,11 @@ def load():
         "gated_scan": [vp] * 9 + [C.c_size_t], "gated_scan_grad": [vp] * 13 + [C.c_size_t],
         "policy_loss_work": [vp, vp], "policy_loss": [vp] * 13 + [C.c_size_t],
         "balance_loss_work": [vp, vp], "balance_loss": [vp] * 9 + [C.c_size_t],
+        "linear_attn_work": [vp, vp], "linear_attn": [vp] * 11 + [C.c_size_t],
+        "linear_attn_grad_work": [vp, vp], "linear_attn_grad": [vp] * 15 + [C.c_size_t],
+        "token_logprobs_work": [vp, vp], "token_logprobs": [vp] * 11 + [C.c_size_t],
+        "token_logprobs_grad_work": [vp, vp], "token_logprobs_grad": [vp] * 10 + [C.c_size_t],
+        "orthogonalize_work": [vp, vp], "orthogonalize": [vp] * 5 + [C.c_size_t],
     }
     for name, args in sig.items():
         f = getattr(L, name)

@@ -162,6 +162,86 @@ int check_balance(const sim_balance* c, const char* who) {
   return SIM_OK;
 }
 
+// three strided dimensions and runs of adjacent elements: the offsets stay below 2^62 bytes, and of an
+// output no two elements are the same
+struct Dim { int64_t stride, n; };
+int check_box(const void* data, const Dim (&dims)[3], int64_t run, int eb, bool out, const char* who,
+              const char* name) {
+  __int128 last = run;
+  bool some = run > 0;
+  for (const Dim& d : dims) {
+    if (d.stride < 0) return op_fail(SIM_EINVAL, "%s: negative stride of %s", who, name);
+    last += (__int128)std::max<int64_t>(d.n - 1, 0) * d.stride;
+    some = some && d.n > 0;
+  }
+  if (last * eb > ((__int128)1 << 62)) return op_fail(SIM_EINVAL, "%s: strides of %s pass 2^62 bytes", who, name);
+  if (!aligned(data, eb)) return op_fail(SIM_EINVAL, "%s: %s is not aligned to its type", who, name);
+  if (out && some) {
+    Dim s[3] = {dims[0], dims[1], dims[2]};
+    std::sort(s, s + 3, [](const Dim& p, const Dim& q) { return p.stride < q.stride; });
+    __int128 span = run;
+    for (const Dim& d : s) {
+      if (d.n <= 1) continue;
+      if (d.stride < span) return op_fail(SIM_EINVAL, "%s: elements of %s share memory", who, name);
+      span += (__int128)d.stride * (d.n - 1);
+    }
+  }
+  return SIM_OK;
+}
+
+int check_attn(const sim_linear_attn* s, const char* who) {
+  if (!s) return op_fail(SIM_EINVAL, "%s: sizes are NULL", who);
+  if (s->dtype < SIM_DT_F32 || s->dtype > SIM_DT_F16) return op_fail(SIM_EINVAL, "%s: arrays of type %d", who, s->dtype);
+  if (s->B < 0 || s->T < 0) return op_fail(SIM_EINVAL, "%s: B and T must be >= 0", who);
+  if (s->H < 1 || s->Hk < 1 || s->H % s->Hk) return op_fail(SIM_EINVAL, "%s: Hk must be >= 1 and divide H", who);
+  if (s->Dk < 1 || s->Dv < 1) return op_fail(SIM_EINVAL, "%s: Dk and Dv must be >= 1", who);
+  if (s->Dk > 256 || s->Dv > 256) return op_fail(SIM_EUNSUPPORTED, "%s: Dk and Dv go up to 256", who);
+  if (!(s->scale - s->scale == 0.0f)) return op_fail(SIM_EINVAL, "%s: scale must be finite", who);
+  if (s->T >= (1 << 30) || s->B >= (1 << 24) || s->B * s->H >= (1 << 24) ||
+      (__int128)s->B * s->T * s->H >= ((__int128)1 << 40))
+    return op_fail(SIM_EUNSUPPORTED, "%s: T must stay below 2^30, B*H below 2^24, B*T*H below 2^40", who);
+  return SIM_OK;
+}
+
+// one array over steps and heads; `need`: it may not be absent, `out`: its elements are written
+int check_heads(const sim_linear_attn& c, const sim_heads* x, int H, int D, bool need, bool out, const char* who,
+                const char* name, sim_heads* got) {
+  *got = sim_heads{nullptr, 0, 0, 0};
+  if (!x || !x->data) {
+    if (need && c.B && c.T) return op_fail(SIM_EINVAL, "%s: %s is NULL", who, name);
+    return SIM_OK;
+  }
+  const Dim dims[3] = {{x->stride_b, c.B}, {x->stride_t, c.T}, {x->stride_h, H}};
+  *got = *x;
+  return check_box(x->data, dims, D, elem_bytes(c.dtype), out, who, name);
+}
+
+int check_logprobs(const sim_logprobs* c, const char* who) {
+  if (!c) return op_fail(SIM_EINVAL, "%s: sizes are NULL", who);
+  if (c->N < 0 || c->N > kMax31) return op_fail(SIM_EINVAL, "%s: N must lie in [0, 2^31)", who);
+  if (c->A < 1) return op_fail(SIM_EINVAL, "%s: A must be >= 1", who);
+  if (c->A >= (1 << 30)) return op_fail(SIM_EUNSUPPORTED, "%s: A must stay below 2^30", who);
+  if (c->top < 0) return op_fail(SIM_EINVAL, "%s: top must be >= 0", who);
+  if (c->top > 64) return op_fail(SIM_EUNSUPPORTED, "%s: at most 64 alternatives", who);
+  if (c->dtype < SIM_DT_F32 || c->dtype > SIM_DT_F16) return op_fail(SIM_EINVAL, "%s: logits of type %d", who, c->dtype);
+  if (c->token_type < SIM_IT_U8 || c->token_type > SIM_IT_I64)
+    return op_fail(SIM_EINVAL, "%s: unknown token type %d", who, c->token_type);
+  return SIM_OK;
+}
+
+int check_ortho(const sim_ortho* c, const char* who) {
+  if (!c) return op_fail(SIM_EINVAL, "%s: sizes are NULL", who);
+  if (c->n < 0 || c->M < 0 || c->N < 0) return op_fail(SIM_EINVAL, "%s: n, M and N must be >= 0", who);
+  if (c->M > 65536 || c->N > 65536 || c->n >= 65536)
+    return op_fail(SIM_EUNSUPPORTED, "%s: M and N go up to 65536, n below 65536", who);
+  if (c->steps < 0 || c->steps > 32) return op_fail(SIM_EINVAL, "%s: steps must lie in [0, 32]", who);
+  if (c->dtype < SIM_DT_F32 || c->dtype > SIM_DT_F16) return op_fail(SIM_EINVAL, "%s: matrices of type %d", who, c->dtype);
+  for (const float v : {c->a, c->b, c->c, c->eps, c->scale})
+    if (!(v - v == 0.0f)) return op_fail(SIM_EINVAL, "%s: coefficients, eps and scale must be finite", who);
+  if (c->eps < 0.0f) return op_fail(SIM_EINVAL, "%s: eps must be >= 0", who);
+  return SIM_OK;
+}
+
 int int_bytes(int t) { return t == SIM_IT_U8 ? 1 : (t == SIM_IT_I32 ? 4 : 8); }
 
 }  // namespace
@@ -296,6 +376,179 @@ int balance_loss(sim_ctx* x, const sim_balance* c, const sim_mat* logits, const 
   const OpCtx o = op_ctx(x);
   a.err = o.err;
   return on_ctx(x, SIM_KC_PPO, who, [&] { return launch_balance(a, o.stream); });
+}
+
+int linear_attn_work(const sim_linear_attn* s, size_t* bytes) {
+  int rc = check_attn(s, "linear_attn_work");
+  if (rc) return rc;
+  if (!bytes) return op_fail(SIM_EINVAL, "linear_attn_work: bytes is NULL");
+  *bytes = attn_work_bytes(*s, false);
+  return SIM_OK;
+}
+
+int linear_attn(sim_ctx* x, const sim_linear_attn* s, const sim_heads* q, const sim_heads* k, const sim_heads* v,
+                const float* d_decay, const int32_t* d_len, const float* d_s0, const sim_heads* y,
+                float* d_state, void* d_work, size_t work_bytes) {
+  const char* who = "linear_attn";
+  if (!x) return op_fail(SIM_EINVAL, "%s: ctx is NULL", who);
+  int rc = check_attn(s, who);
+  if (rc) return rc;
+  AttnArgs a{};
+  a.c = *s;
+  if ((rc = check_heads(*s, y, s->H, s->Dv, false, true, who, "y", &a.y))) return rc;
+  if ((rc = check_heads(*s, q, s->H, s->Dk, a.y.data, false, who, "q", &a.q))) return rc;
+  if ((rc = check_heads(*s, k, s->Hk, s->Dk, true, false, who, "k", &a.k))) return rc;
+  if ((rc = check_heads(*s, v, s->Hk, s->Dv, true, false, who, "v", &a.v))) return rc;
+  if (!d_decay && s->B) return op_fail(SIM_EINVAL, "%s: decay is NULL", who);
+  if (!aligned(d_decay, 4) || !aligned(d_len, 4) || !aligned(d_s0, 4) || !aligned(d_state, 4))
+    return op_fail(SIM_EINVAL, "%s: decays, lengths and states must be aligned to their type", who);
+  if ((rc = check_work(d_work, work_bytes, attn_work_bytes(*s, false), who))) return rc;
+  if (s->B == 0 || ((!a.y.data || s->T == 0) && !d_state)) return SIM_OK;
+  a.decay = d_decay; a.len = d_len; a.s0 = d_s0; a.state = d_state; a.work = d_work;
+  const OpCtx o = op_ctx(x);
+  a.err = o.err;
+  return on_ctx(x, SIM_KC_GAE, who, [&] { return launch_attn(a, false, o.stream); });
+}
+
+int linear_attn_grad_work(const sim_linear_attn* s, size_t* bytes) {
+  int rc = check_attn(s, "linear_attn_grad_work");
+  if (rc) return rc;
+  if (!bytes) return op_fail(SIM_EINVAL, "linear_attn_grad_work: bytes is NULL");
+  *bytes = attn_work_bytes(*s, true);
+  return SIM_OK;
+}
+
+int linear_attn_grad(sim_ctx* x, const sim_linear_attn* s, const sim_heads* q, const sim_heads* k,
+                     const sim_heads* v, const float* d_decay, const sim_heads* dy, const int32_t* d_len,
+                     const float* d_s0, const float* d_dstate, const sim_heads* dq, const sim_heads* dk,
+                     const sim_heads* dv, float* d_ds0, void* d_work, size_t work_bytes) {
+  const char* who = "linear_attn_grad";
+  if (!x) return op_fail(SIM_EINVAL, "%s: ctx is NULL", who);
+  int rc = check_attn(s, who);
+  if (rc) return rc;
+  AttnArgs a{};
+  a.c = *s;
+  if ((rc = check_heads(*s, dq, s->H, s->Dk, false, true, who, "dq", &a.dq))) return rc;
+  if ((rc = check_heads(*s, dk, s->Hk, s->Dk, false, true, who, "dk", &a.dk))) return rc;
+  if ((rc = check_heads(*s, dv, s->Hk, s->Dv, false, true, who, "dv", &a.dv))) return rc;
+  const bool some = a.dq.data || a.dk.data || a.dv.data;
+  if ((rc = check_heads(*s, q, s->H, s->Dk, a.dk.data || a.dv.data || d_ds0, false, who, "q", &a.q))) return rc;
+  if ((rc = check_heads(*s, k, s->Hk, s->Dk, a.dq.data || a.dv.data, false, who, "k", &a.k))) return rc;
+  if ((rc = check_heads(*s, v, s->Hk, s->Dv, a.dq.data || a.dk.data, false, who, "v", &a.v))) return rc;
+  if ((rc = check_heads(*s, dy, s->H, s->Dv, true, false, who, "dy", &a.dy))) return rc;
+  if (!d_decay && s->B) return op_fail(SIM_EINVAL, "%s: decay is NULL", who);
+  if (!aligned(d_decay, 4) || !aligned(d_len, 4) || !aligned(d_s0, 4) || !aligned(d_dstate, 4) || !aligned(d_ds0, 4))
+    return op_fail(SIM_EINVAL, "%s: decays, lengths and states must be aligned to their type", who);
+  if ((rc = check_work(d_work, work_bytes, attn_work_bytes(*s, true), who))) return rc;
+  if (s->B == 0 || ((!some || s->T == 0) && !d_ds0)) return SIM_OK;
+  a.decay = d_decay; a.len = d_len; a.s0 = d_s0; a.ds = d_dstate; a.state = d_ds0; a.work = d_work;
+  const OpCtx o = op_ctx(x);
+  a.err = o.err;
+  return on_ctx(x, SIM_KC_GAE, who, [&] { return launch_attn(a, true, o.stream); });
+}
+
+int token_logprobs_work(const sim_logprobs* c, size_t* bytes) {
+  int rc = check_logprobs(c, "token_logprobs_work");
+  if (rc) return rc;
+  if (!bytes) return op_fail(SIM_EINVAL, "token_logprobs_work: bytes is NULL");
+  *bytes = logprob_bytes(*c, false);
+  return SIM_OK;
+}
+
+int token_logprobs(sim_ctx* x, const sim_logprobs* c, const sim_mat* logits, const sim_mat* mask,
+                   const void* d_tokens, const uint8_t* d_live, float* d_logp, float* d_entropy,
+                   int64_t* d_top_index, float* d_top_logp, void* d_work, size_t work_bytes) {
+  const char* who = "token_logprobs";
+  if (!x) return op_fail(SIM_EINVAL, "%s: ctx is NULL", who);
+  int rc = check_logprobs(c, who);
+  if (rc) return rc;
+  LogprobArgs a{};
+  a.c = *c;
+  if ((rc = check_logits(c->N, c->A, c->dtype, logits, nullptr, who, &a.l, &a.grad))) return rc;
+  if (mask && mask->data) {
+    if ((rc = check_mat(c->N, c->A, mask, 1, false, false, who, "mask"))) return rc;
+    a.mask = *mask;
+  }
+  if (c->N > 0 && d_logp && !d_tokens) return op_fail(SIM_EINVAL, "%s: logp needs tokens", who);
+  if (!aligned(d_tokens, int_bytes(c->token_type)) || !aligned(d_logp, 4) || !aligned(d_entropy, 4) ||
+      !aligned(d_top_index, 8) || !aligned(d_top_logp, 4))
+    return op_fail(SIM_EINVAL, "%s: an array is not aligned to its type", who);
+  if ((rc = check_work(d_work, work_bytes, logprob_bytes(*c, false), who))) return rc;
+  a.tokens = d_tokens; a.live = d_live; a.logp = d_logp; a.entropy = d_entropy;
+  if (c->top) { a.top_index = d_top_index; a.top_logp = d_top_logp; }
+  if (c->N == 0 || (!a.logp && !a.entropy && !a.top_index && !a.top_logp)) return SIM_OK;
+  a.work = d_work;
+  const OpCtx o = op_ctx(x);
+  a.err = o.err;
+  return on_ctx(x, SIM_KC_PPO, who, [&] { return launch_logprobs(a, o.stream); });
+}
+
+int token_logprobs_grad_work(const sim_logprobs* c, size_t* bytes) {
+  int rc = check_logprobs(c, "token_logprobs_grad_work");
+  if (rc) return rc;
+  if (!bytes) return op_fail(SIM_EINVAL, "token_logprobs_grad_work: bytes is NULL");
+  *bytes = logprob_bytes(*c, true);
+  return SIM_OK;
+}
+
+int token_logprobs_grad(sim_ctx* x, const sim_logprobs* c, const sim_mat* logits, const sim_mat* mask,
+                        const void* d_tokens, const uint8_t* d_live, const float* d_dlogp,
+                        const float* d_dentropy, const sim_mat* grad, void* d_work, size_t work_bytes) {
+  const char* who = "token_logprobs_grad";
+  if (!x) return op_fail(SIM_EINVAL, "%s: ctx is NULL", who);
+  int rc = check_logprobs(c, who);
+  if (rc) return rc;
+  LogprobArgs a{};
+  a.c = *c;
+  if ((rc = check_logits(c->N, c->A, c->dtype, logits, grad, who, &a.l, &a.grad))) return rc;
+  if (mask && mask->data) {
+    if ((rc = check_mat(c->N, c->A, mask, 1, false, false, who, "mask"))) return rc;
+    a.mask = *mask;
+  }
+  if (c->N > 0 && !a.grad.data) return op_fail(SIM_EINVAL, "%s: grad is NULL", who);
+  if (c->N > 0 && d_dlogp && !d_tokens) return op_fail(SIM_EINVAL, "%s: dlogp needs tokens", who);
+  if (!aligned(d_tokens, int_bytes(c->token_type)) || !aligned(d_dlogp, 4) || !aligned(d_dentropy, 4))
+    return op_fail(SIM_EINVAL, "%s: an array is not aligned to its type", who);
+  if ((rc = check_work(d_work, work_bytes, logprob_bytes(*c, true), who))) return rc;
+  if (c->N == 0) return SIM_OK;
+  a.tokens = d_tokens; a.live = d_live; a.dlogp = d_dlogp; a.dentropy = d_dentropy; a.work = d_work;
+  const OpCtx o = op_ctx(x);
+  a.err = o.err;
+  return on_ctx(x, SIM_KC_PPO, who, [&] { return launch_logprobs(a, o.stream); });
+}
+
+int orthogonalize_work(const sim_ortho* c, size_t* bytes) {
+  int rc = check_ortho(c, "orthogonalize_work");
+  if (rc) return rc;
+  if (!bytes) return op_fail(SIM_EINVAL, "orthogonalize_work: bytes is NULL");
+  *bytes = ortho_bytes(*c);
+  return SIM_OK;
+}
+
+int orthogonalize(sim_ctx* x, const sim_ortho* c, const sim_mats* update, const sim_mats* out, void* d_work,
+                  size_t work_bytes) {
+  const char* who = "orthogonalize";
+  if (!x) return op_fail(SIM_EINVAL, "%s: ctx is NULL", who);
+  int rc = check_ortho(c, who);
+  if (rc) return rc;
+  OrthoArgs a{};
+  a.c = *c;
+  if (c->n && c->M && c->N) {
+    const sim_mats* both[2] = {update, out};
+    for (int i = 0; i < 2; ++i) {
+      const char* name = i ? "out" : "update";
+      if (!both[i] || !both[i]->data) return op_fail(SIM_EINVAL, "%s: %s is NULL", who, name);
+      const Dim dims[3] = {{both[i]->stride_i, c->n}, {both[i]->stride_r, c->M}, {both[i]->stride_c, c->N}};
+      if ((rc = check_box(both[i]->data, dims, 1, elem_bytes(c->dtype), i, who, name))) return rc;
+    }
+    a.u = *update;
+    a.out = *out;
+  }
+  if ((rc = check_work(d_work, work_bytes, ortho_bytes(*c), who))) return rc;
+  if (!a.u.data) return SIM_OK;
+  a.work = d_work;
+  const OpCtx o = op_ctx(x);
+  return on_ctx(x, SIM_KC_PPO, who, [&] { return launch_ortho(a, o.stream); });
 }
 
 }  // extern "C"

@@ -1379,11 +1379,12 @@ int sim_sync(sim_ctx* x) {
   HIPCHK(hipMemcpy(&err, x->s.err, 4, hipMemcpyDeviceToHost), "copy error flags");
   if (err) {
     HIPCHK(hipMemset(x->s.err, 0, 4), "clear error flags");
-    return fail(SIM_ESTATE, "device error flags 0x%x:%s%s%s%s", err,
+    return fail(SIM_ESTATE, "device error flags 0x%x:%s%s%s%s%s", err,
                 (err & ERR_ACTION) ? " action out of range;" : "",
                 (err & ERR_EVENTS) ? " event bound exceeded in a tick;" : "",
                 (err & ERR_TRACE) ? " trace overrun;" : "",
-                (err & ERR_LENGTH) ? " sequence length out of range;" : "");
+                (err & ERR_LENGTH) ? " sequence length out of range;" : "",
+                (err & ERR_DECAY) ? " decay out of range;" : "");
   }
   return SIM_OK;
 }

@@ -36,6 +36,16 @@ def _seq(t):
     return C.byref(L.SimSeq(t.data_ptr(), sb, st))
 
 
+def _heads(t):
+    """sim_heads of a [B][T][H][D] tensor (None: absent)."""
+    if t is None:
+        return None
+    sb, st, sh, sd = t.stride()
+    if sd != 1 and t.shape[3] > 1:
+        raise ValueError("channels (the last dimension) must be adjacent in memory")
+    return C.byref(L.SimHeads(t.data_ptr(), sb, st, sh))
+
+
 def _mat(t):
     return None if t is None else C.byref(L.SimMat(t.data_ptr(), *t.stride()))
 
@@ -497,6 +507,125 @@ class Sim:
         self._call("balance_loss", sizes, _mat(logits), _a(index), _a(live), _mat(grad), _a(counts),
                    _a(loss))
         return dict(loss=loss, counts=counts, grad=grad)
+
+    def _attn_sizes(self, q, k, v, decay, s0, lengths, scale):
+        """Checks of what linear_attn and its gradient share; (sizes, B, T, H, Dk, Dv)."""
+        if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+            raise ValueError("q, k and v have shape [B][T][heads][channels]")
+        B, T, H, Dk = q.shape
+        Hk, Dv = v.shape[2:]
+        self._check("q", q, (B, T, H, Dk), (torch.float32, torch.bfloat16, torch.float16))
+        self._check("k", k, (B, T, Hk, Dk), (q.dtype,))
+        self._check("v", v, (B, T, Hk, Dv), (q.dtype,))
+        self._flat("decay", decay, (H,), (torch.float32,))
+        self._flat("s0", s0, (B, H, Dk, Dv), (torch.float32,))
+        self._flat("lengths", lengths, (B,), (torch.int32,))
+        return L.SimLinearAttn(B, T, H, Hk, Dk, Dv, _FLOAT[q.dtype], scale), B, T, H, Dk, Dv
+
+    def linear_attn(self, q, k, v, decay, s0=None, lengths=None, scale=1.0, y=None, state=None,
+                    want_y=True):
+        """Linear attention with a decay for each head: per head, from the state s0 [B][H][Dk][Dv]
+        (fp32; default 0), S = decay S + k_t v_t^T and y_t = scale S^T q_t over q [B][T][H][Dk], k
+        [B][T][Hk][Dk] and v [B][T][Hk][Dv] (Hk divides H: consecutive heads share keys and values),
+        decay [H] fp32 in [0, 1]. lengths [B] int32: later steps are padding. Returns (y [B][T][H][Dv]
+        in the inputs' type, None unless want_y; the last state, which may be written over s0:
+        state=s0, as for one token after another while serving)."""
+        sizes, B, T, H, Dk, Dv = self._attn_sizes(q, k, v, decay, s0, lengths, scale)
+        if y is not None:
+            self._check("y", y, (B, T, H, Dv), (q.dtype,))
+        elif want_y:
+            y = q.new_empty((B, T, H, Dv))
+        if state is None:
+            state = q.new_empty((B, H, Dk, Dv), dtype=torch.float32)
+        else:
+            self._flat("state", state, (B, H, Dk, Dv), (torch.float32,))
+        self._call("linear_attn", sizes, _heads(q), _heads(k), _heads(v), _a(decay), _a(lengths),
+                   _a(s0), _heads(y), _a(state))
+        return y, state
+
+    def linear_attn_grad(self, q, k, v, decay, dy, s0=None, dstate=None, lengths=None, scale=1.0,
+                         dq=None, dk=None, dv=None, ds0=None):
+        """Gradient of linear_attn: dy [B][T][H][Dv], dstate [B][H][Dk][Dv] the gradient of its last
+        state. Returns (dq, dk, dv, ds0) of the inputs' shapes (shared heads' gradients are summed; sum
+        over other dimensions that an input was broadcast along). The decays are constants."""
+        sizes, B, T, H, Dk, Dv = self._attn_sizes(q, k, v, decay, s0, lengths, scale)
+        self._check("dy", dy, (B, T, H, Dv), (q.dtype,))
+        self._flat("dstate", dstate, (B, H, Dk, Dv), (torch.float32,))
+        out = []
+        for name, t, like in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
+            if t is None:
+                t = q.new_empty(like.shape)
+            else:
+                self._check(name, t, like.shape, (q.dtype,))
+            out.append(t)
+        if ds0 is None:
+            ds0 = q.new_empty((B, H, Dk, Dv), dtype=torch.float32)
+        else:
+            self._flat("ds0", ds0, (B, H, Dk, Dv), (torch.float32,))
+        self._call("linear_attn_grad", sizes, _heads(q), _heads(k), _heads(v), _a(decay), _heads(dy),
+                   _a(lengths), _a(s0), _a(dstate), *map(_heads, out), _a(ds0))
+        return (*out, ds0)
+
+    def _logprob_sizes(self, logits, tokens, mask, live, top):
+        N, A = logits.shape
+        self._check("logits", logits, (N, A), (torch.float32, torch.bfloat16, torch.float16))
+        self._flat("tokens", tokens, (N,), _INT)
+        if mask is not None:
+            self._check("mask", mask, (N, A), (torch.bool, torch.uint8))
+        self._flat("live", live, (N,), (torch.bool, torch.uint8))
+        return L.SimLogprobs(N, A, top, _FLOAT[logits.dtype],
+                             _INT[torch.int64 if tokens is None else tokens.dtype])
+
+    def token_logprobs(self, logits, tokens=None, mask=None, live=None, top=0):
+        """Log-probabilities of given tokens (or actions) [N] uint8, int32 or int64 (-1: none) over logits
+        [N][A] of any network, in either layout of policy_loss, the entropies and the `top` likeliest
+        columns (up to 64), of equal ones the lowest first. mask [N][A] bool or uint8 (0 forbids), live
+        [N] bool or uint8 (the other rows are padding and give zeros). Returns dict(logp [N] (None
+        without tokens), entropy [N], top_index [N][top] int64, top_logp [N][top]; where a row allows
+        fewer columns the rest is -1 and -inf)."""
+        sizes = self._logprob_sizes(logits, tokens, mask, live, top)
+        N = logits.shape[0]
+        entropy = logits.new_empty(N, dtype=torch.float32)
+        logp = None if tokens is None else torch.empty_like(entropy)
+        index = logits.new_empty((N, max(0, top)), dtype=torch.int64)
+        tlogp = logits.new_empty((N, max(0, top)), dtype=torch.float32)
+        self._call("token_logprobs", sizes, _mat(logits), _mat(mask), _a(tokens), _a(live), _a(logp),
+                   _a(entropy), _a(index), _a(tlogp))
+        return dict(logp=logp, entropy=entropy, top_index=index, top_logp=tlogp)
+
+    def token_logprobs_grad(self, logits, tokens=None, dlogp=None, dentropy=None, mask=None, live=None,
+                            grad=None):
+        """Gradient over the logits of sum(dlogp * logp + dentropy * entropy) of token_logprobs, dlogp and
+        dentropy [N] fp32 (default 0). Returns it [N][A] in the logits' type; it may be the logits
+        themselves (grad=logits)."""
+        sizes = self._logprob_sizes(logits, tokens, mask, live, 0)
+        for name, t in (("dlogp", dlogp), ("dentropy", dentropy)):
+            self._flat(name, t, (logits.shape[0],), (torch.float32,))
+        grad = self._grad_like(logits, grad, True)
+        self._call("token_logprobs_grad", sizes, _mat(logits), _mat(mask), _a(tokens), _a(live),
+                   _a(dlogp), _a(dentropy), _mat(grad))
+        return grad
+
+    def orthogonalize(self, update, steps=5, coeffs=(3.4445, -4.7750, 2.0315), eps=1e-7, scale=1.0,
+                      out=None):
+        """An update of a matrix [M][N], or of n of one shape [n][M][N], orthogonalised by Newton-Schulz
+        products: X = update / (its norm + eps), then `steps` times X = a X + (b A + c A A) X with A = X
+        X^T, and scale X is returned (or written to out, which may be the update itself). Any strides;
+        fp32, bf16 or fp16."""
+        one = update.dim() == 2
+        u, o = (t[None] if one and t is not None else t for t in (update, out))
+        if u.dim() != 3:
+            raise ValueError("update has shape [M][N] or [n][M][N]")
+        self._check("update", u, u.shape, (torch.float32, torch.bfloat16, torch.float16))
+        if o is None:
+            o = u.new_empty(u.shape)
+        else:
+            self._check("out", o, u.shape, (u.dtype,))
+        a, b, c = coeffs
+        sizes = L.SimOrtho(*u.shape, steps, _FLOAT[u.dtype], a, b, c, eps, scale)
+        self._call("orthogonalize", sizes, C.byref(L.SimMats(u.data_ptr(), *u.stride())),
+                   C.byref(L.SimMats(o.data_ptr(), *o.stride())))
+        return o[0] if one else o
 
     def params_from_weights(self, weights):
         p = torch.empty(self.ppo_grad_count(), dtype=torch.float32, device=self.device)
