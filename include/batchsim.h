@@ -551,7 +551,7 @@ typedef struct sim_heads {
 
 /*  B, T    sequences, steps (below 2^30)
  *  H, Hk   heads of q and y, heads of k and v: Hk divides H, and heads [i H/Hk, (i+1) H/Hk) share
- *          the keys and values i (B H below 2^24, B T H below 2^40)
+ *          the keys and values i (B H below 2^22, B T H below 2^40)
  *  Dk, Dv  channels of q and k, of v and y: 1 to 256 each
  *  dtype   of q, k, v, y and their gradients (not SIM_DT_F64); states are fp32
  *  scale   finite                                                                         */
@@ -570,9 +570,10 @@ typedef struct sim_linear_attn {
  * their y is 0; a length outside [0, T] latches SIM_ESTATE and is taken as the nearer bound, and so
  * does a decay outside [0, 1] (NaN as 0).
  * Up to T = 16 steps are taken one after another. With more, a run of steps is taken at once: the
- * products q_t k_s, weighted by l^(t-s), and the state between runs are held in fp32 and multiplied as
- * bf16 parts that add up to them (two for 16-bit types, 16 bits of the value; three for fp32, all 24), so
- * they must be finite in fp32, and results differ from a step-by-step sum by rounding. */
+ * products q_t k_s, weighted by l^(t-s), and the state between runs are held in fp32 and multiplied, for y
+ * alone, as bf16 parts that add up to them (two for 16-bit types, 16 bits of the value; three for fp32, all
+ * 24), so they must be finite in fp32, and results differ from a step-by-step sum by rounding. An infinity or
+ * NaN in v_t (of a live step) reaches y from the start of its run on, up to 63 steps before t. */
 int linear_attn_work(const sim_linear_attn* s, size_t* bytes);
 int linear_attn(sim_ctx* ctx, const sim_linear_attn* s, const sim_heads* q, const sim_heads* k,
                 const sim_heads* v, const float* d_decay, const int32_t* d_len, const float* d_s0,

@@ -8,6 +8,7 @@
 //   dk  (v, dy, q) backwards from dS^T, su = scale, lag = 1
 //   dv  (k, q, dy) backwards from dS, su = scale, lag = 1, whose last state is dS0
 #include <algorithm>
+#include <atomic>
 
 #include "ops_dev.hpp"
 
@@ -32,6 +33,9 @@ struct AttnRun {
   int H, Dq, Dv, lag;
   bool back, wide;      // steps from the last to the first; out in fp32
   float so, su;
+  float* parts;         // states before (after attn_join_k) or of the segments that time is split into
+  int64_t seg;          // steps of a segment
+  int segs;
 };
 
 __device__ __forceinline__ float decay_of(const AttnRun& r, int h) {
@@ -158,6 +162,417 @@ __global__ __launch_bounds__(kStep) void attn_step_k(AttnRun r) {
   }
 }
 
+// ---- runs of steps by matrix instructions ----------------------------------------------------------
+// C steps at once:  out = so (l^(i+1-lag) Q S + (Q K^T o su l^(i-j) [j <= i]) V),  S = l^m S + K^T (su l^(m-1-j+lag) V)
+// for m live ones. Values are bf16 parts that add up to them: NI of an input (bf16 1, fp16 2, fp32 3: exact), NC of
+// what is multiplied again on the way to out (the weighted products, S: 2 for 16-bit types, whose outputs are rounded
+// to fewer bits, 3 for fp32), and 3 of the weighted V, which S, an fp32 output held in the accumulators, is made of. A product of parts
+// i and j is left out where i + j reaches the larger of the counts: it is below the last bits that are kept.
+template <class E> struct PartsOf;
+template <> struct PartsOf<BF16> { static constexpr int kIn = 1, kMade = 2; };
+template <> struct PartsOf<F16> { static constexpr int kIn = 2, kMade = 2; };
+template <> struct PartsOf<F32> { static constexpr int kIn = 3, kMade = 3; };
+
+typedef __bf16 Bf8 __attribute__((ext_vector_type(8)));
+typedef __bf16 Bf4 __attribute__((ext_vector_type(4)));
+typedef float Fl4 __attribute__((ext_vector_type(4)));
+
+// the parts of values, an even number of them (two conversions are one instruction)
+template <int N, int W>
+__device__ __forceinline__ void split(const float (&x)[W], __bf16 (&p)[N][W]) {
+  typedef float F2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 B2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int w = 0; w < W; w += 2) {
+    F2 rest = {x[w], x[w + 1]};
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const B2 h = __builtin_convertvector(rest, B2);
+      p[i][w] = h[0];
+      p[i][w + 1] = h[1];
+      if (i + 1 < N) rest -= __builtin_convertvector(h, F2);
+    }
+  }
+}
+template <int W>
+__device__ __forceinline__ auto packed(const __bf16 (&p)[W]) {
+  typedef __bf16 B __attribute__((ext_vector_type(W)));
+  B v;
+#pragma unroll
+  for (int w = 0; w < W; ++w) v[w] = p[w];
+  return v;
+}
+// c += a b, as far as the parts' products count
+template <int NA, int NB>
+__device__ __forceinline__ void mul_parts(const Bf8 (&a)[NA], const Bf8 (&b)[NB], Fl4& c) {
+  constexpr int most = NA > NB ? NA : NB;
+#pragma unroll
+  for (int i = 0; i < NA; ++i) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+      if (i + j < most) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], c, 0, 0, 0);
+  }
+}
+// Of a matrix in LDS, four rows by 16 columns per 16 lanes, turned: lane i gets column i. p: this lane's place, row
+// i / 4 and column 4 (i % 4).
+__device__ __forceinline__ Bf4 read_turned(const __bf16* p) {
+  typedef short S4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) S4 L4;
+  return __builtin_bit_cast(Bf4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((L4*)(p)));
+}
+__device__ __forceinline__ Bf8 both(Bf4 a, Bf4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+
+constexpr int kPad = 8;   // rows of LDS start four banks apart
+template <class E, int DQ, int NW, int C>
+struct RunLds {
+  static constexpr int NI = PartsOf<E>::kIn, NC = PartsOf<E>::kMade, DV = 16 * NW;
+  __bf16 q[NI][C][DQ + kPad], k[NI][C][DQ + kPad], v[NI][C][DV + kPad], p[NC][C][C + kPad];
+  float pow[C + 1], into[C];   // su l^i; su l^(m-1-j+lag)
+};
+
+// eight elements of a row from p on, of which `have` are there; zeros past its end
+template <class T>
+struct Eight {
+  typedef T Raw __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+  typedef T Val __attribute__((ext_vector_type(8)));
+  Val v;
+  __device__ __forceinline__ void load(const T* p) { v = __builtin_bit_cast(Val, *reinterpret_cast<const Raw*>(p)); }
+  __device__ __forceinline__ void load(const T* p, int have) {
+    if (have >= 8) {
+      load(p);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i < have ? p[i] : (T)0.0f;
+    }
+  }
+};
+
+// a run of C steps of one array, D columns, in registers between global memory and LDS: a thread's units of eight
+// are kRows steps apart
+template <class E, int D, int C, int NT>
+struct Tile {
+  typedef typename E::T T;
+  static constexpr int kUnits = C * D / 8, N = kUnits / NT, NI = PartsOf<E>::kIn, kRows = NT * 8 / D;
+  static_assert(kUnits % NT == 0 && NT * 8 % D == 0, "whole units");
+  Eight<T> u[N];
+  const T* p;
+  int64_t step;   // from one step to the next
+  int row, have;
+  // the next run starts at step i of the processing order; the array's columns from c0 on, `width` of them
+  __device__ __forceinline__ void start(const AttnRun& r, const In& x, int b, int h, int64_t i, int64_t n, int c0, int width) {
+    const int c = threadIdx.x % (D / 8) * 8;
+    row = threadIdx.x / (D / 8);
+    have = width - c;
+    step = r.back ? -x.st : x.st;
+    p = row_of<T>(x, b, r.back ? n - 1 - i : i, h) + c0 + c + row * step;
+  }
+  template <bool WHOLE>
+  __device__ __forceinline__ void fetch(int now) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const T* at = p + j * kRows * step;
+      if (WHOLE) {
+        u[j].load(at);
+      } else {
+        u[j].v = typename Eight<T>::Val{};
+        if (row + j * kRows < now && have > 0) u[j].load(at, have);
+      }
+    }
+    p += C * step;
+  }
+  template <int S>
+  __device__ __forceinline__ void store(__bf16 (*lds)[C][S]) const {
+    const int c = threadIdx.x % (D / 8) * 8;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if constexpr (NI == 1) {
+        *reinterpret_cast<typename Eight<T>::Val*>(&lds[0][row + j * kRows][c]) = u[j].v;
+      } else {
+        float x[8];
+        __bf16 w[NI][8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (float)u[j].v[e];
+        split(x, w);
+#pragma unroll
+        for (int q = 0; q < NI; ++q) *reinterpret_cast<Bf8*>(&lds[q][row + j * kRows][c]) = packed(w[q]);
+      }
+    }
+  }
+};
+
+// A workgroup takes a segment of a sequence and head and 16 columns of its state per wave, which hold them as
+// accumulators (lane: column lane % 16, rows 4 (lane / 16) + 0..3 of each tile of 16), so that two tiles are an operand
+// of the next product as they are. While a run is multiplied the next one's loads fly.
+template <class E, int DQ, int NW, int C, bool OUT>
+__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void attn_run_k(AttnRun r) {
+  typedef typename E::T T;
+  typedef RunLds<E, DQ, NW, C> Lds;
+  constexpr int NI = Lds::NI, NC = Lds::NC, DV = Lds::DV, KT = DQ / 16, TT = C / 16, NT = 64 * NW;
+  extern __shared__ __align__(16) char raw[];
+  Lds& m = *reinterpret_cast<Lds*>(raw);
+  const int lane = threadIdx.x & 63, lc = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // the same in all of a wave's lanes
+  const int cols = (r.Dv + DV - 1) / DV;
+  const int seg = blockIdx.y, c0 = blockIdx.x % cols * DV, bh = blockIdx.x / cols, h = bh % r.H, b = bh / r.H;
+  const float l = decay_of(r, h);
+  const int64_t n = steps_of(r, b), first = seg * r.seg, last = first + r.seg < r.T ? first + r.seg : r.T;
+  const int64_t live = n < last ? n : last;   // of the segment's steps in processing order: [first, live)
+  const int width = r.Dv - c0 < DV ? r.Dv - c0 : DV;
+  const double log2l = log2((double)l);
+  auto power = [&](int i) { return i == 0 ? 1.0f : (float)exp2(i * log2l); };
+  Fl4 st[KT];
+  const bool split_time = r.segs > 1;
+  const float* s0 = split_time ? r.parts + ((int64_t)bh * r.segs + seg) * r.Dq * r.Dv
+                               : (r.s0 ? r.s0 + (int64_t)bh * r.Dq * r.Dv : nullptr);
+  const int64_t sr = split_time ? r.Dv : r.sr, sc = split_time ? 1 : r.sc;
+  if (!OUT && split_time) s0 = nullptr;
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) {
+    const int c = c0 + wave * 16 + lc;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = kt * 16 + 4 * lg + i;
+      st[kt][i] = s0 && row < r.Dq && c < r.Dv ? s0[row * sr + c * sc] : 0.0f;
+    }
+  }
+  if (threadIdx.x <= C) m.pow[threadIdx.x] = r.su * power(threadIdx.x);
+  float out_w[TT];   // so l^(t+1-lag) of this lane's step of each tile
+#pragma unroll
+  for (int t = 0; t < TT; ++t) out_w[t] = r.so * power(16 * t + lc + 1 - r.lag);
+  const float whole = power(C);
+  Tile<E, DQ, C, NT> q, k;
+  Tile<E, DV, C, NT> v;
+  if (OUT) q.start(r, r.q, b, h, first, n, 0, r.Dq);
+  k.start(r, r.k, b, h, first, n, 0, r.Dq);
+  v.start(r, r.v, b, h, first, n, c0, width);
+  const bool full = r.Dq == DQ && width == DV;
+  auto fetch = [&](int64_t left) {
+    either(full && left >= C, [&](auto W) {
+      constexpr bool WHOLE = decltype(W)::value;
+      const int now = left < C ? (int)left : C;
+      if (OUT) q.template fetch<WHOLE>(now);
+      k.template fetch<WHOLE>(now);
+      v.template fetch<WHOLE>(now);
+    });
+  };
+  const int64_t turn = r.back ? -r.ot : r.ot;   // of out, from one step to the next
+  int64_t at0 = b * r.ob + (r.back ? n - 1 - first : first) * r.ot + h * r.oh + c0 + lc * turn + wave * 16 + 4 * lg;
+  fetch(live - first);
+  for (int64_t i0 = first; i0 < live; i0 += C) {
+    const int now = live - i0 < C ? (int)(live - i0) : C;
+    __syncthreads();
+    if (OUT) q.store(m.q);
+    k.store(m.k);
+    v.store(m.v);
+    if (threadIdx.x < C) {
+      const int j = threadIdx.x;
+      m.into[j] = j < now ? m.pow[now - 1 - j + r.lag] : 0.0f;
+    }
+    __syncthreads();
+    if (i0 + C < live) fetch(live - i0 - C);
+    if constexpr (OUT) {
+      // weighted products, turned: rows j, columns i
+      constexpr int kPairs = TT * TT / 2 + TT / 2 + (TT / 2);   // tiles of j <= i, and those beside them in a step of 32
+      static_assert(TT % 2 == 0, "steps of 32");
+#pragma unroll
+      for (int w0 = 0; w0 < kPairs; w0 += NW) {
+        int at = w0 + wave, ti = 0;
+        // row of tiles ti has 2 (ti / 2 + 1) of them
+#pragma unroll
+        for (int x = 0; x < TT - 1; ++x) {
+          const int have = 2 * (x / 2 + 1);
+          if (ti == x && at >= have) { at -= have; ++ti; }
+        }
+        if (w0 + wave >= kPairs) continue;
+        const int tj = at;
+        Fl4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (tj <= ti) {
+#pragma unroll
+          for (int kk = 0; kk < DQ / 32; ++kk) {
+            Bf8 a[NI], x[NI];
+#pragma unroll
+            for (int p = 0; p < NI; ++p) {
+              a[p] = *reinterpret_cast<const Bf8*>(&m.k[p][16 * tj + lc][32 * kk + 8 * lg]);
+              x[p] = *reinterpret_cast<const Bf8*>(&m.q[p][16 * ti + lc][32 * kk + 8 * lg]);
+            }
+            mul_parts(a, x, acc);
+          }
+        }
+        float w[4];
+        __bf16 o[NC][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int gap = 16 * (ti - tj) + lc - (4 * lg + i);
+          w[i] = gap >= 0 ? acc[i] * (r.so * m.pow[gap < 0 ? 0 : gap]) : 0.0f;
+        }
+        split(w, o);
+#pragma unroll
+        for (int x = 0; x < NC; ++x) *reinterpret_cast<Bf4*>(&m.p[x][16 * ti + lc][16 * tj + 4 * lg]) = packed(o[x]);
+      }
+      // S^T Q^T, columns i
+      Fl4 acc[TT];
+#pragma unroll
+      for (int t = 0; t < TT; ++t) acc[t] = Fl4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int kk = 0; kk < DQ / 32; ++kk) {
+        Bf8 s[NC];
+        float w[8];
+        __bf16 p[NC][8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = st[2 * kk + i / 4][i % 4];
+        split(w, p);
+#pragma unroll
+        for (int x = 0; x < NC; ++x) s[x] = packed(p[x]);
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+          Bf8 x[NI];
+#pragma unroll
+          for (int p = 0; p < NI; ++p) {
+            const __bf16* row = &m.q[p][16 * t + lc][32 * kk + 4 * lg];
+            x[p] = both(*reinterpret_cast<const Bf4*>(row), *reinterpret_cast<const Bf4*>(row + 16));
+          }
+          mul_parts(s, x, acc[t]);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        acc[t] *= out_w[t];
+      }
+      __syncthreads();   // the weighted products are there
+#pragma unroll
+      for (int j = 0; j < C / 32; ++j) {
+        Bf8 a[NI];
+#pragma unroll
+        for (int p = 0; p < NI; ++p) {
+          const __bf16* at = &m.v[p][32 * j + 8 * lg + lc / 4][wave * 16 + 4 * (lc % 4)];
+          a[p] = both(read_turned(at), read_turned(at + 4 * (DV + kPad)));
+        }
+#pragma unroll
+        for (int t = 2 * j; t < TT; ++t) {
+          Bf8 x[NC];
+#pragma unroll
+          for (int p = 0; p < NC; ++p) x[p] = *reinterpret_cast<const Bf8*>(&m.p[p][16 * t + lc][32 * j + 8 * lg]);
+          mul_parts(a, x, acc[t]);
+        }
+      }
+      either(full && now == C && !r.wide, [&](auto W) {
+        constexpr bool WHOLE = decltype(W)::value;
+        typedef T Raw __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+        typedef T Val __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+          const int64_t at = at0 + 16 * t * turn;
+          const Fl4 y = acc[t];
+          if (WHOLE) {
+            *reinterpret_cast<Raw*>(static_cast<T*>(r.out) + at) = __builtin_bit_cast(Raw, __builtin_convertvector(y, Val));
+          } else if (16 * t + lc < now) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if (wave * 16 + 4 * lg + e >= width) continue;
+              if (r.wide) static_cast<float*>(r.out)[at + e] = y[e];
+              else static_cast<T*>(r.out)[at + e] = (T)y[e];
+            }
+          }
+        }
+      });
+      at0 += C * turn;
+    }
+    // S = l^m S + K^T V weighted
+    const float fade = now == C ? whole : power(now);
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+      st[kt] *= fade;
+    }
+#pragma unroll
+    for (int j = 0; j < C / 32; ++j) {
+      Bf8 x[3];
+      Bf8 a[NI];
+#pragma unroll
+      for (int p = 0; p < NI; ++p) {
+        const __bf16* at = &m.v[p][32 * j + 8 * lg + lc / 4][wave * 16 + 4 * (lc % 4)];
+        a[p] = both(read_turned(at), read_turned(at + 4 * (DV + kPad)));
+      }
+      float w[8];
+      __bf16 o[3][8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        w[i] = (float)a[0][i];
+#pragma unroll
+        for (int p = 1; p < NI; ++p) w[i] += (float)a[p][i];
+        w[i] *= m.into[32 * j + 8 * lg + i];
+      }
+      split(w, o);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) x[p] = packed(o[p]);
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        Bf8 a[NI];
+#pragma unroll
+        for (int p = 0; p < NI; ++p) {
+          const __bf16* at = &m.k[p][32 * j + 8 * lg + lc / 4][16 * kt + 4 * (lc % 4)];
+          a[p] = both(read_turned(at), read_turned(at + 4 * (DQ + kPad)));
+        }
+        mul_parts(a, x, st[kt]);
+      }
+    }
+  }
+  if (OUT) {   // padding
+    const int c = threadIdx.x % (DV / 8) * 8, row = threadIdx.x / (DV / 8);
+    for (int64_t i = (live > first ? live : first) + row; i < last; i += NT * 8 / DV) {
+      const int64_t at = b * r.ob + i * r.ot + h * r.oh + c0 + c;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (c + e >= width) continue;
+        if (r.wide) static_cast<float*>(r.out)[at + e] = 0.0f;
+        else static_cast<T*>(r.out)[at + e] = (T)0.0f;
+      }
+    }
+  }
+  float* to = OUT ? (split_time || !r.state ? nullptr : r.state + (int64_t)bh * r.Dq * r.Dv)
+                  : (split_time ? r.parts + ((int64_t)bh * r.segs + seg) * r.Dq * r.Dv : r.state + (int64_t)bh * r.Dq * r.Dv);
+  if (!to) return;
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) {
+    const int c = c0 + wave * 16 + lc;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = kt * 16 + 4 * lg + i;
+      if (row < r.Dq && c < r.Dv) to[row * sr + c * sc] = st[kt][i];
+    }
+  }
+}
+
+// The segments' own last states become the states that they start from: an element of the state a thread.
+__global__ __launch_bounds__(256) void attn_join_k(AttnRun r) {
+  const int h = blockIdx.y % r.H, b = blockIdx.y / r.H;
+  const int cells = r.Dq * r.Dv, i = blockIdx.x * 256 + threadIdx.x;
+  float l = r.decay[h];
+  l = l >= 0.0f ? (l > 1.0f ? 1.0f : l) : 0.0f;
+  int64_t n = r.len ? r.len[b] : r.T;
+  n = n < 0 ? 0 : (n > r.T ? r.T : n);
+  if (i >= cells) return;
+  const int64_t at = (int64_t)blockIdx.y * cells + i / r.Dv * r.sr + i % r.Dv * r.sc;
+  float s = r.s0 ? r.s0[at] : 0.0f;
+  const double log2l = log2((double)l);
+  const float whole = (float)exp2((double)r.seg * log2l);
+  float* p = r.parts + (int64_t)blockIdx.y * r.segs * cells + i;
+  constexpr int kAhead = 16;   // loads that fly together
+  for (int g0 = 0; g0 < r.segs; g0 += kAhead) {
+    float own[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (g0 + u < r.segs) own[u] = p[(int64_t)(g0 + u) * cells];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (g0 + u >= r.segs) continue;
+      p[(int64_t)(g0 + u) * cells] = s;
+      const int64_t left = n - (g0 + u) * r.seg;
+      if (left > 0) s = fmaf(left >= r.seg ? whole : (float)exp2((double)left * log2l), s, own[u]);
+    }
+  }
+  if (r.state) r.state[at] = s;
+}
+
 // Gradients of shared keys and values: the sum over the heads that share them, in order.
 template <class E>
 __global__ __launch_bounds__(256) void attn_share_k(const float* w, sim_heads o, int64_t cells, int64_t T, int Hk,
@@ -172,29 +587,99 @@ __global__ __launch_bounds__(256) void attn_share_k(const float* w, sim_heads o,
   }
 }
 
+// Steps one after another up to kFew of them, by runs beyond.
+constexpr int kFew = 16;
+constexpr int run_steps(int dtype, int DQ) {   // of a run: as many as LDS holds of q, k, v and the products
+  return (dtype == SIM_DT_F32 && DQ > 64) || (dtype == SIM_DT_F16 && DQ > 128) ? 32 : 64;
+}
+// Columns of a state per workgroup: 128 where two workgroups of 64 do not share a CU (their registers or LDS) or there are
+// enough sequences and heads for both; 64 otherwise, q and k read twice from L2 (bf16 8 x 2048 x 16 x 128: 64 132 us, 128
+// 147; 2 x 2048 x 16 x 256: 293, 184; fp16 4 x 2048 x 16 x 128: 178, 130).
+int run_columns(int dtype, int64_t B, int H, int Dq, int Dv) {
+  return Dv <= 64 || (Dq <= 128 && dtype != SIM_DT_F16 && B * H < 512) ? 64 : 128;
+}
+// Time is split where workgroups are few, at the cost of reading k and v once more: below kSplit of them, into kFill segments
+// (fp32 16 x 385 x 6 x 80, 192 workgroups: whole 263 us, in two 317; bf16 1 x 32768 x 8 x 64 training step: 256 segments
+// 310, 512 258, 1024 328)
+constexpr int kSplit = 128, kFill = 512, kLeast = 256;
+int segments(int dtype, int64_t B, int64_t T, int H, int Dq, int Dv) {
+  const int wide = run_columns(dtype, B, H, Dq, Dv);
+  const int64_t groups = B * H * ((Dv + wide - 1) / wide);
+  if (T <= kFew || groups >= kSplit || groups == 0) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>((T + kLeast - 1) / kLeast, (kFill + groups - 1) / groups));
+}
+size_t parts_bytes(int dtype, int64_t B, int64_t T, int H, int Dq, int Dv) {
+  const int g = segments(dtype, B, T, H, Dq, Dv);
+  return g > 1 ? (size_t)B * H * g * Dq * Dv * sizeof(float) : 0;
+}
+
+template <class E, int DQ, int NW, int C>
+hipError_t launch_runs(AttnRun r, int64_t B, hipStream_t st) {
+  typedef RunLds<E, DQ, NW, C> Lds;
+  static std::atomic<uint64_t> done[2];
+  hipError_t e = allow_lds(reinterpret_cast<const void*>(&attn_run_k<E, DQ, NW, C, true>), sizeof(Lds), done[0]);
+  if (e == hipSuccess) e = allow_lds(reinterpret_cast<const void*>(&attn_run_k<E, DQ, NW, C, false>), sizeof(Lds), done[1]);
+  if (e != hipSuccess) return e;
+  const int cols = (r.Dv + Lds::DV - 1) / Lds::DV;
+  const dim3 grid((unsigned)(B * r.H * cols), r.segs), block(64 * NW);
+  if (r.segs > 1) {
+    hipLaunchKernelGGL((attn_run_k<E, DQ, NW, C, false>), grid, block, sizeof(Lds), st, r);
+    hipLaunchKernelGGL(attn_join_k, dim3((r.Dq * r.Dv + 255) / 256, (unsigned)(B * r.H)), dim3(256), 0, st, r);
+    r.err = nullptr;
+    if (!r.out) return hipSuccess;
+  }
+  if (r.out) hipLaunchKernelGGL((attn_run_k<E, DQ, NW, C, true>), grid, block, sizeof(Lds), st, r);
+  else hipLaunchKernelGGL((attn_run_k<E, DQ, NW, C, false>), grid, block, sizeof(Lds), st, r);
+  return hipSuccess;
+}
+
 template <class E>
-void launch_run(const AttnRun& r, int64_t B, hipStream_t st) {
-  const dim3 grid((unsigned)(B * r.H), (r.Dv + 63) / 64), block(kStep);
-  if (r.Dq <= 64) hipLaunchKernelGGL((attn_step_k<E, 4>), grid, block, 0, st, r);
-  else if (r.Dq <= 128) hipLaunchKernelGGL((attn_step_k<E, 8>), grid, block, 0, st, r);
-  else hipLaunchKernelGGL((attn_step_k<E, 16>), grid, block, 0, st, r);
+hipError_t launch_run(AttnRun r, int64_t B, float* parts, hipStream_t st) {
+  constexpr int dt = std::is_same<E, F32>::value ? SIM_DT_F32 : (std::is_same<E, F16>::value ? SIM_DT_F16 : SIM_DT_BF16);
+  if (r.T <= kFew) {
+    const dim3 grid((unsigned)(B * r.H), (r.Dv + 63) / 64), block(kStep);
+    if (r.Dq <= 64) hipLaunchKernelGGL((attn_step_k<E, 4>), grid, block, 0, st, r);
+    else if (r.Dq <= 128) hipLaunchKernelGGL((attn_step_k<E, 8>), grid, block, 0, st, r);
+    else hipLaunchKernelGGL((attn_step_k<E, 16>), grid, block, 0, st, r);
+    return hipSuccess;
+  }
+  r.segs = segments(dt, B, r.T, r.H, r.Dq, r.Dv);
+  r.seg = r.T;
+  if (r.segs > 1) {   // whole runs
+    const int64_t each = (r.T + r.segs - 1) / r.segs;
+    r.seg = (each + 63) / 64 * 64;
+    r.segs = (int)((r.T + r.seg - 1) / r.seg);
+    r.parts = parts;
+  }
+  const bool wide = run_columns(dt, B, r.H, r.Dq, r.Dv) == 128;
+  if (r.Dq > 128) return wide ? launch_runs<E, 256, 8, run_steps(dt, 256)>(r, B, st) : launch_runs<E, 256, 4, run_steps(dt, 256)>(r, B, st);
+  if (r.Dq > 64) return wide ? launch_runs<E, 128, 8, run_steps(dt, 128)>(r, B, st) : launch_runs<E, 128, 4, run_steps(dt, 128)>(r, B, st);
+  return wide ? launch_runs<E, 64, 8, run_steps(dt, 64)>(r, B, st) : launch_runs<E, 64, 4, run_steps(dt, 64)>(r, B, st);
 }
 
 In in_of(const sim_heads& x, int share) { return In{x.data, x.stride_b, x.stride_t, x.stride_h, share}; }
 
+// fp32 gradients of shared heads before they are added up
+size_t share_cells(const sim_linear_attn& c, bool grad) {
+  return grad && c.H > c.Hk ? ((size_t)c.B * c.T * c.H * std::max(c.Dk, c.Dv) + 3) / 4 * 4 : 0;
+}
+
 template <class E>
-void launch_typed(const AttnArgs& a, bool grad, hipStream_t st) {
+hipError_t launch_typed(const AttnArgs& a, bool grad, hipStream_t st) {
   const sim_linear_attn& c = a.c;
   const int g = c.H / c.Hk;
   AttnRun f{};
   f.decay = a.decay; f.len = a.len; f.err = a.err; f.T = c.T; f.H = c.H;
+  f.segs = 1; f.seg = c.T;
   const In q = in_of(a.q, 1), k = in_of(a.k, g), v = in_of(a.v, g), dy = in_of(a.dy, 1);
+  float* const shares = static_cast<float*>(a.work);
+  float* const parts = shares + share_cells(c, grad);
   auto dims = [&](AttnRun& r, int Dq, int Dv, bool turned) {   // turned: states are [Dv][Dq] in memory
     r.Dq = Dq; r.Dv = Dv;
     r.sr = turned ? 1 : Dv; r.sc = turned ? Dq : 1;
   };
   auto out = [&](AttnRun& r, const sim_heads& o) {
-    r.out = o.data; r.ob = o.stride_b; r.ot = o.stride_t; r.oh = o.stride_h;
+    r.out = c.T ? o.data : nullptr; r.ob = o.stride_b; r.ot = o.stride_t; r.oh = o.stride_h;
   };
   if (!grad) {
     AttnRun r = f;
@@ -202,40 +687,38 @@ void launch_typed(const AttnArgs& a, bool grad, hipStream_t st) {
     dims(r, c.Dk, c.Dv, false);
     out(r, a.y);
     r.s0 = a.s0; r.state = a.state; r.so = c.scale; r.su = 1.0f;
-    launch_run<E>(r, c.B, st);
-    return;
+    return launch_run<E>(r, c.B, parts, st);
   }
-  // each told by the first run there is
+  hipError_t e = hipSuccess;
+  // lengths and decays are told of by the first run there is
   if (a.dq.data) {
     AttnRun r = f;
     r.q = dy; r.k = v; r.v = k;
     dims(r, c.Dv, c.Dk, true);
     out(r, a.dq);
     r.s0 = a.s0; r.so = c.scale; r.su = 1.0f;
-    launch_run<E>(r, c.B, st);
+    if ((e = launch_run<E>(r, c.B, parts, st)) != hipSuccess) return e;
     f.err = nullptr;
   }
   f.back = true; f.lag = 1; f.so = 1.0f; f.su = c.scale;
   auto shared = [&](AttnRun& r, const sim_heads& o, int D) {
-    if (g == 1 || !o.data) {
-      out(r, o);
-      launch_run<E>(r, c.B, st);
-      return;
-    }
-    r.out = a.work; r.wide = true;
+    out(r, o);
+    if (g == 1 || !r.out) return launch_run<E>(r, c.B, parts, st);
+    r.out = shares; r.wide = true;
     r.oh = D; r.ot = (int64_t)c.H * D; r.ob = c.T * r.ot;
-    launch_run<E>(r, c.B, st);
+    const hipError_t e = launch_run<E>(r, c.B, parts, st);
+    if (e != hipSuccess) return e;
     const int64_t cells = c.B * c.T * c.Hk * D;
-    if (cells)
-      hipLaunchKernelGGL(attn_share_k<E>, dim3((unsigned)std::min<int64_t>((cells + 255) / 256, 1 << 16)), dim3(256), 0,
-                         st, static_cast<const float*>(a.work), o, cells, c.T, c.Hk, g, D);
+    hipLaunchKernelGGL(attn_share_k<E>, dim3((unsigned)std::min<int64_t>((cells + 255) / 256, 1 << 16)), dim3(256), 0, st,
+                       shares, o, cells, c.T, c.Hk, g, D);
+    return hipSuccess;
   };
   if (a.dk.data) {
     AttnRun r = f;
     r.q = v; r.k = dy; r.v = q;
     dims(r, c.Dv, c.Dk, true);
     r.s0 = a.ds;
-    shared(r, a.dk, c.Dk);
+    if ((e = shared(r, a.dk, c.Dk)) != hipSuccess) return e;
     f.err = nullptr;
   }
   if (a.dv.data || a.state) {   // the last one: ds0 may be written over dstate
@@ -243,21 +726,23 @@ void launch_typed(const AttnArgs& a, bool grad, hipStream_t st) {
     r.q = k; r.k = q; r.v = dy;
     dims(r, c.Dk, c.Dv, false);
     r.s0 = a.ds; r.state = a.state;
-    shared(r, a.dv, c.Dv);
+    e = shared(r, a.dv, c.Dv);
   }
+  return e;
 }
 
 }  // namespace
 
 size_t attn_work_bytes(const sim_linear_attn& c, bool grad) {
-  return grad && c.H > c.Hk ? (size_t)c.B * c.T * c.H * std::max(c.Dk, c.Dv) * sizeof(float) : 0;
+  size_t parts = parts_bytes(c.dtype, c.B, c.T, c.H, c.Dk, c.Dv);
+  if (grad) parts = std::max(parts, parts_bytes(c.dtype, c.B, c.T, c.H, c.Dv, c.Dk));
+  return share_cells(c, grad) * sizeof(float) + parts;
 }
 
 hipError_t launch_attn(const AttnArgs& a, bool grad, hipStream_t st) {
-  if (a.c.dtype == SIM_DT_F32) launch_typed<F32>(a, grad, st);
-  else if (a.c.dtype == SIM_DT_BF16) launch_typed<BF16>(a, grad, st);
-  else launch_typed<F16>(a, grad, st);
-  return hipGetLastError();
+  const hipError_t e = a.c.dtype == SIM_DT_F32 ? launch_typed<F32>(a, grad, st)
+                       : a.c.dtype == SIM_DT_BF16 ? launch_typed<BF16>(a, grad, st) : launch_typed<F16>(a, grad, st);
+  return e == hipSuccess ? hipGetLastError() : e;
 }
 
 }  // namespace bsim

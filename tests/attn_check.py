@@ -9,8 +9,8 @@ by at most what its terms lose on their way:
   - for T > 16, values are split into parts of 8 bits: 16-bit types keep 16 bits of the four values that are
     split or multiplied on a term's way (the product q k, its weighted sum, the weighted k or v, the state), each
     off by at most 2^-17 (half a step of the second part), and leave out the product of two second parts, at most
-    2^-18, in up to two products: 4 2^-17 + 2 2^-18 <= 2^-14.6; fp32 keeps three parts, 24 bits: 4 u and four
-    products of a second and a third part, 2^-26 each, and of two third ones: 6 u in all.
+    2^-18, in up to two products: 4 2^-17 + 2 2^-18 <= 2^-14.6; fp32, and states of any type, keep three parts, 24
+    bits: 4 u and four products of a second and a third part, 2^-26 each, and of two third ones: 6 u in all.
 The output's rounding adds half a step of its type."""
 import numpy as np
 import torch
@@ -51,11 +51,11 @@ def check_forward(d, y, state):
     n = None if d["lengths"] is None else d["lengths"].cpu().numpy()
     want, last = ops.linear_attn(q, k, v, l, s0, n, d["scale"])
     m, ms = ops.linear_attn(*map(np.abs, (q, k, v, l)), None if s0 is None else np.abs(s0), n, abs(d["scale"]))
-    e = _loss(d["q"].dtype, q.shape[1], q.shape[3])
+    e, es = (_loss(t, q.shape[1], q.shape[3]) for t in (d["q"].dtype, torch.float32))
     if y is not None:
         near(host(y), want, e * m + rounding(want, d["q"].dtype), "y")
     if state is not None:
-        near(host(state), last, e * ms + rounding(last, torch.float32), "state")
+        near(host(state), last, es * ms + rounding(last, torch.float32), "state")
 
 
 def check_grad(d, dq, dk, dv, ds0):
@@ -64,8 +64,8 @@ def check_grad(d, dq, dk, dv, ds0):
     want = ops.linear_attn_grad(q, k, v, l, dy, s0, ds, n, d["scale"])
     a = [None if x is None else np.abs(x) for x in (q, k, v, l, dy, s0, ds)]
     m = ops.linear_attn_grad(*a, n, abs(d["scale"]))
-    e = _loss(d["q"].dtype, q.shape[1], max(q.shape[3], v.shape[3]) + q.shape[2] // k.shape[2])
+    D = max(q.shape[3], v.shape[3]) + q.shape[2] // k.shape[2]
     for name, got, w, b, dt in zip(("dq", "dk", "dv", "ds0"), (dq, dk, dv, ds0), want, m,
                                    [d["q"].dtype] * 3 + [torch.float32]):
         if got is not None:
-            near(host(got), w, e * b + rounding(w, dt), name)
+            near(host(got), w, _loss(dt, q.shape[1], D) * b + rounding(w, dt), name)
