@@ -55,16 +55,333 @@ struct LogprobOp {
   __device__ static __forceinline__ void finish(const Args&, const Sums&) {}
 };
 
-// The order of alternatives as whole numbers: the logit's (a NaN above all, -0 as 0), then the lowest
-// column first. 0: not an alternative.
-__device__ __forceinline__ uint64_t key_of(float v, uint32_t j) {
-  if (v == -INFINITY) return 0;
-  const uint32_t u = __float_as_uint(v + 0.0f);
-  const uint32_t o = v == v ? ((int32_t)u < 0 ? ~u : u | 0x80000000u) : 0xFFFFFFFFu;
-  return (uint64_t)o << 32 | (uint32_t)~j;
+// ---- with alternatives -------------------------------------------------------------------------
+// The order of logits as signed whole numbers (a NaN above all, -0 as 0), kNone for those that are no alternative; and
+// back.
+constexpr int kNone = INT32_MIN;
+__device__ __forceinline__ int order_of(float v) {
+  const int u = __float_as_int(v + 0.0f), o = u ^ ((u >> 31) & 0x7FFFFFFF);
+  return v == v ? (v == -INFINITY ? kNone : o) : INT32_MAX;
+}
+__device__ __forceinline__ float value_of(int o) { return __int_as_float(o ^ ((o >> 31) & 0x7FFFFFFF)); }
+
+template <int CTRL>
+__device__ __forceinline__ int dpp_of(int v) { return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false); }
+// over 16 or 64 adjacent lanes, in every one: rotations within 16 lanes, then across
+template <int LG, class F>
+__device__ __forceinline__ int group(int v, F f) {
+  v = f(v, dpp_of<0x128>(v));   // row_ror 8, 4, 2, 1
+  v = f(v, dpp_of<0x124>(v));
+  v = f(v, dpp_of<0x122>(v));
+  v = f(v, dpp_of<0x121>(v));
+  if constexpr (LG == 6) {
+    v = f(v, __shfl_xor(v, 16));
+    v = f(v, __shfl_xor(v, 32));
+  }
+  return v;
+}
+template <int LG, class F>
+__device__ __forceinline__ float group_f(float v, F f) {
+  return __int_as_float(group<LG>(__float_as_int(v), [&](int a, int b) { return __float_as_int(f(__int_as_float(a), __int_as_float(b))); }));
 }
 
-// One workgroup per row, one look over the row per alternative.
+// Rows of up to 1024: 1 << LG lanes take a row, V logits each, in registers; an alternative is the largest that is left,
+// found by a round over the lanes. Of adjacent samples (COLS) a workgroup first turns S of them in LDS. Bound by the
+// rounds' chains (some 40 instructions per alternative and 4 rows).
+constexpr int kGroups = 256;
+template <class E, int LG, int V, bool COLS>
+__global__ __launch_bounds__(kGroups) void logprob_short_k(LogprobArgs s, int S) {
+  typedef typename E::T T;
+  extern __shared__ float tile[];
+  const int A = s.c.A, top = s.c.top, gl = threadIdx.x & ((1 << LG) - 1), per = kGroups >> LG;
+  const int64_t N = s.c.N, each = COLS ? S : per;
+  const T* l = static_cast<const T*>(s.l.data);
+  const uint8_t* mk = static_cast<const uint8_t*>(s.mask.data);
+  Sums sums;
+  for (int64_t n0 = blockIdx.x * each; n0 < N; n0 += gridDim.x * each) {
+    if (COLS) {
+      __syncthreads();
+      const int k = threadIdx.x % S;
+      if (n0 + k < N) {
+        const int64_t n = n0 + k;
+#pragma unroll 4
+        for (int j = threadIdx.x / S; j < A; j += kGroups / S) {
+          const float v = (float)l[n * s.l.stride_n + j * s.l.stride_a];
+          tile[j * (S + 1) + k] = mk && !mk[n * s.mask.stride_n + j * s.mask.stride_a] ? -INFINITY : v;
+        }
+      }
+      __syncthreads();
+    }
+    for (int k0 = 0; k0 < each; k0 += per) {
+      const int k = k0 + (threadIdx.x >> LG);
+      const int64_t n = n0 + k;
+      const bool in = n < N && k < each;
+      LogprobOp::Row row{0.0f, 0.0f, -1};
+      bool on = in && LogprobOp::open(s, n, row);
+      float x[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int j = gl + (i << LG);
+        x[i] = -INFINITY;
+        if (on && j < A) {
+          if (COLS) x[i] = tile[j * (S + 1) + k];
+          else x[i] = mk && !mk[n * s.mask.stride_n + j * s.mask.stride_a] ? -INFINITY : (float)l[n * s.l.stride_n + j];
+        }
+      }
+      const float la = on && gl == 0 ? LogprobOp::taken<T>(s, n, row) : 0.0f;
+      Part p{-INFINITY, 0.0f, 0.0f};
+#pragma unroll
+      for (int i = 0; i < V; ++i) p.m = max_nan(p.m, x[i]);
+      p.m = group_f<LG>(p.m, [](float a, float b) { return max_nan(a, b); });
+      const float m = p.m == -INFINITY ? 0.0f : p.m;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float d = max_nan(x[i] - m, kLowest), e = exp_of(d);
+        p.S += e;
+        p.X = fmaf(e, d, p.X);
+      }
+      p.S = group_f<LG>(p.S, [](float a, float b) { return a + b; });
+      p.X = group_f<LG>(p.X, [](float a, float b) { return a + b; });
+      RowOut o;
+      if (gl == 0 && in && !(on && LogprobOp::close(s, n, row, p, la, true, sums, o))) LogprobOp::shut(s, n);
+      const float logS = log_of(p.S);
+      int q[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) q[i] = order_of(x[i]);
+      for (int t = 0; t < top; ++t) {
+        int best = kNone, at = 0;
+#pragma unroll
+        for (int i = V - 1; i >= 0; --i) {   // of equal ones the first
+          at = q[i] >= best ? i : at;
+          best = q[i] >= best ? q[i] : best;
+        }
+        const int most = group<LG>(best, [](int a, int b) { return a > b ? a : b; });
+        const int j = gl + (at << LG);
+        const int first = group<LG>(best == most ? j : INT32_MAX, [](int a, int b) { return a < b ? a : b; });
+        if (first == j && most != kNone) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) q[i] = i == at ? kNone : q[i];
+        }
+        if (in && gl == (t & ((1 << LG) - 1))) {
+          if (s.top_index) s.top_index[n * top + t] = most == kNone ? -1 : first;
+          if (s.top_logp) s.top_logp[n * top + t] = most == kNone ? -INFINITY : (value_of(most) - p.m) - logS;
+        }
+      }
+    }
+  }
+}
+
+// The largest logits that a wave has seen, largest first, one a lane, of equal ones the lower column first.
+struct Best {
+  int v, j;   // kNone where there is none yet
+  __device__ __forceinline__ void clear() { v = kNone; j = INT32_MAX; }
+  // (most, col), the same in all lanes, joins; `top` are kept
+  __device__ __forceinline__ void join(int most, int col) {
+    const int pos = __popcll(__ballot(v > most || (v == most && j < col))), lane = threadIdx.x & 63;
+    const int pv = dpp_of<0x138>(v), pj = dpp_of<0x138>(j);   // wave_shr 1
+    v = lane < pos ? v : (lane == pos ? most : pv);
+    j = lane < pos ? j : (lane == pos ? col : pj);
+  }
+  __device__ __forceinline__ int least(int top) const { return __builtin_amdgcn_readlane(v, top - 1); }
+  __device__ __forceinline__ int least_col(int top) const { return __builtin_amdgcn_readlane(j, top - 1); }
+};
+
+// Longer rows: a workgroup takes a row or one of gridDim.y parts of it, its waves every fourth stretch of 512 logits; each
+// keeps its largest ones, in lanes, and the least of them as the bound that a stretch's largest logit is compared with, so
+// that after the first stretches few get further. Of those that do the largest joins first, then the next, so that
+// no more than `top` of a stretch do, rising rows or not. Bound by HBM for many rows (and by the chains of the first
+// stretches for few).
+constexpr int kLong = 256, kLongWaves = kLong / 64;
+struct LongPart {
+  Part p;
+  int have;                  // 0: the row is not looked at
+  int v[64], j[64];
+};
+template <class E>
+__global__ __launch_bounds__(kLong) void logprob_long_k(LogprobArgs s) {
+  typedef typename E::T T;
+  constexpr int N = 8, U = 2;   // logits of a lane that are compared together, and chunks that fly together
+  typedef Chunk<E, N> Ch;
+  __shared__ Part parts[kLongWaves];
+  __shared__ int lv[kLongWaves][64], lj[kLongWaves][64];
+  __shared__ float taken;
+  const int A = s.c.A, top = s.c.top, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int units = (A + N - 1) / N, c0 = (int)((int64_t)units * blockIdx.y / gridDim.y),
+            c1 = (int)((int64_t)units * (blockIdx.y + 1) / gridDim.y);
+  for (int64_t n = blockIdx.x; n < s.c.N; n += gridDim.x) {
+    LogprobOp::Row row;
+    const bool on = LogprobOp::open(s, n, row);
+    Part p{-INFINITY, 0.0f, 0.0f};
+    Best best;
+    best.clear();
+    if (on) {
+      if (threadIdx.x == 0) taken = LogprobOp::taken<T>(s, n, row);
+      const T* l = static_cast<const T*>(s.l.data) + n * s.l.stride_n;
+      const uint8_t* mk = s.mask.data ? static_cast<const uint8_t*>(s.mask.data) + n * s.mask.stride_n : nullptr;
+      float bound = -INFINITY;
+      for (int at = c0 + threadIdx.x; at - lane < c1; at += U * kLong) {
+        Ch ch[U];
+        MaskBytes<N> mb[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int j = (at + u * kLong) * N;
+          if (at + u * kLong < c1) {
+            if (j + N <= A) {
+              ch[u].load(l + j);
+              if (mk) mb[u].load(mk + j * s.mask.stride_a, s.mask.stride_a);
+            } else {
+#pragma unroll
+              for (int i = 0; i < N; ++i) {
+                ch[u].v[i] = j + i < A ? l[j + i] : (T)-INFINITY;
+                if (i % 4 == 0) mb[u].w[i / 4] = 0;
+                if (mk && j + i < A) mb[u].w[i / 4] |= (uint32_t)mk[(j + i) * s.mask.stride_a] << (8 * (i % 4));
+              }
+            }
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          float x[N], M = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            x[i] = at + u * kLong < c1 ? ch[u].get(i) : -INFINITY;
+            if (mk) x[i] = at + u * kLong < c1 && mb[u].open(i) ? x[i] : -INFINITY;
+            M = max_nan(M, x[i]);
+          }
+          if (!(M == -INFINITY)) {
+            p = against<false>(p, max_nan(p.m, M));
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+              const float d = max_nan(x[i] - p.m, kLowest), e = exp_of(d);
+              p.S += e;
+              p.X = fmaf(e, d, p.X);
+            }
+          }
+          if (!__any(!(M <= bound))) continue;
+          int q[N], mine, i0;
+#pragma unroll
+          for (int i = 0; i < N; ++i) q[i] = order_of(x[i]);
+          auto pick = [&]() {
+            mine = kNone, i0 = 0;
+#pragma unroll
+            for (int i = N - 1; i >= 0; --i) {
+              i0 = q[i] >= mine ? i : i0;
+              mine = q[i] >= mine ? q[i] : mine;
+            }
+          };
+          pick();
+          int least = best.least(top);
+          for (;;) {
+            const int most = __builtin_amdgcn_readfirstlane(group<6>(mine, [](int a, int b) { return a > b ? a : b; }));
+            if (most <= least) break;   // an equal one has a higher column than those that are kept
+            const int who = __builtin_ctzll(__ballot(mine == most));   // the lowest column
+            best.join(most, (at - lane + u * kLong + who) * N + __builtin_amdgcn_readlane(i0, who));
+            least = best.least(top);
+            if (lane == who) {
+#pragma unroll
+              for (int i = 0; i < N; ++i) q[i] = i == i0 ? kNone : q[i];
+              pick();
+            }
+          }
+          bound = least == kNone ? -INFINITY : (least == INT32_MAX ? INFINITY : value_of(least));
+        }
+      }
+      __syncthreads();   // a row before may still be read
+      p = join_threads<false, kLongWaves>(p, parts);
+      lv[wave][lane] = best.v;
+      lj[wave][lane] = best.j;
+      __syncthreads();
+      if (wave == 0) {
+        for (int w = 1; w < kLongWaves; ++w) {
+          const int wv = lv[w][lane], wj = lj[w][lane];
+          for (int i = 0; i < top; ++i) {
+            const int v = __builtin_amdgcn_readlane(wv, i), j = __builtin_amdgcn_readlane(wj, i), least = best.least(top);
+            if (v < least || v == kNone || (v == least && j > best.least_col(top))) break;
+            best.join(v, j);
+          }
+        }
+      }
+    }
+    if (wave != 0) continue;
+    if (gridDim.y > 1) {
+      LongPart& o = static_cast<LongPart*>(s.work)[n * gridDim.y + blockIdx.y];
+      if (lane == 0) {
+        o.p = p;
+        o.have = on;
+      }
+      o.v[lane] = best.v;
+      o.j[lane] = best.j;
+      continue;
+    }
+    const float logS = log_of(p.S);
+    RowOut o;
+    Sums sums;
+    if (lane == 0 && !(on && LogprobOp::close(s, n, row, p, taken, true, sums, o))) LogprobOp::shut(s, n);
+    if (lane < top) {
+      if (s.top_index) s.top_index[n * top + lane] = best.v == kNone ? -1 : best.j;
+      if (s.top_logp) s.top_logp[n * top + lane] = best.v == kNone ? -INFINITY : (value_of(best.v) - p.m) - logS;
+    }
+  }
+}
+// The parts of a row: a wave.
+template <class E>
+__global__ __launch_bounds__(64) void logprob_join_k(LogprobArgs s, int parts) {
+  const int64_t n = blockIdx.x;
+  const int lane = threadIdx.x, top = s.c.top;
+  const LongPart* in = static_cast<const LongPart*>(s.work) + n * parts;
+  LogprobOp::Row row;
+  const bool on = LogprobOp::open(s, n, row);
+  float M = -INFINITY;
+  for (int i = lane; i < parts; i += 64) M = max_nan(M, in[i].p.m);
+  M = wave_max(M);
+  Part p{M, 0.0f, 0.0f};
+  for (int i = lane; i < parts; i += 64) {
+    const Part q = against<false>(in[i].p, M);
+    p.S += q.S;
+    p.X += q.X;
+  }
+  p.S = wave_add(p.S);
+  p.X = wave_add(p.X);
+  Best best;
+  best.clear();
+  constexpr int U = 8;   // loads that fly together
+  for (int i0 = 0; i0 < parts; i0 += U) {
+    int wv[U], wj[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const LongPart& q = in[i0 + u < parts ? i0 + u : parts - 1];
+      wv[u] = i0 + u < parts ? q.v[lane] : kNone;
+      wj[u] = q.j[lane];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      for (int i = 0; i < top; ++i) {
+        const int v = __builtin_amdgcn_readlane(wv[u], i), j = __builtin_amdgcn_readlane(wj[u], i), least = best.least(top);
+        if (v == kNone || v < least || (v == least && j > best.least_col(top))) break;
+        best.join(v, j);
+      }
+    }
+  }
+  const float logS = log_of(p.S);
+  RowOut o;
+  Sums sums;
+  if (lane == 0) {
+    const float la = on ? LogprobOp::taken<typename E::T>(s, n, row) : 0.0f;
+    if (!(on && LogprobOp::close(s, n, row, p, la, true, sums, o))) LogprobOp::shut(s, n);
+  }
+  if (lane < top) {
+    if (s.top_index) s.top_index[n * top + lane] = best.v == kNone || !on ? -1 : best.j;
+    if (s.top_logp) s.top_logp[n * top + lane] = best.v == kNone || !on ? -INFINITY : (value_of(best.v) - p.m) - logS;
+  }
+}
+
+// Many adjacent samples of more than 960 columns: one look over the row per alternative, as slow as it is rare.
+// an alternative's place in the order of them all, 0 for none
+__device__ __forceinline__ uint64_t key_of(float v, uint32_t j) {
+  const int o = order_of(v);
+  return o == kNone ? 0 : (uint64_t)((uint32_t)o ^ 0x80000000u) << 32 | (uint32_t)~j;
+}
 constexpr int kTop = 256;
 template <class E>
 __global__ __launch_bounds__(kTop) void logprob_top_k(LogprobArgs s) {
@@ -118,24 +435,58 @@ __global__ __launch_bounds__(kTop) void logprob_top_k(LogprobArgs s) {
   }
 }
 
+constexpr int kShort = 1024, kTurned = 960;
+constexpr int kLongFill = 1024, kLongLeast = 4096;
+// parts of a long row: enough to fill the chip
+int parts_of(int64_t N, int A) {
+  const int64_t want = (kLongFill + N - 1) / std::max<int64_t>(N, 1);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(want, A / kLongLeast));
+}
+
+template <class E, bool COLS>
+void launch_short(const LogprobArgs& a, hipStream_t st) {
+  const int A = a.c.A, S = A <= 240 ? 64 : 16;
+  const int per = COLS ? S : (A <= 256 ? kGroups / 16 : kGroups / 64);
+  const dim3 grid(blocks_for(a.c.N, per, 1 << 16)), block(kGroups);
+  const size_t lds = COLS ? (size_t)A * (S + 1) * sizeof(float) : 0;
+  if (A <= 64) hipLaunchKernelGGL((logprob_short_k<E, 4, 4, COLS>), grid, block, lds, st, a, S);
+  else if (A <= 128) hipLaunchKernelGGL((logprob_short_k<E, 4, 8, COLS>), grid, block, lds, st, a, S);
+  else if (A <= 256) hipLaunchKernelGGL((logprob_short_k<E, 4, 16, COLS>), grid, block, lds, st, a, S);
+  else if (A <= 512) hipLaunchKernelGGL((logprob_short_k<E, 6, 8, COLS>), grid, block, lds, st, a, S);
+  else hipLaunchKernelGGL((logprob_short_k<E, 6, 16, COLS>), grid, block, lds, st, a, S);
+}
+
+template <class E>
+hipError_t launch_top(const LogprobArgs& a, hipStream_t st) {
+  const bool rows = a.l.stride_a == 1 || a.c.A == 1;
+  if (rows && a.c.A <= kShort) {
+    launch_short<E, false>(a, st);
+  } else if (rows) {
+    const int parts = parts_of(a.c.N, a.c.A);
+    hipLaunchKernelGGL(logprob_long_k<E>, dim3(blocks_for(a.c.N, 1, 1 << 16), parts), dim3(kLong), 0, st, a);
+    if (parts > 1) hipLaunchKernelGGL(logprob_join_k<E>, dim3((unsigned)a.c.N), dim3(64), 0, st, a, parts);
+  } else if (a.c.A <= kTurned) {
+    launch_short<E, true>(a, st);
+  } else {
+    const hipError_t e = launch_loss<LogprobOp>(a, 0, st);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(logprob_top_k<E>, dim3(blocks_for(a.c.N, 1, 1 << 20)), dim3(kTop), 0, st, a);
+  }
+  return hipGetLastError();
+}
+
 }  // namespace
 
-size_t logprob_bytes(const sim_logprobs&, bool) {
-  return (size_t)kMaxBlocks * 3 * sizeof(double) + kSplitMost * (sizeof(Part) + sizeof(float));
+size_t logprob_bytes(const sim_logprobs& c, bool grad) {
+  const size_t split = (size_t)kMaxBlocks * 3 * sizeof(double) + kSplitMost * (sizeof(Part) + sizeof(float));
+  if (grad || c.top == 0) return split;
+  const int parts = c.A > kShort ? parts_of(c.N, c.A) : 1;
+  return std::max(split, parts > 1 ? (size_t)c.N * parts * sizeof(LongPart) : 0);
 }
 
 hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t st) {
-  if (a.logp || a.entropy || a.grad.data) {
-    const hipError_t e = launch_loss<LogprobOp>(a, 0, st);
-    if (e != hipSuccess) return e;
-  }
-  if (a.top_index || a.top_logp) {
-    const dim3 grid(blocks_for(a.c.N, 1, 1 << 20)), block(kTop);
-    if (a.c.dtype == SIM_DT_F32) hipLaunchKernelGGL(logprob_top_k<F32>, grid, block, 0, st, a);
-    else if (a.c.dtype == SIM_DT_BF16) hipLaunchKernelGGL(logprob_top_k<BF16>, grid, block, 0, st, a);
-    else hipLaunchKernelGGL(logprob_top_k<F16>, grid, block, 0, st, a);
-  }
-  return hipGetLastError();
+  if (!a.top_index && !a.top_logp) return launch_loss<LogprobOp>(a, 0, st);
+  return a.c.dtype == SIM_DT_F32 ? launch_top<F32>(a, st) : a.c.dtype == SIM_DT_BF16 ? launch_top<BF16>(a, st) : launch_top<F16>(a, st);
 }
 
 }  // namespace bsim
