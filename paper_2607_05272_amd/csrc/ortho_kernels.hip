@@ -9,6 +9,7 @@
 // singular value of X stays below about 1.2 with the usual coefficients, so elements lie within fp16's range with room for 60,
 // and the elements of a 65536 x 65536 update, 2^-16 of its norm, are still normal numbers. Sums are fp32.
 #include <algorithm>
+#include <atomic>
 
 #include "ops_dev.hpp"
 
@@ -28,26 +29,41 @@ struct OrthoDims {
 };
 struct Layout {
   OrthoDims d;
-  int tile, parts;
+  int half, whole, parts;      // tiles of the symmetric products and of X
+  int sums_n;                  // workgroups that add up squares of a matrix
   size_t x, a;                 // elements of a part of one matrix
   size_t sums, x0, x1, A, B, bytes;   // offsets in bytes
 };
-constexpr int kNorm = 256, kNormParts = 64, kFill = 256;
+constexpr int kNorm = 256;
 int round_up(int v, int to) { return (v + to - 1) / to * to; }
+// The largest tile of which there are enough to fill the chip (256: a workgroup on each CU, of 128 and 64 several), measured
+// (us, tiles of the symmetric products / of X):
+//   bf16 4096 x 8192       64/64 4866, 128/128 3546, 128/256 3319, 256/256 3177
+//   bf16 2048 x 8192       64/64 1198, 64/128 1042, 64/256 1008, 128/256 1047, 256/256 1867
+//   bf16 8 x 1024 x 4096   64/64 1297, 64/128 1178, 128/128 1077, 128/256 1073, 256/256 1398
+//   bf16 2 x 2048 x 2048   64/64 752, 64/128 667, 128/128 671, 64/256 778
+//   bf16 32 x 512 x 512    64/64 355, 64/128 334, 128/128 351, 64/256 377
+//   fp32 4 x 256 x 256     64/64 111, 64/128 147, 128/128 214
+template <class F>
+int tile_for(F tiles, int64_t of256, int64_t of128) {
+  return tiles(256) >= of256 ? 256 : (tiles(128) >= of128 ? 128 : 64);
+}
 Layout layout_of(const sim_ortho& o) {
   Layout l;
   const bool t = o.M > o.N;
   l.d = OrthoDims{(int)o.n, (int)(t ? o.N : o.M), (int)(t ? o.M : o.N), 0, 0, t};
-  const int64_t wide = (int64_t)l.d.n * ((l.d.r + 127) / 128) * ((l.d.c + 127) / 128);
-  l.tile = wide >= kFill ? 128 : 64;
+  const int64_t r = l.d.r, c = l.d.c, n = l.d.n;
+  l.half = tile_for([&](int64_t t) { const int64_t k = (r + t - 1) / t; return n * k * (k + 1) / 2; }, 128, 280);
+  l.whole = tile_for([&](int64_t t) { return n * ((r + t - 1) / t) * ((c + t - 1) / t); }, 200, 256);
   l.parts = o.dtype == SIM_DT_BF16 ? 1 : 2;
-  l.d.R = round_up(l.d.r, l.tile);
-  l.d.C = round_up(l.d.c, l.tile);
+  l.d.R = round_up(l.d.r, std::max(l.half, l.whole));
+  l.d.C = round_up(l.d.c, l.whole);
   l.x = (size_t)l.d.R * l.d.C;
   l.a = (size_t)l.d.R * l.d.R;
-  const size_t n = l.d.n, e = sizeof(_Float16) * l.parts;
+  const size_t e = sizeof(_Float16) * l.parts;
   l.sums = 0;
-  l.x0 = n * kNormParts * sizeof(double);
+  l.sums_n = (int)std::max<int64_t>(1, std::min<int64_t>({std::max(o.M, o.N), 1024, (2048 + n - 1) / n}));
+  l.x0 = (n * l.sums_n * sizeof(double) + 15) / 16 * 16;
   l.x1 = l.x0 + n * l.x * e;
   l.A = l.x1 + n * l.x * e;
   l.B = l.A + n * l.a * e;
@@ -73,7 +89,7 @@ __global__ __launch_bounds__(kNorm) void ortho_norm_k(const void* u0, View v, do
   __shared__ double lds[kNorm / 64];
   const T* u = static_cast<const T*>(u0) + blockIdx.y * v.si;
   double s = 0.0;
-  for (int i = blockIdx.x; i < v.rows; i += kNormParts) {
+  for (int i = blockIdx.x; i < v.rows; i += gridDim.x) {
     const T* row = u + i * v.slow;
 #pragma unroll 4
     for (int j = threadIdx.x; j < v.cols; j += kNorm) {
@@ -84,7 +100,7 @@ __global__ __launch_bounds__(kNorm) void ortho_norm_k(const void* u0, View v, do
   for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o);
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
   __syncthreads();
-  if (threadIdx.x == 0) part[blockIdx.y * kNormParts + blockIdx.x] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
+  if (threadIdx.x == 0) part[blockIdx.y * gridDim.x + blockIdx.x] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
 __device__ __forceinline__ void split(float x, _Float16 (&p)[2]) {
@@ -95,13 +111,14 @@ __device__ __forceinline__ void split(float x, _Float16 (&p)[1]) { p[0] = (_Floa
 
 // X's parts, padding included: tiles of 64 x 64, read along U's faster axis and written along X's rows.
 template <class E, int NP>
-__global__ __launch_bounds__(256) void ortho_load_k(const void* u0, View v, OrthoDims d, const double* part, double eps,
-                                                    _Float16* x) {
+__global__ __launch_bounds__(256) void ortho_load_k(const void* u0, View v, OrthoDims d, const double* part, int parts,
+                                                    double eps, _Float16* x) {
   typedef typename E::T T;
   __shared__ float t[64][65];
   const int tiles = d.C / 64, r0 = blockIdx.x / tiles * 64, c0 = blockIdx.x % tiles * 64;
-  double s = 0.0;
-  for (int p = 0; p < kNormParts; ++p) s += part[blockIdx.y * kNormParts + p];
+  double s = 0.0;   // every wave adds them up in the same order
+  for (int p = threadIdx.x & 63; p < parts; p += 64) s += part[(size_t)blockIdx.y * parts + p];
+  for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o);
   // an infinity or NaN makes NaN of the whole; of no update nothing is left, whatever eps
   const double f = s == 0.0 ? 0.0 : (s - s == 0.0 ? (double)kUp / (sqrt(s) + eps) : __longlong_as_double(0x7FF8000000000000ll));
   const T* u = static_cast<const T*>(u0) + blockIdx.y * v.si;
@@ -155,12 +172,14 @@ __device__ __forceinline__ H4 read_turned(const _Float16* p) {
   return __builtin_bit_cast(H4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((L4*)(p)));
 }
 
-// The three products, tiles of TM x TM by four waves, each TM/2 x TM/2 in tiles of 32:
+// The three products, tiles of TM x TM:
 //   kGram   out = P P^T             P = X, K = C
 //   kPoly   out = b P + c P P^T     P = A (symmetric), K = R
 //   kStep   out = a Q + P Q         P = B, Q = X [K][.], read turned from LDS
-// K goes by BK; its next part is loaded into registers while the present one is multiplied, and goes to the other half of LDS.
-// In LDS a row's chunks of 16 bytes are exchanged so that 16 rows at one place of K lie in different banks.
+// K goes by BK; its next parts are on their way to registers while the present one is multiplied, and go to the other half
+// of LDS one after another. In LDS a row's chunks of 16 bytes are exchanged so that 16 rows at one place of K lie in
+// different banks. Tiles of 256 are shared by eight waves, 128 x 64 each (of 64 x 64 LDS feeds the matrix units too slowly:
+// it gives 128 bytes a cycle, and a wave needs 128 of them per 8 cycles of MFMA), smaller ones by four.
 enum { kGram = 0, kPoly = 1, kStep = 2 };
 struct Mul {
   const _Float16 *P, *Q;
@@ -173,13 +192,25 @@ struct Mul {
   int r, c;
   bool end;
 };
+constexpr int threads_of(int TM) { return TM == 256 ? 512 : 256; }
+template <int NP, int TM>
+struct Form {
+  static constexpr int kThreads = threads_of(TM), kRows = TM == 256 ? 4 : TM / 64, kCols = TM == 256 ? 2 : TM / 64;
+  static constexpr int BK = NP == 1 || TM == 64 ? 64 : 32, kStage = NP * TM * BK;   // elements of P or Q in half of LDS
+  static constexpr size_t kLds = 4 * kStage * sizeof(_Float16);
+  static_assert(64 * (TM + 1) * sizeof(float) <= kLds, "a band of the result");
+};
 template <int NP, int TM, int KIND>
-__global__ __launch_bounds__(256, 2) void ortho_mul_k(Mul m) {
-  constexpr int BK = NP == 1 ? 64 : 32, CH = BK / 8, W = TM / 64, U = TM * BK / 8 / 256;
+__global__ __launch_bounds__(threads_of(TM), TM == 256 ? 1 : 2) void ortho_mul_k(Mul m) {
+  typedef Form<NP, TM> Fm;
+  constexpr int BK = Fm::BK, CH = BK / 8, NT = Fm::kThreads, U = TM * BK / 8 / NT, WR = Fm::kRows, WC = Fm::kCols;
+  constexpr int AHEAD = TM == 64 && NP == 1 ? 3 : (TM == 256 ? 1 : 2);   // parts of K on their way
   constexpr int QC = TM / 8;   // chunks of a row of Q, turned
-  __shared__ __align__(16) _Float16 ps[2][NP][TM * BK], qs[2][NP][TM * BK];
+  extern __shared__ __align__(16) char raw[];
+  _Float16* const lds = reinterpret_cast<_Float16*>(raw);   // [half][P, Q][part]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wr = (wave >> 1) * (TM / 2), wc = (wave & 1) * (TM / 2), l32 = lane & 31, half = lane >> 5;
+  constexpr int AC = TM / (32 * WC);   // waves along the columns
+  const int wr = wave / AC * 32 * WR, wc = wave % AC * 32 * WC, l32 = lane & 31, half = lane >> 5;
   // neighbours of a run of tiles per XCD share their operands in its L2; runs go down bands of eight rows of tiles
   const int all = gridDim.x, xcd = blockIdx.x & 7, each = all >> 3, more = all & 7;
   int id = xcd * each + (xcd < more ? xcd : more) + (blockIdx.x >> 3);
@@ -197,54 +228,59 @@ __global__ __launch_bounds__(256, 2) void ortho_mul_k(Mul m) {
   const int i = blockIdx.y, r0 = ti * TM, c0 = tj * TM, K = m.K;
   const _Float16* P = m.P + (size_t)i * NP * m.p + (size_t)r0 * K;
   const _Float16* Q = KIND == kStep ? m.Q + (size_t)i * NP * m.q + c0 : m.P + (size_t)i * NP * m.p + (size_t)c0 * K;
-  H8 pr[NP][U], qr[NP][U];
-  auto fetch = [&](int k0) {
+  struct Stage { H8 p[NP][U], q[NP][U]; };
+  Stage in[AHEAD];
+  auto fetch = [&](Stage& g, int k0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int unit = threadIdx.x + u * 256, row = unit / CH, ch = unit % CH;
+      const int unit = threadIdx.x + u * NT, row = unit / CH, ch = unit % CH;
 #pragma unroll
       for (int q = 0; q < NP; ++q) {
-        pr[q][u] = *reinterpret_cast<const H8*>(P + q * m.p + (size_t)row * K + k0 + ch * 8);
-        if (KIND == kStep) qr[q][u] = *reinterpret_cast<const H8*>(Q + q * m.q + (size_t)(k0 + unit / QC) * m.ld + unit % QC * 8);
-        else qr[q][u] = *reinterpret_cast<const H8*>(Q + q * m.p + (size_t)row * K + k0 + ch * 8);
+        g.p[q][u] = *reinterpret_cast<const H8*>(P + q * m.p + (size_t)row * K + k0 + ch * 8);
+        if (KIND == kStep) g.q[q][u] = *reinterpret_cast<const H8*>(Q + q * m.q + (size_t)(k0 + unit / QC) * m.ld + unit % QC * 8);
+        else g.q[q][u] = *reinterpret_cast<const H8*>(Q + q * m.p + (size_t)row * K + k0 + ch * 8);
       }
     }
   };
   auto swap_p = [](int row, int ch) { return row * BK + ((ch ^ ((row / (16 / CH)) & (CH - 1))) * 8); };
   auto swap_q = [](int row, int ch) { return row * TM + ((ch ^ ((row & 3) << 2 & (QC - 1))) * 8); };
-  auto store = [&](int to) {
+  auto ps = [&](int h, int q) { return lds + (2 * h) * Fm::kStage + q * (TM * BK); };
+  auto qs = [&](int h, int q) { return lds + (2 * h + 1) * Fm::kStage + q * (TM * BK); };
+  auto store = [&](const Stage& g, int to) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int unit = threadIdx.x + u * 256, at = swap_p(unit / CH, unit % CH);
+      const int unit = threadIdx.x + u * NT, at = swap_p(unit / CH, unit % CH);
 #pragma unroll
       for (int q = 0; q < NP; ++q) {
-        *reinterpret_cast<H8*>(&ps[to][q][at]) = pr[q][u];
-        *reinterpret_cast<H8*>(&qs[to][q][KIND == kStep ? swap_q(unit / QC, unit % QC) : at]) = qr[q][u];
+        *reinterpret_cast<H8*>(ps(to, q) + at) = g.p[q][u];
+        *reinterpret_cast<H8*>(qs(to, q) + (KIND == kStep ? swap_q(unit / QC, unit % QC) : at)) = g.q[q][u];
       }
     }
   };
-  F16x acc[W][W];
+  F16x acc[WR][WC];
 #pragma unroll
-  for (int x = 0; x < W; ++x) {
+  for (int x = 0; x < WR; ++x) {
 #pragma unroll
-    for (int y = 0; y < W; ++y) acc[x][y] = F16x{};
+    for (int y = 0; y < WC; ++y) acc[x][y] = F16x{};
   }
   auto multiply = [&](int from) {
 #pragma unroll
     for (int kk = 0; kk < BK / 16; ++kk) {
-      H8 a[W][NP], b[W][NP];
+      H8 a[WR][NP], b[WC][NP];
 #pragma unroll
-      for (int x = 0; x < W; ++x) {
+      for (int q = 0; q < NP; ++q) {
 #pragma unroll
-        for (int q = 0; q < NP; ++q) {
-          a[x][q] = *reinterpret_cast<const H8*>(&ps[from][q][swap_p(wr + 32 * x + l32, 2 * kk + half)]);
+        for (int x = 0; x < WR; ++x)
+          a[x][q] = *reinterpret_cast<const H8*>(ps(from, q) + swap_p(wr + 32 * x + l32, 2 * kk + half));
+#pragma unroll
+        for (int y = 0; y < WC; ++y) {
           if (KIND == kStep) {
-            const int k = 16 * kk + 8 * half + ((lane & 15) >> 2), c = wc + 32 * x + (lane & 16) + 4 * (lane & 3);
-            const H4 lo = read_turned(&qs[from][q][swap_q(k, c / 8) + (c & 7)]);
-            const H4 hi = read_turned(&qs[from][q][swap_q(k + 4, c / 8) + (c & 7)]);
-            b[x][q] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            const int k = 16 * kk + 8 * half + ((lane & 15) >> 2), c = wc + 32 * y + (lane & 16) + 4 * (lane & 3);
+            const H4 lo = read_turned(qs(from, q) + swap_q(k, c / 8) + (c & 7));
+            const H4 hi = read_turned(qs(from, q) + swap_q(k + 4, c / 8) + (c & 7));
+            b[y][q] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
           } else {
-            b[x][q] = *reinterpret_cast<const H8*>(&qs[from][q][swap_p(wc + 32 * x + l32, 2 * kk + half)]);
+            b[y][q] = *reinterpret_cast<const H8*>(qs(from, q) + swap_p(wc + 32 * y + l32, 2 * kk + half));
           }
         }
       }
@@ -253,93 +289,157 @@ __global__ __launch_bounds__(256, 2) void ortho_mul_k(Mul m) {
 #pragma unroll
         for (int q = 0; q + p < NP; ++q) {
 #pragma unroll
-          for (int x = 0; x < W; ++x) {
+          for (int x = 0; x < WR; ++x) {
 #pragma unroll
-            for (int y = 0; y < W; ++y)
+            for (int y = 0; y < WC; ++y)
               acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[x][p], b[y][q], acc[x][y], 0, 0, 0);
           }
         }
       }
     }
   };
-  fetch(0);
-  store(0);
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j)
+    if (j * BK < K) fetch(in[j], j * BK);
+  store(in[0], 0);
+  if (AHEAD * BK < K) fetch(in[0], AHEAD * BK);
   __syncthreads();
   int use = 0;
-  for (int k0 = 0; k0 < K; k0 += BK) {
-    if (k0 + BK < K) fetch(k0 + BK);
-    multiply(use);
-    if (k0 + BK < K) store(use ^ 1);
-    __syncthreads();
-    use ^= 1;
-  }
-  // lane: column l32 of a tile, rows 8 (e / 4) + 4 half + e % 4
-  const _Float16* own = KIND == kStep ? m.Q + (size_t)i * NP * m.q : m.P + (size_t)i * NP * m.p;
-  const size_t own_part = KIND == kStep ? m.q : m.p;
-  _Float16* out = m.out + (size_t)i * NP * m.o;
+  for (int k1 = 0; k1 < K; k1 += AHEAD * BK) {
 #pragma unroll
-  for (int x = 0; x < W; ++x) {
-#pragma unroll
-    for (int y = 0; y < W; ++y) {
-      const int c = c0 + wc + 32 * y + l32;
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int r = r0 + wr + 32 * x + 8 * g + 4 * half;
-        H4 keep[NP];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const size_t at = (size_t)(r + e) * m.ld + c;
-          float v = acc[x][y][4 * g + e] * m.mul;
-          if (KIND != kGram) {
-            float w = 0.0f;
-#pragma unroll
-            for (int q = NP - 1; q >= 0; --q) w += (float)own[q * own_part + at];
-            v = fmaf(m.own, w, v);
-          }
-          if (KIND == kStep && m.end) {
-            if (r + e < m.r && c < m.c) m.last.put(i, r + e, c, v);
-            continue;
-          }
-          _Float16 p[NP];
-          split(v, p);
-#pragma unroll
-          for (int q = 0; q < NP; ++q) {
-            out[q * m.o + at] = p[q];
-            keep[q][e] = p[q];
-          }
-        }
-        if (KIND != kStep && ti != tj) {
-#pragma unroll
-          for (int q = 0; q < NP; ++q) *reinterpret_cast<H4*>(&out[q * m.o + (size_t)c * m.ld + r]) = keep[q];
-        }
+    for (int j = 0; j < AHEAD; ++j) {
+      const int k0 = k1 + j * BK;
+      if (k0 < K) {
+        Stage& next = in[(j + 1) % AHEAD];
+        multiply(use);
+        if (k0 + BK < K) store(next, use ^ 1);
+        if (k0 + (AHEAD + 1) * BK < K) fetch(next, k0 + (AHEAD + 1) * BK);
+        __syncthreads();
+        use ^= 1;
       }
     }
   }
-}
-
-template <int NP, int TM>
-void steps_of(const OrthoArgs& a, const Layout& l, const Out& last, hipStream_t st) {
-  char* w = static_cast<char*>(a.work);
-  _Float16 *x = reinterpret_cast<_Float16*>(w + l.x0), *y = reinterpret_cast<_Float16*>(w + l.x1);
-  _Float16 *A = reinterpret_cast<_Float16*>(w + l.A), *B = reinterpret_cast<_Float16*>(w + l.B);
-  const int tr = l.d.R / TM, tc = l.d.C / TM;
-  const unsigned n = (unsigned)l.d.n;
-  const dim3 half((unsigned)((int64_t)tr * (tr + 1) / 2), n), whole((unsigned)((int64_t)tr * tc), n), block(256);
-  for (int i = 0; i < a.c.steps; ++i) {
-    Mul m{};
-    m.P = x; m.p = l.x; m.out = A; m.o = l.a; m.K = l.d.C; m.ld = l.d.R; m.mul = kDown;
-    hipLaunchKernelGGL((ortho_mul_k<NP, TM, kGram>), half, block, 0, st, m);
-    m.P = A; m.p = l.a; m.out = B; m.K = l.d.R; m.own = a.c.b; m.mul = a.c.c * kDown;
-    hipLaunchKernelGGL((ortho_mul_k<NP, TM, kPoly>), half, block, 0, st, m);
-    m.P = B; m.Q = x; m.q = l.x; m.out = y; m.o = l.x; m.ld = l.d.C; m.own = a.c.a; m.mul = kDown;
-    m.rows = tr; m.cols = tc; m.r = l.d.r; m.c = l.d.c; m.last = last; m.end = i + 1 == a.c.steps;
-    hipLaunchKernelGGL((ortho_mul_k<NP, TM, kStep>), whole, block, 0, st, m);
-    std::swap(x, y);
+  // The result goes through LDS, 64 rows at once, so that memory is read and written in chunks of 16 bytes, also where a
+  // tile is written a second time, turned.
+  constexpr int S = TM + 1;   // eight rows apart lie in different banks
+  float* const t = reinterpret_cast<float*>(raw);
+  const _Float16* own = KIND == kStep ? m.Q + (size_t)i * NP * m.q : m.P + (size_t)i * NP * m.p;
+  const size_t own_part = KIND == kStep ? m.q : m.p;
+  _Float16* out = m.out + (size_t)i * NP * m.o;
+  const bool end = KIND == kStep && m.end, twice = KIND != kStep && ti != tj;
+  for (int band = 0; band < TM; band += 64) {
+#pragma unroll
+    for (int x = 0; x < WR; ++x) {
+      const int rr = wr + 32 * x - band;   // lane: column l32 of a tile, rows 8 (e / 4) + 4 half + e % 4
+      if (rr < 0 || rr >= 64) continue;
+#pragma unroll
+      for (int y = 0; y < WC; ++y) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) t[(rr + 8 * (e / 4) + 4 * half + e % 4) * S + wc + 32 * y + l32] = acc[x][y][e];
+      }
+    }
+    __syncthreads();
+    for (int unit = threadIdx.x; unit < 64 * QC; unit += NT) {
+      const int rr = unit / QC, c = unit % QC * 8;
+      const size_t at = (size_t)(r0 + band + rr) * m.ld + c0 + c;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = t[rr * S + c + e] * m.mul;
+      if (KIND != kGram) {
+        H8 w[NP];
+#pragma unroll
+        for (int q = 0; q < NP; ++q) w[q] = *reinterpret_cast<const H8*>(own + q * own_part + at);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float x = (float)w[NP - 1][e];
+          if constexpr (NP == 2) x += (float)w[0][e];
+          v[e] = fmaf(m.own, x, v[e]);
+        }
+      }
+      if (end || twice) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[rr * S + c + e] = v[e];
+      }
+      if (!end) {
+        H8 w[NP];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          _Float16 p[NP];
+          split(v[e], p);
+#pragma unroll
+          for (int q = 0; q < NP; ++q) w[q][e] = p[q];
+        }
+#pragma unroll
+        for (int q = 0; q < NP; ++q) *reinterpret_cast<H8*>(out + q * m.o + at) = w[q];
+      }
+    }
+    __syncthreads();
+    if (twice) {
+      for (int unit = threadIdx.x; unit < 8 * TM; unit += NT) {
+        const int c = unit / 8, rr = unit % 8 * 8;
+        H8 w[NP];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          _Float16 p[NP];
+          split(t[(rr + e) * S + c], p);
+#pragma unroll
+          for (int q = 0; q < NP; ++q) w[q][e] = p[q];
+        }
+#pragma unroll
+        for (int q = 0; q < NP; ++q)
+          *reinterpret_cast<H8*>(out + q * m.o + (size_t)(c0 + c) * m.ld + r0 + band + rr) = w[q];
+      }
+    }
+    if (end) {
+      const bool down = m.last.sr < m.last.sc;   // along the result's adjacent elements
+      for (int cell = threadIdx.x; cell < 64 * TM; cell += NT) {
+        const int rr = down ? cell & 63 : cell / TM, c = down ? cell >> 6 : cell % TM;
+        if (r0 + band + rr < m.r && c0 + c < m.c) m.last.put(i, r0 + band + rr, c0 + c, t[rr * S + c]);
+      }
+    }
+    if (end || twice) __syncthreads();
   }
 }
 
+template <int NP, int TM, int KIND>
+hipError_t launch_mul(const Mul& m, const Layout& l, hipStream_t st) {
+  static std::atomic<uint64_t> done;
+  const size_t lds = Form<NP, TM>::kLds;
+  const hipError_t e = allow_lds(reinterpret_cast<const void*>(&ortho_mul_k<NP, TM, KIND>), lds, done);
+  if (e != hipSuccess) return e;
+  const int64_t tr = l.d.R / TM, tc = l.d.C / TM;
+  const dim3 grid((unsigned)(KIND == kStep ? tr * tc : tr * (tr + 1) / 2), (unsigned)l.d.n), block(Form<NP, TM>::kThreads);
+  hipLaunchKernelGGL((ortho_mul_k<NP, TM, KIND>), grid, block, lds, st, m);
+  return hipSuccess;
+}
+template <int NP, int KIND>
+hipError_t launch_mul(int tile, const Mul& m, const Layout& l, hipStream_t st) {
+  return tile == 256 ? launch_mul<NP, 256, KIND>(m, l, st)
+         : tile == 128 ? launch_mul<NP, 128, KIND>(m, l, st) : launch_mul<NP, 64, KIND>(m, l, st);
+}
+
+template <int NP>
+hipError_t steps_of(const OrthoArgs& a, const Layout& l, const Out& last, hipStream_t st) {
+  char* w = static_cast<char*>(a.work);
+  _Float16 *x = reinterpret_cast<_Float16*>(w + l.x0), *y = reinterpret_cast<_Float16*>(w + l.x1);
+  _Float16 *A = reinterpret_cast<_Float16*>(w + l.A), *B = reinterpret_cast<_Float16*>(w + l.B);
+  hipError_t e = hipSuccess;
+  for (int i = 0; i < a.c.steps && e == hipSuccess; ++i) {
+    Mul m{};
+    m.P = x; m.p = l.x; m.out = A; m.o = l.a; m.K = l.d.C; m.ld = l.d.R; m.mul = kDown;
+    if ((e = launch_mul<NP, kGram>(l.half, m, l, st)) != hipSuccess) break;
+    m.P = A; m.p = l.a; m.out = B; m.K = l.d.R; m.own = a.c.b; m.mul = a.c.c * kDown;
+    if ((e = launch_mul<NP, kPoly>(l.half, m, l, st)) != hipSuccess) break;
+    m.P = B; m.Q = x; m.q = l.x; m.out = y; m.o = l.x; m.ld = l.d.C; m.own = a.c.a; m.mul = kDown;
+    m.rows = l.d.R / l.whole; m.cols = l.d.C / l.whole; m.r = l.d.r; m.c = l.d.c; m.last = last; m.end = i + 1 == a.c.steps;
+    e = launch_mul<NP, kStep>(l.whole, m, l, st);
+    std::swap(x, y);
+  }
+  return e;
+}
+
 template <class E, int NP>
-void launch_typed(const OrthoArgs& a, hipStream_t st) {
+hipError_t launch_typed(const OrthoArgs& a, hipStream_t st) {
   const Layout l = layout_of(a.c);
   char* w = static_cast<char*>(a.work);
   double* sums = reinterpret_cast<double*>(w + l.sums);
@@ -348,12 +448,14 @@ void launch_typed(const OrthoArgs& a, hipStream_t st) {
   const View v = view_of(a.u, a.c);
   const Out out{a.out.data, a.out.stride_i, l.d.turned ? a.out.stride_c : a.out.stride_r,
                 l.d.turned ? a.out.stride_r : a.out.stride_c, a.c.dtype, a.c.scale * kDown};
-  hipLaunchKernelGGL(ortho_norm_k<E>, dim3(kNormParts, n), dim3(kNorm), 0, st, a.u.data, v, sums);
+  hipLaunchKernelGGL(ortho_norm_k<E>, dim3(l.sums_n, n), dim3(kNorm), 0, st, a.u.data, v, sums);
   hipLaunchKernelGGL((ortho_load_k<E, NP>), dim3((unsigned)((int64_t)(l.d.R / 64) * (l.d.C / 64)), n), dim3(256), 0, st, a.u.data, v,
-                     l.d, sums, (double)a.c.eps, x);
-  if (a.c.steps == 0) hipLaunchKernelGGL(ortho_store_k<NP>, dim3(l.d.r, n), dim3(256), 0, st, x, l.d, out);
-  else if (l.tile == 128) steps_of<NP, 128>(a, l, out, st);
-  else steps_of<NP, 64>(a, l, out, st);
+                     l.d, sums, l.sums_n, (double)a.c.eps, x);
+  if (a.c.steps == 0) {
+    hipLaunchKernelGGL(ortho_store_k<NP>, dim3(l.d.r, n), dim3(256), 0, st, x, l.d, out);
+    return hipSuccess;
+  }
+  return steps_of<NP>(a, l, out, st);
 }
 
 }  // namespace
@@ -361,10 +463,9 @@ void launch_typed(const OrthoArgs& a, hipStream_t st) {
 size_t ortho_bytes(const sim_ortho& c) { return c.n && c.M && c.N ? layout_of(c).bytes : 0; }
 
 hipError_t launch_ortho(const OrthoArgs& a, hipStream_t st) {
-  if (a.c.dtype == SIM_DT_F32) launch_typed<F32, 2>(a, st);
-  else if (a.c.dtype == SIM_DT_BF16) launch_typed<BF16, 1>(a, st);
-  else launch_typed<F16, 2>(a, st);
-  return hipGetLastError();
+  const hipError_t e = a.c.dtype == SIM_DT_F32 ? launch_typed<F32, 2>(a, st)
+                       : a.c.dtype == SIM_DT_BF16 ? launch_typed<BF16, 1>(a, st) : launch_typed<F16, 2>(a, st);
+  return e == hipSuccess ? hipGetLastError() : e;
 }
 
 }  // namespace bsim
