@@ -551,7 +551,7 @@ typedef struct sim_heads {
 
 /*  B, T    sequences, steps (below 2^30)
  *  H, Hk   heads of q and y, heads of k and v: Hk divides H, and heads [i H/Hk, (i+1) H/Hk) share
- *          the keys and values i (B H below 2^22, B T H below 2^40)
+ *          the keys and values i (B H below 2^21, B T H below 2^40)
  *  Dk, Dv  channels of q and k, of v and y: 1 to 256 each
  *  dtype   of q, k, v, y and their gradients (not SIM_DT_F64); states are fp32
  *  scale   finite                                                                         */

@@ -223,70 +223,82 @@ __device__ __forceinline__ Bf4 read_turned(const __bf16* p) {
 __device__ __forceinline__ Bf8 both(Bf4 a, Bf4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
 constexpr int kPad = 8;   // rows of LDS start four banks apart
-template <class E, int DQ, int NW, int C>
+template <class E, int DQ, int NW, int HV, int C>
 struct RunLds {
-  static constexpr int NI = PartsOf<E>::kIn, NC = PartsOf<E>::kMade, DV = 16 * NW;
+  static constexpr int NI = PartsOf<E>::kIn, NC = PartsOf<E>::kMade, DV = 16 * NW, TT = C / 16;
   __bf16 q[NI][C][DQ + kPad], k[NI][C][DQ + kPad], v[NI][C][DV + kPad], p[NC][C][C + kPad];
+  Fl4 half[HV > 1 ? NW : 1][HV][HV > 1 ? TT / HV : 1][HV > 1 ? 64 : 1];   // a half's sums that the other one needs
   float pow[C + 1], into[C];   // su l^i; su l^(m-1-j+lag)
 };
 
-// eight elements of a row from p on, of which `have` are there; zeros past its end
+// eight elements of a row from p on
 template <class T>
 struct Eight {
   typedef T Raw __attribute__((ext_vector_type(8), aligned(sizeof(T))));
   typedef T Val __attribute__((ext_vector_type(8)));
   Val v;
   __device__ __forceinline__ void load(const T* p) { v = __builtin_bit_cast(Val, *reinterpret_cast<const Raw*>(p)); }
-  __device__ __forceinline__ void load(const T* p, int have) {
-    if (have >= 8) {
-      load(p);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i < have ? p[i] : (T)0.0f;
-    }
-  }
 };
 
+// How much of a run there is: all; some steps or columns, the latter by whole eights; anything.
+enum { kAll = 0, kSome = 1, kOdd = 2 };
+
 // a run of C steps of one array, D columns, in registers between global memory and LDS: a thread's units of eight
-// are kRows steps apart
+// are kRows steps apart. What is not there is read elsewhere in the row or run, so that no load waits for a condition, and
+// becomes zero on its way to LDS.
 template <class E, int D, int C, int NT>
 struct Tile {
   typedef typename E::T T;
-  static constexpr int kUnits = C * D / 8, N = kUnits / NT, NI = PartsOf<E>::kIn, kRows = NT * 8 / D;
-  static_assert(kUnits % NT == 0 && NT * 8 % D == 0, "whole units");
+  static constexpr int kUnits = C * D / 8, N = (kUnits + NT - 1) / NT, NI = PartsOf<E>::kIn, kRows = NT * 8 / D;
+  static constexpr bool kPart = kUnits < NT;   // more threads than units: the last ones follow the last step
+  static_assert((kPart || kUnits % NT == 0) && NT * 8 % D == 0, "whole units");
   Eight<T> u[N];
   const T* p;
-  int64_t step;   // from one step to the next
-  int row, have;
+  __device__ static __forceinline__ int column() { return threadIdx.x % (D / 8) * 8; }
+  __device__ static __forceinline__ int row() {
+    const int i = threadIdx.x / (D / 8);
+    return kPart && i >= C ? C - 1 : i;
+  }
   // the next run starts at step i of the processing order; the array's columns from c0 on, `width` of them
   __device__ __forceinline__ void start(const AttnRun& r, const In& x, int b, int h, int64_t i, int64_t n, int c0, int width) {
-    const int c = threadIdx.x % (D / 8) * 8;
-    row = threadIdx.x / (D / 8);
-    have = width - c;
-    step = r.back ? -x.st : x.st;
-    p = row_of<T>(x, b, r.back ? n - 1 - i : i, h) + c0 + c + row * step;
+    const int64_t step = r.back ? -x.st : x.st;
+    p = row_of<T>(x, b, r.back ? n - 1 - i : i, h) + c0 + (column() < width ? column() : 0) + row() * step;
   }
-  template <bool WHOLE>
-  __device__ __forceinline__ void fetch(int now) {
+  // `now` steps, `step` elements from one to the next
+  template <int HOW>
+  __device__ __forceinline__ void fetch(int now, int64_t step, int width) {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const T* at = p + j * kRows * step;
-      if (WHOLE) {
-        u[j].load(at);
+      const int at = row() + j * kRows;
+      if (HOW == kAll) {
+        u[j].load(p + j * kRows * step);
       } else {
-        u[j].v = typename Eight<T>::Val{};
-        if (row + j * kRows < now && have > 0) u[j].load(at, have);
+        const T* q = p + ((at < now ? at : now - 1) - row()) * step;
+        if (HOW == kSome) {
+          u[j].load(q);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) u[j].v[i] = q[column() + i < width ? i : 0];
+        }
       }
     }
     p += C * step;
   }
   template <int S>
-  __device__ __forceinline__ void store(__bf16 (*lds)[C][S]) const {
-    const int c = threadIdx.x % (D / 8) * 8;
+  __device__ __forceinline__ void store(__bf16 (*lds)[C][S], bool all, int now, int width) {
+    const int c = column();
+    if (!all) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[j].v[i] = row() + j * kRows < now && c + i < width ? u[j].v[i] : (T)0.0f;
+      }
+    }
 #pragma unroll
     for (int j = 0; j < N; ++j) {
+      if (kPart && threadIdx.x >= kUnits) continue;
       if constexpr (NI == 1) {
-        *reinterpret_cast<typename Eight<T>::Val*>(&lds[0][row + j * kRows][c]) = u[j].v;
+        *reinterpret_cast<typename Eight<T>::Val*>(&lds[0][row() + j * kRows][c]) = u[j].v;
       } else {
         float x[8];
         __bf16 w[NI][8];
@@ -294,24 +306,27 @@ struct Tile {
         for (int e = 0; e < 8; ++e) x[e] = (float)u[j].v[e];
         split(x, w);
 #pragma unroll
-        for (int q = 0; q < NI; ++q) *reinterpret_cast<Bf8*>(&lds[q][row + j * kRows][c]) = packed(w[q]);
+        for (int q = 0; q < NI; ++q) *reinterpret_cast<Bf8*>(&lds[q][row() + j * kRows][c]) = packed(w[q]);
       }
     }
   }
 };
 
-// A workgroup takes a segment of a sequence and head and 16 columns of its state per wave, which hold them as
-// accumulators (lane: column lane % 16, rows 4 (lane / 16) + 0..3 of each tile of 16), so that two tiles are an operand
-// of the next product as they are. While a run is multiplied the next one's loads fly.
-template <class E, int DQ, int NW, int C, bool OUT>
-__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void attn_run_k(AttnRun r) {
+// A workgroup takes a segment of a sequence and head and 16 columns of its state per wave, or per HV waves that share its
+// rows, which hold them as accumulators (lane: column lane % 16, rows 4 (lane / 16) + 0..3 of each tile of 16), so that two
+// tiles are an operand of the next product as they are. While a run is multiplied the next one's loads fly. Bound by the
+// chains of the phases (LDS reads, conversions, products) where a SIMD has one wave, which is what the halves are for, by
+// HBM where there are many sequences and heads.
+template <class E, int DQ, int NW, int HV, int C, bool OUT>
+__global__ __launch_bounds__(64 * NW * HV, NW * HV == 4 ? 2 : 1) void attn_run_k(AttnRun r) {
   typedef typename E::T T;
-  typedef RunLds<E, DQ, NW, C> Lds;
-  constexpr int NI = Lds::NI, NC = Lds::NC, DV = Lds::DV, KT = DQ / 16, TT = C / 16, NT = 64 * NW;
+  typedef RunLds<E, DQ, NW, HV, C> Lds;
+  constexpr int NI = Lds::NI, NC = Lds::NC, DV = Lds::DV, KT = DQ / 16 / HV, TT = C / 16, NT = 64 * NW * HV, TO = TT / HV;
   extern __shared__ __align__(16) char raw[];
   Lds& m = *reinterpret_cast<Lds*>(raw);
   const int lane = threadIdx.x & 63, lc = lane & 15, lg = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // the same in all of a wave's lanes
+  const int any = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // the same in all of a wave's lanes
+  const int wave = any % NW, hv = any / NW, k0 = hv * KT;             // its columns, and its rows' first tile
   const int cols = (r.Dv + DV - 1) / DV;
   const int seg = blockIdx.y, c0 = blockIdx.x % cols * DV, bh = blockIdx.x / cols, h = bh % r.H, b = bh / r.H;
   const float l = decay_of(r, h);
@@ -331,7 +346,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void attn_run_k(AttnRun r
     const int c = c0 + wave * 16 + lc;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int row = kt * 16 + 4 * lg + i;
+      const int row = (k0 + kt) * 16 + 4 * lg + i;
       st[kt][i] = s0 && row < r.Dq && c < r.Dv ? s0[row * sr + c * sc] : 0.0f;
     }
   }
@@ -345,25 +360,29 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void attn_run_k(AttnRun r
   if (OUT) q.start(r, r.q, b, h, first, n, 0, r.Dq);
   k.start(r, r.k, b, h, first, n, 0, r.Dq);
   v.start(r, r.v, b, h, first, n, c0, width);
-  const bool full = r.Dq == DQ && width == DV;
+  const bool full = r.Dq == DQ && width == DV, eights = (r.Dq & 7) == 0 && (width & 7) == 0;
   auto fetch = [&](int64_t left) {
-    either(full && left >= C, [&](auto W) {
-      constexpr bool WHOLE = decltype(W)::value;
-      const int now = left < C ? (int)left : C;
-      if (OUT) q.template fetch<WHOLE>(now);
-      k.template fetch<WHOLE>(now);
-      v.template fetch<WHOLE>(now);
-    });
+    const int now = left < C ? (int)left : C;
+    auto go = [&](auto H) {
+      constexpr int HOW = decltype(H)::value;
+      if (OUT) q.template fetch<HOW>(now, r.back ? -r.q.st : r.q.st, r.Dq);
+      k.template fetch<HOW>(now, r.back ? -r.k.st : r.k.st, r.Dq);
+      v.template fetch<HOW>(now, r.back ? -r.v.st : r.v.st, width);
+    };
+    if (full && now == C) go(std::integral_constant<int, kAll>{});
+    else if (eights) go(std::integral_constant<int, kSome>{});
+    else go(std::integral_constant<int, kOdd>{});
   };
   const int64_t turn = r.back ? -r.ot : r.ot;   // of out, from one step to the next
   int64_t at0 = b * r.ob + (r.back ? n - 1 - first : first) * r.ot + h * r.oh + c0 + lc * turn + wave * 16 + 4 * lg;
-  fetch(live - first);
+  if (first < live) fetch(live - first);
   for (int64_t i0 = first; i0 < live; i0 += C) {
     const int now = live - i0 < C ? (int)(live - i0) : C;
     __syncthreads();
-    if (OUT) q.store(m.q);
-    k.store(m.k);
-    v.store(m.v);
+    const bool all = full && now == C;
+    if (OUT) q.store(m.q, all, now, r.Dq);
+    k.store(m.k, all, now, r.Dq);
+    v.store(m.v, all, now, width);
     if (threadIdx.x < C) {
       const int j = threadIdx.x;
       m.into[j] = j < now ? m.pow[now - 1 - j + r.lag] : 0.0f;
@@ -375,15 +394,15 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void attn_run_k(AttnRun r
       constexpr int kPairs = TT * TT / 2 + TT / 2 + (TT / 2);   // tiles of j <= i, and those beside them in a step of 32
       static_assert(TT % 2 == 0, "steps of 32");
 #pragma unroll
-      for (int w0 = 0; w0 < kPairs; w0 += NW) {
-        int at = w0 + wave, ti = 0;
+      for (int w0 = 0; w0 < kPairs; w0 += NW * HV) {
+        int at = w0 + any, ti = 0;
         // row of tiles ti has 2 (ti / 2 + 1) of them
 #pragma unroll
         for (int x = 0; x < TT - 1; ++x) {
           const int have = 2 * (x / 2 + 1);
           if (ti == x && at >= have) { at -= have; ++ti; }
         }
-        if (w0 + wave >= kPairs) continue;
+        if (w0 + any >= kPairs) continue;
         const int tj = at;
         Fl4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
         if (tj <= ti) {
@@ -414,7 +433,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void attn_run_k(AttnRun r
 #pragma unroll
       for (int t = 0; t < TT; ++t) acc[t] = Fl4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int kk = 0; kk < DQ / 32; ++kk) {
+      for (int kk = 0; kk < KT / 2; ++kk) {
         Bf8 s[NC];
         float w[8];
         __bf16 p[NC][8];
@@ -428,17 +447,26 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void attn_run_k(AttnRun r
           Bf8 x[NI];
 #pragma unroll
           for (int p = 0; p < NI; ++p) {
-            const __bf16* row = &m.q[p][16 * t + lc][32 * kk + 4 * lg];
+            const __bf16* row = &m.q[p][16 * t + lc][16 * k0 + 32 * kk + 4 * lg];
             x[p] = both(*reinterpret_cast<const Bf4*>(row), *reinterpret_cast<const Bf4*>(row + 16));
           }
           mul_parts(s, x, acc[t]);
         }
       }
 #pragma unroll
+      for (int t = 0; t < TT; ++t) acc[t] *= out_w[t];
+      // of the halves' sums each goes on with every HV-th tile
+      Fl4 y[TO];
+#pragma unroll
       for (int t = 0; t < TT; ++t) {
-        acc[t] *= out_w[t];
+        if (HV == 1 || t % HV == hv) y[t / HV] = acc[t];
+        else m.half[wave][t % HV][t / HV][lane] = acc[t];
       }
       __syncthreads();   // the weighted products are there
+      if constexpr (HV > 1) {
+#pragma unroll
+        for (int t = 0; t < TO; ++t) y[t] += m.half[wave][hv][t][lane];
+      }
 #pragma unroll
       for (int j = 0; j < C / 32; ++j) {
         Bf8 a[NI];
@@ -448,11 +476,12 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void attn_run_k(AttnRun r
           a[p] = both(read_turned(at), read_turned(at + 4 * (DV + kPad)));
         }
 #pragma unroll
-        for (int t = 2 * j; t < TT; ++t) {
+        for (int o = 2 * j / HV; o < TO; ++o) {   // tiles below the diagonal, those that stand on it in 32 x 32 among them
+          const int t = HV * o + hv;
           Bf8 x[NC];
 #pragma unroll
           for (int p = 0; p < NC; ++p) x[p] = *reinterpret_cast<const Bf8*>(&m.p[p][16 * t + lc][32 * j + 8 * lg]);
-          mul_parts(a, x, acc[t]);
+          mul_parts(a, x, y[o]);
         }
       }
       either(full && now == C && !r.wide, [&](auto W) {
@@ -460,17 +489,17 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void attn_run_k(AttnRun r
         typedef T Raw __attribute__((ext_vector_type(4), aligned(sizeof(T))));
         typedef T Val __attribute__((ext_vector_type(4)));
 #pragma unroll
-        for (int t = 0; t < TT; ++t) {
+        for (int o = 0; o < TO; ++o) {
+          const int t = HV * o + hv;
           const int64_t at = at0 + 16 * t * turn;
-          const Fl4 y = acc[t];
           if (WHOLE) {
-            *reinterpret_cast<Raw*>(static_cast<T*>(r.out) + at) = __builtin_bit_cast(Raw, __builtin_convertvector(y, Val));
+            *reinterpret_cast<Raw*>(static_cast<T*>(r.out) + at) = __builtin_bit_cast(Raw, __builtin_convertvector(y[o], Val));
           } else if (16 * t + lc < now) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               if (wave * 16 + 4 * lg + e >= width) continue;
-              if (r.wide) static_cast<float*>(r.out)[at + e] = y[e];
-              else static_cast<T*>(r.out)[at + e] = (T)y[e];
+              if (r.wide) static_cast<float*>(r.out)[at + e] = y[o][e];
+              else static_cast<T*>(r.out)[at + e] = (T)y[o][e];
             }
           }
         }
@@ -509,7 +538,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void attn_run_k(AttnRun r
         Bf8 a[NI];
 #pragma unroll
         for (int p = 0; p < NI; ++p) {
-          const __bf16* at = &m.k[p][32 * j + 8 * lg + lc / 4][16 * kt + 4 * (lc % 4)];
+          const __bf16* at = &m.k[p][32 * j + 8 * lg + lc / 4][16 * (k0 + kt) + 4 * (lc % 4)];
           a[p] = both(read_turned(at), read_turned(at + 4 * (DQ + kPad)));
         }
         mul_parts(a, x, st[kt]);
@@ -517,12 +546,16 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void attn_run_k(AttnRun r
     }
   }
   if (OUT) {   // padding
-    const int c = threadIdx.x % (DV / 8) * 8, row = threadIdx.x / (DV / 8);
-    for (int64_t i = (live > first ? live : first) + row; i < last; i += NT * 8 / DV) {
+    const int c = threadIdx.x % (DV / 8) * 8, row = threadIdx.x / (DV / 8), have = width - c;
+    for (int64_t i = (live > first ? live : first) + row; i < last && have > 0; i += NT * 8 / DV) {
       const int64_t at = b * r.ob + i * r.ot + h * r.oh + c0 + c;
+      if (!r.wide && have >= 8) {
+        *reinterpret_cast<typename Eight<T>::Raw*>(static_cast<T*>(r.out) + at) = typename Eight<T>::Raw{};
+        continue;
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if (c + e >= width) continue;
+        if (e >= have) continue;
         if (r.wide) static_cast<float*>(r.out)[at + e] = 0.0f;
         else static_cast<T*>(r.out)[at + e] = (T)0.0f;
       }
@@ -536,7 +569,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void attn_run_k(AttnRun r
     const int c = c0 + wave * 16 + lc;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int row = kt * 16 + 4 * lg + i;
+      const int row = (k0 + kt) * 16 + 4 * lg + i;
       if (row < r.Dq && c < r.Dv) to[row * sr + c * sc] = st[kt][i];
     }
   }
@@ -592,44 +625,57 @@ constexpr int kFew = 16;
 constexpr int run_steps(int dtype, int DQ) {   // of a run: as many as LDS holds of q, k, v and the products
   return (dtype == SIM_DT_F32 && DQ > 64) || (dtype == SIM_DT_F16 && DQ > 128) ? 32 : 64;
 }
-// Columns of a state per workgroup: 128 where two workgroups of 64 do not share a CU (their registers or LDS) or there are
-// enough sequences and heads for both; 64 otherwise, q and k read twice from L2 (bf16 8 x 2048 x 16 x 128: 64 132 us, 128
-// 147; 2 x 2048 x 16 x 256: 293, 184; fp16 4 x 2048 x 16 x 128: 178, 130).
-int run_columns(int dtype, int64_t B, int H, int Dq, int Dv) {
-  return Dv <= 64 || (Dq <= 128 && dtype != SIM_DT_F16 && B * H < 512) ? 64 : 128;
+// What a workgroup takes: columns of a state (128 by eight waves; 64 by four, or by eight that halve its rows), and a sequence's
+// steps or a segment of them, at the cost of reading k and v once more. By the sequences and heads there are and what their
+// registers leave room for, measured (us; bf16 but where stated):
+//   8 x 2048 x 16 heads x 128 (ragged)   64 148, halves 108, 128 154, halves in two segments 177
+//   32 x 2048 x 16 x 128                 64 393, halves 435, 128 339
+//   1 x 4096 x 16 x 128                  128 in 256 segments 54, halves 58, whole 290
+//   4 x 2048 x 16 x 128 fp16             128 in 256 segments 112, halves 140, whole 218
+//   4 x 1024 x 16 x 128 fp32             128 in 256 segments 92, halves 120, whole 148
+//   16 x 2048 x 16 x 64                  64 102, halves 85
+//   1 x 32768 x 8 x 64, a training step  64 in 512 segments 266, in 256 333, halves 319
+//   16 x 385 x 6 x 72 and 80 fp32, same  halves 242, 128 316, halves in segments 335
+//   2 x 2048 x 16 x 256                  halves 161
+struct Plan { int columns, halves, segs; };
+constexpr int kLeast = 256;   // steps of a segment
+Plan plan_of(int64_t B, int64_t T, int H, int Dq, int Dv) {
+  const int64_t heads = B * H;
+  Plan p{64, 1, 1};
+  if (T <= kFew || heads == 0) return p;
+  int fill = 0;   // workgroups that segments make
+  if (Dq > 128) { p.halves = 2; fill = 256; }
+  else if (Dv > 64 && (heads < 96 || heads >= 256)) { p.columns = 128; fill = heads < 96 ? 256 : 0; }
+  else if (Dv > 64) p.halves = 2;
+  else if (Dq > 64) { p.halves = 2; fill = heads < 128 ? 256 : 0; }
+  else if (heads < 128) fill = 512;
+  else if (heads < 384) p.halves = 2;
+  const int64_t groups = heads * ((Dv + p.columns - 1) / p.columns);
+  p.segs = (int)std::max<int64_t>(1, std::min<int64_t>((T + kLeast - 1) / kLeast, (fill + groups - 1) / groups));
+  return p;
 }
-// Time is split where workgroups are few, at the cost of reading k and v once more: below kSplit of them, into kFill segments
-// (fp32 16 x 385 x 6 x 80, 192 workgroups: whole 263 us, in two 317; bf16 1 x 32768 x 8 x 64 training step: 256 segments
-// 310, 512 258, 1024 328)
-constexpr int kSplit = 128, kFill = 512, kLeast = 256;
-int segments(int dtype, int64_t B, int64_t T, int H, int Dq, int Dv) {
-  const int wide = run_columns(dtype, B, H, Dq, Dv);
-  const int64_t groups = B * H * ((Dv + wide - 1) / wide);
-  if (T <= kFew || groups >= kSplit || groups == 0) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>((T + kLeast - 1) / kLeast, (kFill + groups - 1) / groups));
-}
-size_t parts_bytes(int dtype, int64_t B, int64_t T, int H, int Dq, int Dv) {
-  const int g = segments(dtype, B, T, H, Dq, Dv);
+size_t parts_bytes(int64_t B, int64_t T, int H, int Dq, int Dv) {
+  const int g = plan_of(B, T, H, Dq, Dv).segs;
   return g > 1 ? (size_t)B * H * g * Dq * Dv * sizeof(float) : 0;
 }
 
-template <class E, int DQ, int NW, int C>
+template <class E, int DQ, int NW, int HV, int C>
 hipError_t launch_runs(AttnRun r, int64_t B, hipStream_t st) {
-  typedef RunLds<E, DQ, NW, C> Lds;
+  typedef RunLds<E, DQ, NW, HV, C> Lds;
   static std::atomic<uint64_t> done[2];
-  hipError_t e = allow_lds(reinterpret_cast<const void*>(&attn_run_k<E, DQ, NW, C, true>), sizeof(Lds), done[0]);
-  if (e == hipSuccess) e = allow_lds(reinterpret_cast<const void*>(&attn_run_k<E, DQ, NW, C, false>), sizeof(Lds), done[1]);
+  hipError_t e = allow_lds(reinterpret_cast<const void*>(&attn_run_k<E, DQ, NW, HV, C, true>), sizeof(Lds), done[0]);
+  if (e == hipSuccess) e = allow_lds(reinterpret_cast<const void*>(&attn_run_k<E, DQ, NW, HV, C, false>), sizeof(Lds), done[1]);
   if (e != hipSuccess) return e;
   const int cols = (r.Dv + Lds::DV - 1) / Lds::DV;
-  const dim3 grid((unsigned)(B * r.H * cols), r.segs), block(64 * NW);
+  const dim3 grid((unsigned)(B * r.H * cols), r.segs), block(64 * NW * HV);
   if (r.segs > 1) {
-    hipLaunchKernelGGL((attn_run_k<E, DQ, NW, C, false>), grid, block, sizeof(Lds), st, r);
+    hipLaunchKernelGGL((attn_run_k<E, DQ, NW, HV, C, false>), grid, block, sizeof(Lds), st, r);
     hipLaunchKernelGGL(attn_join_k, dim3((r.Dq * r.Dv + 255) / 256, (unsigned)(B * r.H)), dim3(256), 0, st, r);
     r.err = nullptr;
     if (!r.out) return hipSuccess;
   }
-  if (r.out) hipLaunchKernelGGL((attn_run_k<E, DQ, NW, C, true>), grid, block, sizeof(Lds), st, r);
-  else hipLaunchKernelGGL((attn_run_k<E, DQ, NW, C, false>), grid, block, sizeof(Lds), st, r);
+  if (r.out) hipLaunchKernelGGL((attn_run_k<E, DQ, NW, HV, C, true>), grid, block, sizeof(Lds), st, r);
+  else hipLaunchKernelGGL((attn_run_k<E, DQ, NW, HV, C, false>), grid, block, sizeof(Lds), st, r);
   return hipSuccess;
 }
 
@@ -643,7 +689,8 @@ hipError_t launch_run(AttnRun r, int64_t B, float* parts, hipStream_t st) {
     else hipLaunchKernelGGL((attn_step_k<E, 16>), grid, block, 0, st, r);
     return hipSuccess;
   }
-  r.segs = segments(dt, B, r.T, r.H, r.Dq, r.Dv);
+  const Plan plan = plan_of(B, r.T, r.H, r.Dq, r.Dv);
+  r.segs = plan.segs;
   r.seg = r.T;
   if (r.segs > 1) {   // whole runs
     const int64_t each = (r.T + r.segs - 1) / r.segs;
@@ -651,10 +698,12 @@ hipError_t launch_run(AttnRun r, int64_t B, float* parts, hipStream_t st) {
     r.segs = (int)((r.T + r.seg - 1) / r.seg);
     r.parts = parts;
   }
-  const bool wide = run_columns(dt, B, r.H, r.Dq, r.Dv) == 128;
-  if (r.Dq > 128) return wide ? launch_runs<E, 256, 8, run_steps(dt, 256)>(r, B, st) : launch_runs<E, 256, 4, run_steps(dt, 256)>(r, B, st);
-  if (r.Dq > 64) return wide ? launch_runs<E, 128, 8, run_steps(dt, 128)>(r, B, st) : launch_runs<E, 128, 4, run_steps(dt, 128)>(r, B, st);
-  return wide ? launch_runs<E, 64, 8, run_steps(dt, 64)>(r, B, st) : launch_runs<E, 64, 4, run_steps(dt, 64)>(r, B, st);
+  constexpr int C64 = run_steps(dt, 64), C128 = run_steps(dt, 128), C256 = run_steps(dt, 256);
+  if (r.Dq > 128) return launch_runs<E, 256, 4, 2, C256>(r, B, st);
+  if (r.Dq > 64)
+    return plan.columns == 128 ? launch_runs<E, 128, 8, 1, C128>(r, B, st) : launch_runs<E, 128, 4, 2, C128>(r, B, st);
+  return plan.columns == 128 ? launch_runs<E, 64, 8, 1, C64>(r, B, st)
+         : plan.halves == 2 ? launch_runs<E, 64, 4, 2, C64>(r, B, st) : launch_runs<E, 64, 4, 1, C64>(r, B, st);
 }
 
 In in_of(const sim_heads& x, int share) { return In{x.data, x.stride_b, x.stride_t, x.stride_h, share}; }
@@ -734,8 +783,8 @@ hipError_t launch_typed(const AttnArgs& a, bool grad, hipStream_t st) {
 }  // namespace
 
 size_t attn_work_bytes(const sim_linear_attn& c, bool grad) {
-  size_t parts = parts_bytes(c.dtype, c.B, c.T, c.H, c.Dk, c.Dv);
-  if (grad) parts = std::max(parts, parts_bytes(c.dtype, c.B, c.T, c.H, c.Dv, c.Dk));
+  size_t parts = parts_bytes(c.B, c.T, c.H, c.Dk, c.Dv);
+  if (grad) parts = std::max(parts, parts_bytes(c.B, c.T, c.H, c.Dv, c.Dk));
   return share_cells(c, grad) * sizeof(float) + parts;
 }
 

@@ -197,9 +197,9 @@ int check_attn(const sim_linear_attn* s, const char* who) {
   if (s->Dk < 1 || s->Dv < 1) return op_fail(SIM_EINVAL, "%s: Dk and Dv must be >= 1", who);
   if (s->Dk > 256 || s->Dv > 256) return op_fail(SIM_EUNSUPPORTED, "%s: Dk and Dv go up to 256", who);
   if (!(s->scale - s->scale == 0.0f)) return op_fail(SIM_EINVAL, "%s: scale must be finite", who);
-  if (s->T >= (1 << 30) || s->B >= (1 << 22) || s->B * s->H >= (1 << 22) ||
+  if (s->T >= (1 << 30) || s->B >= (1 << 21) || s->B * s->H >= (1 << 21) ||
       (__int128)s->B * s->T * s->H >= ((__int128)1 << 40))
-    return op_fail(SIM_EUNSUPPORTED, "%s: T must stay below 2^30, B*H below 2^22, B*T*H below 2^40", who);
+    return op_fail(SIM_EUNSUPPORTED, "%s: T must stay below 2^30, B*H below 2^21, B*T*H below 2^40", who);
   return SIM_OK;
 }
 

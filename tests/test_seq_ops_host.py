@@ -103,7 +103,7 @@ def accepted(stub, good):
 def test_linear_attn_refusals(stub):
     f, g = "linear_attn", "linear_attn_grad"
     refused(stub, [
-        (">= 0", call(f, dict(B=-1))), (">= 0", call(f, dict(T=-1))), ("2^30", call(f, dict(T=1 << 30))), ("2^22", call(f, dict(B=1 << 20))),
+        (">= 0", call(f, dict(B=-1))), (">= 0", call(f, dict(T=-1))), ("2^30", call(f, dict(T=1 << 30))), ("2^21", call(f, dict(B=1 << 19))),
         ("divide", call(f, dict(H=3))), ("divide", call(f, dict(Hk=0))), ("divide", call(f, dict(H=0))), (">= 1", call(f, dict(Dk=0))),
         ("256", call(f, dict(Dk=257))), ("256", call(f, dict(Dv=257))), ("scale", call(f, dict(scale=float("nan")))),
         ("scale", call(f, dict(scale=float("inf")))), ("q is NULL", call(f, a0=None)), ("k is NULL", call(f, a1=None)),
@@ -154,7 +154,7 @@ def test_every_size_launches_within_limits(stub):
     calls = []
     for name, (B, T, H, Hk), (Dk, Dv), dt in itertools.product(
             ("linear_attn", "linear_attn_grad"),
-            [(1, 1, 1, 1), (64, 1, 16, 4), (8, 2048, 16, 4), (1, 32768, 8, 8), ((1 << 22) - 1, 1, 1, 1), ((1 << 22) - 1, 17, 1, 1), (3, 17, 1 << 20, 1 << 10), (1, (1 << 30) - 1, 2, 1),
+            [(1, 1, 1, 1), (64, 1, 16, 4), (8, 2048, 16, 4), (1, 32768, 8, 8), ((1 << 21) - 1, 1, 1, 1), ((1 << 21) - 1, 17, 1, 1), (3, 17, 1 << 19, 1 << 10), (1, (1 << 30) - 1, 2, 1),
              (1, 1 << 20, 64, 64), (2, 5, 1, 1), (2, 0, 3, 1), (40000, 20, 2, 2)],
             [(1, 1), (64, 64), (128, 128), (256, 256), (256, 1), (33, 200)], (1, 2, 3)):
         h = lambda i, n, d: [P + (i << 42), T * n * d, n * d, d]   # noqa: E731
