@@ -18,6 +18,7 @@ namespace {
 
 typedef _Float16 H8 __attribute__((ext_vector_type(8)));
 typedef _Float16 H4 __attribute__((ext_vector_type(4)));
+typedef float Fl4 __attribute__((ext_vector_type(4)));
 typedef float F16x __attribute__((ext_vector_type(16)));
 
 constexpr float kUp = 1024.0f, kDown = 1.0f / 1024.0f;   // of what is held
@@ -32,9 +33,10 @@ struct Layout {
   int half, whole, parts;      // tiles of the symmetric products and of X
   int sums_n;                  // workgroups that add up squares of a matrix
   size_t x, a;                 // elements of a part of one matrix
-  size_t sums, x0, x1, A, B, bytes;   // offsets in bytes
+  size_t sums, x0, x1, A, B, parts_at, bytes;   // offsets in bytes
+  int split;                   // parts of X X^T's sum over K, each by workgroups of its own
 };
-constexpr int kNorm = 256;
+constexpr int kNorm = 256, kFillTiles = 512, kShare = 512;
 int round_up(int v, int to) { return (v + to - 1) / to * to; }
 // The largest tile of which there are enough to fill the chip (256: a workgroup on each CU, of 128 and 64 several), measured
 // (us, tiles of the symmetric products / of X):
@@ -67,7 +69,12 @@ Layout layout_of(const sim_ortho& o) {
   l.x1 = l.x0 + n * l.x * e;
   l.A = l.x1 + n * l.x * e;
   l.B = l.A + n * l.a * e;
-  l.bytes = l.B + n * l.a * e;
+  l.parts_at = (l.B + n * l.a * e + 15) / 16 * 16;
+  // Few tiles and many columns: K in shares of at least kShare (us, whole and in shares: bf16 64 x 16384 503, 101; 1024 x 16384
+  // 812, 588; 768 x 2048 190, 169; fp32 2 x 40 x 4000 256, 117)
+  const int64_t k = l.d.R / l.half, tiles = n * k * (k + 1) / 2;
+  l.split = (int)std::max<int64_t>(1, std::min<int64_t>(kFillTiles / tiles, l.d.C / kShare));
+  l.bytes = l.parts_at + (l.split > 1 ? n * l.split * l.a * sizeof(float) : 0);
   return l;
 }
 
@@ -188,6 +195,7 @@ struct Mul {
   int K, rows, cols;  // tiles of the result
   int ld;             // of out and Q
   float own, mul;     // the result is own * (P or Q) + mul * product, as it is held
+  float* parts;       // kGram, shares of K: their sums
   Out last;           // kStep: where the last step goes
   int r, c;
   bool end;
@@ -225,9 +233,16 @@ __global__ __launch_bounds__(threads_of(TM), TM == 256 ? 1 : 2) void ortho_mul_k
     while (ti * (ti + 1) / 2 > id) --ti;
     tj = id - ti * (ti + 1) / 2;
   }
-  const int i = blockIdx.y, r0 = ti * TM, c0 = tj * TM, K = m.K;
-  const _Float16* P = m.P + (size_t)i * NP * m.p + (size_t)r0 * K;
-  const _Float16* Q = KIND == kStep ? m.Q + (size_t)i * NP * m.q + c0 : m.P + (size_t)i * NP * m.p + (size_t)c0 * K;
+  const int i = blockIdx.y, r0 = ti * TM, c0 = tj * TM, ldk = m.K;
+  const bool shares = KIND == kGram && gridDim.z > 1;
+  int K = ldk, from = 0;   // the steps of BK that are this workgroup's
+  if (shares) {
+    const int all_k = ldk / BK;
+    from = (int)((int64_t)all_k * blockIdx.z / gridDim.z) * BK;
+    K = (int)((int64_t)all_k * (blockIdx.z + 1) / gridDim.z) * BK - from;
+  }
+  const _Float16* P = m.P + (size_t)i * NP * m.p + (size_t)r0 * ldk + from;
+  const _Float16* Q = KIND == kStep ? m.Q + (size_t)i * NP * m.q + c0 : m.P + (size_t)i * NP * m.p + (size_t)c0 * ldk + from;
   struct Stage { H8 p[NP][U], q[NP][U]; };
   Stage in[AHEAD];
   auto fetch = [&](Stage& g, int k0) {
@@ -236,9 +251,9 @@ __global__ __launch_bounds__(threads_of(TM), TM == 256 ? 1 : 2) void ortho_mul_k
       const int unit = threadIdx.x + u * NT, row = unit / CH, ch = unit % CH;
 #pragma unroll
       for (int q = 0; q < NP; ++q) {
-        g.p[q][u] = *reinterpret_cast<const H8*>(P + q * m.p + (size_t)row * K + k0 + ch * 8);
+        g.p[q][u] = *reinterpret_cast<const H8*>(P + q * m.p + (size_t)row * ldk + k0 + ch * 8);
         if (KIND == kStep) g.q[q][u] = *reinterpret_cast<const H8*>(Q + q * m.q + (size_t)(k0 + unit / QC) * m.ld + unit % QC * 8);
-        else g.q[q][u] = *reinterpret_cast<const H8*>(Q + q * m.p + (size_t)row * K + k0 + ch * 8);
+        else g.q[q][u] = *reinterpret_cast<const H8*>(Q + q * m.p + (size_t)row * ldk + k0 + ch * 8);
       }
     }
   };
@@ -326,7 +341,7 @@ __global__ __launch_bounds__(threads_of(TM), TM == 256 ? 1 : 2) void ortho_mul_k
   const _Float16* own = KIND == kStep ? m.Q + (size_t)i * NP * m.q : m.P + (size_t)i * NP * m.p;
   const size_t own_part = KIND == kStep ? m.q : m.p;
   _Float16* out = m.out + (size_t)i * NP * m.o;
-  const bool end = KIND == kStep && m.end, twice = KIND != kStep && ti != tj;
+  const bool end = KIND == kStep && m.end, twice = KIND != kStep && ti != tj && !shares;
   for (int band = 0; band < TM; band += 64) {
 #pragma unroll
     for (int x = 0; x < WR; ++x) {
@@ -345,6 +360,12 @@ __global__ __launch_bounds__(threads_of(TM), TM == 256 ? 1 : 2) void ortho_mul_k
       float v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = t[rr * S + c + e] * m.mul;
+      if (shares) {
+        Fl4* to = reinterpret_cast<Fl4*>(m.parts + ((size_t)i * gridDim.z + blockIdx.z) * m.o + at);
+        to[0] = Fl4{v[0], v[1], v[2], v[3]};
+        to[1] = Fl4{v[4], v[5], v[6], v[7]};
+        continue;
+      }
       if (KIND != kGram) {
         H8 w[NP];
 #pragma unroll
@@ -401,6 +422,45 @@ __global__ __launch_bounds__(threads_of(TM), TM == 256 ? 1 : 2) void ortho_mul_k
   }
 }
 
+// The shares' sums, in order, to A's parts: 16 x 64 at once, on and below the diagonal, and turned.
+template <int NP>
+__global__ __launch_bounds__(256) void ortho_sum_k(const float* in, int shares, _Float16* out, int R, int half) {
+  __shared__ float t[16][65];
+  const int tiles = R / 64, r0 = blockIdx.x / tiles * 16, c0 = blockIdx.x % tiles * 64;
+  if (r0 / half < c0 / half) return;   // formed turned (by tiles of `half`, as they are there)
+  const size_t cells = (size_t)R * R;
+  in += (size_t)blockIdx.y * shares * cells;
+  out += (size_t)blockIdx.y * NP * cells;
+  const int row = threadIdx.x >> 4, c = (threadIdx.x & 15) * 4;
+  const size_t at = (size_t)(r0 + row) * R + c0 + c;
+  Fl4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+  for (int z = 0; z < shares; ++z) s += *reinterpret_cast<const Fl4*>(in + z * cells + at);
+  H4 w[NP];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    _Float16 p[NP];
+    split(s[e], p);
+    t[row][c + e] = s[e];
+#pragma unroll
+    for (int q = 0; q < NP; ++q) w[q][e] = p[q];
+  }
+#pragma unroll
+  for (int q = 0; q < NP; ++q) *reinterpret_cast<H4*>(out + q * cells + at) = w[q];
+  if (r0 / half == c0 / half) return;
+  __syncthreads();
+  const int col = threadIdx.x >> 2, rr = (threadIdx.x & 3) * 4;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    _Float16 p[NP];
+    split(t[rr + e][col], p);
+#pragma unroll
+    for (int q = 0; q < NP; ++q) w[q][e] = p[q];
+  }
+#pragma unroll
+  for (int q = 0; q < NP; ++q) *reinterpret_cast<H4*>(out + q * cells + (size_t)(c0 + col) * R + r0 + rr) = w[q];
+}
+
 template <int NP, int TM, int KIND>
 hipError_t launch_mul(const Mul& m, const Layout& l, hipStream_t st) {
   static std::atomic<uint64_t> done;
@@ -408,7 +468,8 @@ hipError_t launch_mul(const Mul& m, const Layout& l, hipStream_t st) {
   const hipError_t e = allow_lds(reinterpret_cast<const void*>(&ortho_mul_k<NP, TM, KIND>), lds, done);
   if (e != hipSuccess) return e;
   const int64_t tr = l.d.R / TM, tc = l.d.C / TM;
-  const dim3 grid((unsigned)(KIND == kStep ? tr * tc : tr * (tr + 1) / 2), (unsigned)l.d.n), block(Form<NP, TM>::kThreads);
+  const dim3 grid((unsigned)(KIND == kStep ? tr * tc : tr * (tr + 1) / 2), (unsigned)l.d.n,
+                  KIND == kGram ? l.split : 1), block(Form<NP, TM>::kThreads);
   hipLaunchKernelGGL((ortho_mul_k<NP, TM, KIND>), grid, block, lds, st, m);
   return hipSuccess;
 }
@@ -427,7 +488,11 @@ hipError_t steps_of(const OrthoArgs& a, const Layout& l, const Out& last, hipStr
   for (int i = 0; i < a.c.steps && e == hipSuccess; ++i) {
     Mul m{};
     m.P = x; m.p = l.x; m.out = A; m.o = l.a; m.K = l.d.C; m.ld = l.d.R; m.mul = kDown;
+    m.parts = reinterpret_cast<float*>(w + l.parts_at);
     if ((e = launch_mul<NP, kGram>(l.half, m, l, st)) != hipSuccess) break;
+    if (l.split > 1)
+      hipLaunchKernelGGL(ortho_sum_k<NP>, dim3((unsigned)((int64_t)(l.d.R / 64) * (l.d.R / 16)), (unsigned)l.d.n), dim3(256), 0, st, m.parts,
+                         l.split, A, l.d.R, l.half);
     m.P = A; m.p = l.a; m.out = B; m.K = l.d.R; m.own = a.c.b; m.mul = a.c.c * kDown;
     if ((e = launch_mul<NP, kPoly>(l.half, m, l, st)) != hipSuccess) break;
     m.P = B; m.Q = x; m.q = l.x; m.out = y; m.o = l.x; m.ld = l.d.C; m.own = a.c.a; m.mul = kDown;
