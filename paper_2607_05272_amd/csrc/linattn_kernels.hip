@@ -238,10 +238,27 @@ struct Eight {
   typedef T Val __attribute__((ext_vector_type(8)));
   Val v;
   __device__ __forceinline__ void load(const T* p) { v = __builtin_bit_cast(Val, *reinterpret_cast<const Raw*>(p)); }
+  // the elements from n on (n <= 0: all), then zeros
+  __device__ __forceinline__ void skip(int n) {
+    constexpr int W = sizeof(Val) / 4, each = 8 / W;   // words, elements of one
+    typedef uint32_t Words __attribute__((ext_vector_type(W)));
+    Words w = __builtin_bit_cast(Words, v);
+    n = n < 0 ? 0 : n;
+#pragma unroll
+    for (int bit = 4; bit >= each; bit /= 2) {
+#pragma unroll
+      for (int i = 0; i < W; ++i) w[i] = n & bit ? (i + bit / each < W ? w[i + bit / each] : 0u) : w[i];
+    }
+    if constexpr (each == 2) {
+#pragma unroll
+      for (int i = 0; i < W; ++i) w[i] = n & 1 ? __builtin_amdgcn_alignbit(i + 1 < W ? w[i + 1] : 0u, w[i], 16) : w[i];
+    }
+    v = __builtin_bit_cast(Val, w);
+  }
 };
 
-// How much of a run there is: all; some steps or columns, the latter by whole eights; anything.
-enum { kAll = 0, kSome = 1, kOdd = 2 };
+// How much of a run there is: all; some steps or columns, of those eight at least; fewer.
+enum { kAll = 0, kSome = 1, kFewer = 2 };
 
 // a run of C steps of one array, D columns, in registers between global memory and LDS: a thread's units of eight
 // are kRows steps apart. What is not there is read elsewhere in the row or run, so that no load waits for a condition, and
@@ -262,7 +279,8 @@ struct Tile {
   // the next run starts at step i of the processing order; the array's columns from c0 on, `width` of them
   __device__ __forceinline__ void start(const AttnRun& r, const In& x, int b, int h, int64_t i, int64_t n, int c0, int width) {
     const int64_t step = r.back ? -x.st : x.st;
-    p = row_of<T>(x, b, r.back ? n - 1 - i : i, h) + c0 + (column() < width ? column() : 0) + row() * step;
+    const int c = column(), from = c >= width ? 0 : (c + 8 > width && width >= 8 ? width - 8 : c);   // the last ones end with the row
+    p = row_of<T>(x, b, r.back ? n - 1 - i : i, h) + c0 + from + row() * step;
   }
   // `now` steps, `step` elements from one to the next
   template <int HOW>
@@ -274,7 +292,7 @@ struct Tile {
         u[j].load(p + j * kRows * step);
       } else {
         const T* q = p + ((at < now ? at : now - 1) - row()) * step;
-        if (HOW == kSome) {
+        if (HOW == kSome || width >= 8) {
           u[j].load(q);
         } else {
 #pragma unroll
@@ -288,11 +306,19 @@ struct Tile {
   __device__ __forceinline__ void store(__bf16 (*lds)[C][S], bool all, int now, int width) {
     const int c = column();
     if (!all) {
+      if ((width & 7) && width >= 8) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
+        for (int j = 0; j < N; ++j) u[j].skip(c + 8 - width);   // the last ones end with the row
+      } else if (width < 8) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) u[j].v[i] = row() + j * kRows < now && c + i < width ? u[j].v[i] : (T)0.0f;
+        for (int j = 0; j < N; ++j) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) u[j].v[i] = c + i < width ? u[j].v[i] : (T)0.0f;
+        }
       }
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (row() + j * kRows >= now || c >= width) u[j].v = typename Eight<T>::Val{};
     }
 #pragma unroll
     for (int j = 0; j < N; ++j) {
@@ -360,7 +386,7 @@ __global__ __launch_bounds__(64 * NW * HV, NW * HV == 4 ? 2 : 1) void attn_run_k
   if (OUT) q.start(r, r.q, b, h, first, n, 0, r.Dq);
   k.start(r, r.k, b, h, first, n, 0, r.Dq);
   v.start(r, r.v, b, h, first, n, c0, width);
-  const bool full = r.Dq == DQ && width == DV, eights = (r.Dq & 7) == 0 && (width & 7) == 0;
+  const bool full = r.Dq == DQ && width == DV, eights = r.Dq >= 8 && width >= 8;
   auto fetch = [&](int64_t left) {
     const int now = left < C ? (int)left : C;
     auto go = [&](auto H) {
@@ -371,7 +397,7 @@ __global__ __launch_bounds__(64 * NW * HV, NW * HV == 4 ? 2 : 1) void attn_run_k
     };
     if (full && now == C) go(std::integral_constant<int, kAll>{});
     else if (eights) go(std::integral_constant<int, kSome>{});
-    else go(std::integral_constant<int, kOdd>{});
+    else go(std::integral_constant<int, kFewer>{});
   };
   const int64_t turn = r.back ? -r.ot : r.ot;   // of out, from one step to the next
   int64_t at0 = b * r.ob + (r.back ? n - 1 - first : first) * r.ot + h * r.oh + c0 + lc * turn + wave * 16 + 4 * lg;
