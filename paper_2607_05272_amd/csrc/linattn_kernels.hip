@@ -669,7 +669,7 @@ Plan plan_of(int64_t B, int64_t T, int H, int Dq, int Dv) {
   const int64_t heads = B * H;
   Plan p{64, 1, 1};
   if (T <= kFew || heads == 0) return p;
-  int fill = 0;   // workgroups that segments make
+  int fill = 0;   // workgroups that are resident at once: segments make no more
   if (Dq > 128) { p.halves = 2; fill = 256; }
   else if (Dv > 64 && (heads < 96 || heads >= 256)) { p.columns = 128; fill = heads < 96 ? 256 : 0; }
   else if (Dv > 64) p.halves = 2;
@@ -677,7 +677,7 @@ Plan plan_of(int64_t B, int64_t T, int H, int Dq, int Dv) {
   else if (heads < 128) fill = 512;
   else if (heads < 384) p.halves = 2;
   const int64_t groups = heads * ((Dv + p.columns - 1) / p.columns);
-  p.segs = (int)std::max<int64_t>(1, std::min<int64_t>((T + kLeast - 1) / kLeast, (fill + groups - 1) / groups));
+  p.segs = (int)std::max<int64_t>(1, std::min<int64_t>((T + kLeast - 1) / kLeast, fill / groups));
   return p;
 }
 size_t parts_bytes(int64_t B, int64_t T, int H, int Dq, int Dv) {
