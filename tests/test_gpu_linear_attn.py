@@ -155,6 +155,100 @@ def test_state_in_place_and_runs_that_follow_each_other(sim, T):
     ac.check_forward(d, None, only)
 
 
+def reference(d, grad=True):
+    """The steps taken by torch in fp64 on the GPU: y, state and (dq, dk, dv, ds0), with the sums of their terms'
+    magnitudes."""
+    def run(q, k, v, l, dy, s0, ds, n, scale):
+        B, T, H, Dk = q.shape
+        g = H // k.shape[2]
+        S, G = s0.clone(), ds.clone()
+        l = l[:, None, None]
+        y, dq = torch.zeros_like(dy), torch.zeros_like(q)
+        dk, dv = torch.zeros_like(q), torch.zeros_like(dy)
+        for t in range(T):
+            on = (t < n)[:, None, None, None]
+            kt, vt = k[:, t].repeat_interleave(g, 1), v[:, t].repeat_interleave(g, 1)
+            S = torch.where(on, l * S + kt[..., None] * vt[..., None, :], S)
+            y[:, t] = torch.where(on[..., 0], scale * (q[:, t][..., None] * S).sum(2), 0.0)
+            dq[:, t] = torch.where(on[..., 0], scale * (S * dy[:, t][..., None, :]).sum(3), 0.0)
+        for t in reversed(range(T) if grad else range(0)):
+            on = (t < n)[:, None, None, None]
+            kt, vt = k[:, t].repeat_interleave(g, 1), v[:, t].repeat_interleave(g, 1)
+            Gt = G + scale * q[:, t][..., None] * dy[:, t][..., None, :]
+            dk[:, t] = torch.where(on[..., 0], (Gt * vt[..., None, :]).sum(3), 0.0)
+            dv[:, t] = torch.where(on[..., 0], (Gt * kt[..., None]).sum(2), 0.0)
+            G = torch.where(on, l * Gt, G)
+        share = lambda x: x.unflatten(2, (H // g, g)).sum(3)   # noqa: E731
+        return y, S, dq, share(dk), share(dv), G
+    a = [d[x].double() for x in ("q", "k", "v", "decay", "dy", "s0", "dstate")]
+    n = d["lengths"] if d["lengths"] is not None else torch.full((d["q"].shape[0],), d["q"].shape[1], device="cuda")
+    return run(*a, n, d["scale"]), run(*(x.abs() for x in a), n, abs(d["scale"]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32", "f16"])
+@pytest.mark.parametrize("B,T,H,Hk,Dk,Dv,lengths", [
+    (2, 2500, 2, 1, 64, 64, True), (1, 3000, 1, 1, 128, 128, False), (1, 1111, 3, 1, 200, 96, False), (3, 700, 2, 2, 48, 130, True),
+    (40, 70, 4, 2, 64, 64, True), (100, 40, 4, 4, 128, 128, False), (70, 100, 4, 1, 100, 120, True), (130, 33, 3, 3, 64, 40, True),
+    (5, 600, 1, 1, 256, 256, True), (7000, 20, 2, 1, 8, 8, True), (30000, 3, 1, 1, 16, 16, True)])
+def test_segments_and_many_sequences(sim, B, T, H, Hk, Dk, Dv, lengths, dtype):
+    """Every form of a run: time in segments, 64 and 128 columns, halves, more sequences than the chip holds."""
+    if B * T * H * max(Dk, Dv) > 1 << 22 and dtype == "f16":
+        pytest.skip("the types share their forms")
+    d = cuda(ac.inputs(B, T, H, Hk, Dk, Dv, TYPES[dtype], T, lengths=lengths))
+    y, state = sim.linear_attn(d["q"], d["k"], d["v"], d["decay"], d["s0"], d["lengths"], d["scale"])
+    g = sim.linear_attn_grad(d["q"], d["k"], d["v"], d["decay"], d["dy"], d["s0"], d["dstate"], d["lengths"], d["scale"])
+    sim.sync()
+    want, size = reference(d)
+    D = max(Dk, Dv) + H // Hk
+    for name, got, w, m in zip(("y", "state", "dq", "dk", "dv", "ds0"), (y, state, *g), want, size):
+        e = ac._loss(got.dtype, T, D)
+        tol = e * m + torch.finfo(got.dtype).eps / 2 * w.abs() + torch.finfo(got.dtype).smallest_normal * torch.finfo(got.dtype).eps
+        off = ~((got.double() - w).abs() <= tol)
+        assert not off.any(), (name, int(off.sum()), off.nonzero()[0].tolist())
+
+
+def test_single_outputs_of_the_entry_points(sim):
+    """Through the C entry points: each gradient alone is what it is with the others; nothing else is read or written."""
+    import ctypes as C
+    from paper_2607_05272_amd import _lib as L
+    from paper_2607_05272_amd.sim import _heads
+    for T in (5, 100, 700):
+        d = cuda(ac.inputs(2, T, 4, 2, 32, 48, torch.bfloat16, 15))
+        all_of = sim.linear_attn_grad(d["q"], d["k"], d["v"], d["decay"], d["dy"], d["s0"], d["dstate"], None, d["scale"])
+        sizes = L.SimLinearAttn(2, T, 4, 2, 32, 48, 2, d["scale"])
+        for i in range(4):
+            out = [torch.empty_like(x) if j == i else None for j, x in enumerate(all_of)]
+            ptr = lambda x: None if x is None else x.data_ptr()   # noqa: E731
+            q = d["q"] if i else None                  # q is not needed for dq, k not for dk, v not for dv and ds0
+            k = d["k"] if i in (0, 2) else None
+            v = d["v"] if i in (0, 1) else None
+            sim._call("linear_attn_grad", sizes, _heads(q), _heads(k), _heads(v), ptr(d["decay"]), _heads(d["dy"]), None, ptr(d["s0"]),
+                      ptr(d["dstate"]), _heads(out[0]), _heads(out[1]), _heads(out[2]), ptr(out[3]))
+            sim.sync()
+            assert torch.equal(out[i], all_of[i]), (T, i)
+    assert C.sizeof(L.SimHeads) == 32
+
+
+def test_from_another_stream(sim):
+    """Called while another stream is current: ordered after its work, and its later work after the call."""
+    d = ac.inputs(2, 300, 2, 2, 64, 64, torch.float32, 16)
+    c = cuda(d)
+    want = sim.linear_attn(c["q"], c["k"], c["v"], c["decay"], c["s0"], None, c["scale"])
+    sim.sync()
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        st.wait_stream(torch.cuda.default_stream())
+        for _ in range(3):
+            big = torch.randn(4096, 4096, device="cuda")
+            for _ in range(8):
+                big = big @ big * 1e-3             # keeps the stream busy before the inputs are there
+            q = c["q"] + 0.0 * big[0, 0].nan_to_num(0.0, 0.0, 0.0)
+            y, s = sim.linear_attn(q, c["k"], c["v"], c["decay"], c["s0"], None, c["scale"])
+            copy = y.clone()
+            st.synchronize()
+            assert torch.equal(copy, want[0]) and torch.equal(s, want[1])
+
+
 def test_sizes_of_zero(sim):
     for B, T in ((0, 5), (2, 0), (0, 0)):
         z = lambda h, c: torch.zeros(B, T, h, c, device="cuda")   # noqa: E731

@@ -111,6 +111,21 @@ def test_larger(sim, dtype):
     assert 0.5 < s.min() and s.max() < 1.3
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,M,N", [(94, 256, 256), (43, 512, 600), (1, 64, 4000), (2, 2100, 130), (1, 200, 1100)])
+def test_tiles_and_shares(sim, n, M, N, dtype):
+    """Batches that are given the larger tiles, and few rows of many columns, whose sums are shared by workgroups: one
+    matrix n times, so every result is the first one's."""
+    u = update(1, M, N, TYPES[dtype], M)
+    d = u.cuda().expand(n, M, N)
+    got = sim.orthogonalize(d)
+    sim.sync()
+    assert all(torch.equal(got[i], got[0]) for i in range(1, n))
+    want, way = ops.orthogonalize(u[0].double().numpy())
+    e = bound(way, NS, dtype != "bf16") + fro(rounding(want, u.dtype))
+    assert fro(got[0].double().cpu().numpy() - want) <= e
+
+
 @pytest.mark.parametrize("steps", [0, 1, 2, 7])
 def test_steps_coefficients_and_scale(sim, steps):
     check(sim, update(2, 40, 70, torch.float32, 7), steps=steps, scale=0.25)
