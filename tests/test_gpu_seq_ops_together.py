@@ -72,8 +72,10 @@ def test_training_step(sim):
     # at rho = 1 the policy loss is the same loss but for its value: -adv for -adv logp
     assert (pol["grad"] - dl).norm() <= 1e-5 * dl.norm()
     # two sums of the same row in other orders: each log-probability is off by at most eL + u |log p| of loss_check.py, with
-    # |x|, |log p| < 24 and log S < log 12 at most (3 24 + 4) + (12/64 + 12 + 16) + (24 + 24 + 8 + 1) + 24 < 186 u
-    assert logits.abs().max() < 12 and (pol["logp"] - lp["logp"])[Live].abs().max() <= 2 * 186 * 2.0 ** -24
+    # |x| at most the row's spread s, |log p| at most s + log 12 and log S at most log 12:
+    # (3 s + 4) + (12/64 + 12 + 16) + (s + s + 2.5 + 3 2.5 + 1) + s + 2.5 <= 6 s + 46 u
+    spread = (logits.amax(1) - logits.amin(1)).max()
+    assert (pol["logp"] - lp["logp"])[Live].abs().max() <= 2 * (6 * spread + 46) * 2.0 ** -24
     top = ls.detach().sort(1, descending=True).values[:, :3]
     assert (lp["top_logp"].double().cpu()[live] - top[live]).abs().max() < 1e-4
     assert (lp["top_index"][~Live] == -1).all() and not dl[~Live].any()
