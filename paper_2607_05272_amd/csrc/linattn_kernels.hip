@@ -222,13 +222,15 @@ __device__ __forceinline__ Bf4 read_turned(const __bf16* p) {
 }
 __device__ __forceinline__ Bf8 both(Bf4 a, Bf4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
-constexpr int kPad = 8;   // rows of LDS start four banks apart
+// Rows of LDS start four banks apart where they are read along (q, the products), eight where they are read turned, eight
+// rows by 16 columns per 32 lanes (k, which is read both ways, v): no two lanes of a step meet in a bank.
+constexpr int kPad = 8, kPadTurned = 16;
 template <class E, int DQ, int NW, int HV, int C>
 struct RunLds {
   static constexpr int NI = PartsOf<E>::kIn, NC = PartsOf<E>::kMade, DV = 16 * NW, TT = C / 16;
-  __bf16 q[NI][C][DQ + kPad], k[NI][C][DQ + kPad], v[NI][C][DV + kPad], p[NC][C][C + kPad];
+  __bf16 q[NI][C][DQ + kPad], k[NI][C][DQ + kPadTurned], v[NI][C][DV + kPadTurned], p[NC][C][C + kPad];
   Fl4 half[HV > 1 ? NW : 1][HV][HV > 1 ? TT / HV : 1][HV > 1 ? 64 : 1];   // a half's sums that the other one needs
-  float pow[C + 1], into[C];   // su l^i; su l^(m-1-j+lag)
+  float pow[C + 1], into[C];   // l^i; su l^(m-1-j+lag)
 };
 
 // eight elements of a row from p on
@@ -376,11 +378,12 @@ __global__ __launch_bounds__(64 * NW * HV, NW * HV == 4 ? 2 : 1) void attn_run_k
       st[kt][i] = s0 && row < r.Dq && c < r.Dv ? s0[row * sr + c * sc] : 0.0f;
     }
   }
-  if (threadIdx.x <= C) m.pow[threadIdx.x] = r.su * power(threadIdx.x);
+  if (threadIdx.x <= C) m.pow[threadIdx.x] = power(threadIdx.x);
+  __syncthreads();
   float out_w[TT];   // so l^(t+1-lag) of this lane's step of each tile
 #pragma unroll
-  for (int t = 0; t < TT; ++t) out_w[t] = r.so * power(16 * t + lc + 1 - r.lag);
-  const float whole = power(C);
+  for (int t = 0; t < TT; ++t) out_w[t] = r.so * m.pow[16 * t + lc + 1 - r.lag];
+  const float inner = r.so * r.su;
   Tile<E, DQ, C, NT> q, k;
   Tile<E, DV, C, NT> v;
   if (OUT) q.start(r, r.q, b, h, first, n, 0, r.Dq);
@@ -411,7 +414,7 @@ __global__ __launch_bounds__(64 * NW * HV, NW * HV == 4 ? 2 : 1) void attn_run_k
     v.store(m.v, all, now, width);
     if (threadIdx.x < C) {
       const int j = threadIdx.x;
-      m.into[j] = j < now ? m.pow[now - 1 - j + r.lag] : 0.0f;
+      m.into[j] = j < now ? r.su * m.pow[now - 1 - j + r.lag] : 0.0f;
     }
     __syncthreads();
     if (i0 + C < live) fetch(live - i0 - C);
@@ -448,7 +451,7 @@ __global__ __launch_bounds__(64 * NW * HV, NW * HV == 4 ? 2 : 1) void attn_run_k
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int gap = 16 * (ti - tj) + lc - (4 * lg + i);
-          w[i] = gap >= 0 ? acc[i] * (r.so * m.pow[gap < 0 ? 0 : gap]) : 0.0f;
+          w[i] = gap >= 0 ? acc[i] * (inner * m.pow[gap < 0 ? 0 : gap]) : 0.0f;
         }
         split(w, o);
 #pragma unroll
@@ -498,15 +501,18 @@ __global__ __launch_bounds__(64 * NW * HV, NW * HV == 4 ? 2 : 1) void attn_run_k
         Bf8 a[NI];
 #pragma unroll
         for (int p = 0; p < NI; ++p) {
-          const __bf16* at = &m.v[p][32 * j + 8 * lg + lc / 4][wave * 16 + 4 * (lc % 4)];
-          a[p] = both(read_turned(at), read_turned(at + 4 * (DV + kPad)));
+          const __bf16* at = &m.v[p][32 * j + 4 * lg + lc / 4][wave * 16 + 4 * (lc % 4)];
+          a[p] = both(read_turned(at), read_turned(at + 16 * (DV + kPadTurned)));
         }
 #pragma unroll
         for (int o = 2 * j / HV; o < TO; ++o) {   // tiles below the diagonal, those that stand on it in 32 x 32 among them
           const int t = HV * o + hv;
           Bf8 x[NC];
 #pragma unroll
-          for (int p = 0; p < NC; ++p) x[p] = *reinterpret_cast<const Bf8*>(&m.p[p][16 * t + lc][32 * j + 8 * lg]);
+          for (int p = 0; p < NC; ++p) {
+            const __bf16* row = &m.p[p][16 * t + lc][32 * j + 4 * lg];
+            x[p] = both(*reinterpret_cast<const Bf4*>(row), *reinterpret_cast<const Bf4*>(row + 16));
+          }
           mul_parts(a, x, y[o]);
         }
       }
@@ -533,7 +539,7 @@ __global__ __launch_bounds__(64 * NW * HV, NW * HV == 4 ? 2 : 1) void attn_run_k
       at0 += C * turn;
     }
     // S = l^m S + K^T V weighted
-    const float fade = now == C ? whole : power(now);
+    const float fade = m.pow[now];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
       st[kt] *= fade;
@@ -544,8 +550,8 @@ __global__ __launch_bounds__(64 * NW * HV, NW * HV == 4 ? 2 : 1) void attn_run_k
       Bf8 a[NI];
 #pragma unroll
       for (int p = 0; p < NI; ++p) {
-        const __bf16* at = &m.v[p][32 * j + 8 * lg + lc / 4][wave * 16 + 4 * (lc % 4)];
-        a[p] = both(read_turned(at), read_turned(at + 4 * (DV + kPad)));
+        const __bf16* at = &m.v[p][32 * j + 4 * lg + lc / 4][wave * 16 + 4 * (lc % 4)];
+        a[p] = both(read_turned(at), read_turned(at + 16 * (DV + kPadTurned)));
       }
       float w[8];
       __bf16 o[3][8];
@@ -554,7 +560,7 @@ __global__ __launch_bounds__(64 * NW * HV, NW * HV == 4 ? 2 : 1) void attn_run_k
         w[i] = (float)a[0][i];
 #pragma unroll
         for (int p = 1; p < NI; ++p) w[i] += (float)a[p][i];
-        w[i] *= m.into[32 * j + 8 * lg + i];
+        w[i] *= m.into[32 * j + 16 * (i / 4) + 4 * lg + i % 4];
       }
       split(w, o);
 #pragma unroll
@@ -564,8 +570,8 @@ __global__ __launch_bounds__(64 * NW * HV, NW * HV == 4 ? 2 : 1) void attn_run_k
         Bf8 a[NI];
 #pragma unroll
         for (int p = 0; p < NI; ++p) {
-          const __bf16* at = &m.k[p][32 * j + 8 * lg + lc / 4][16 * (k0 + kt) + 4 * (lc % 4)];
-          a[p] = both(read_turned(at), read_turned(at + 4 * (DQ + kPad)));
+          const __bf16* at = &m.k[p][32 * j + 4 * lg + lc / 4][16 * (k0 + kt) + 4 * (lc % 4)];
+          a[p] = both(read_turned(at), read_turned(at + 16 * (DQ + kPadTurned)));
         }
         mul_parts(a, x, st[kt]);
       }
