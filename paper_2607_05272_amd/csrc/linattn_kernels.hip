@@ -379,6 +379,12 @@ __global__ __launch_bounds__(64 * NW * HV, NW * HV == 4 ? 2 : 1) void attn_run_k
     }
   }
   if (threadIdx.x <= C) m.pow[threadIdx.x] = power(threadIdx.x);
+  // the tiles beside the diagonal in a step of 32 stay zeros
+  static_assert(TT % 2 == 0, "steps of 32");
+  if (OUT) {
+    for (int i = threadIdx.x; i < NC * TT / 2 * 256; i += NT)
+      m.p[i / (TT / 2 * 256)][i / 256 % (TT / 2) * 32 + (i & 15)][i / 256 % (TT / 2) * 32 + 16 + (i >> 4 & 15)] = (__bf16)0.0f;
+  }
   __syncthreads();
   float out_w[TT];   // so l^(t+1-lag) of this lane's step of each tile
 #pragma unroll
@@ -419,44 +425,53 @@ __global__ __launch_bounds__(64 * NW * HV, NW * HV == 4 ? 2 : 1) void attn_run_k
     __syncthreads();
     if (i0 + C < live) fetch(live - i0 - C);
     if constexpr (OUT) {
-      // weighted products, turned: rows j, columns i
-      constexpr int kPairs = TT * TT / 2 + TT / 2 + (TT / 2);   // tiles of j <= i, and those beside them in a step of 32
-      static_assert(TT % 2 == 0, "steps of 32");
+      // weighted products, turned: rows j, columns i; a wave's tiles of j <= i side by side
+      constexpr int W = NW * HV, kTiles = TT * (TT + 1) / 2, kMost = (kTiles + W - 1) / W;
+      auto products = [&](auto N) {
+        constexpr int MINE = decltype(N)::value;
+        if constexpr (MINE > 0) {
+          int ti[MINE], tj[MINE];
+          Fl4 w[MINE];
 #pragma unroll
-      for (int w0 = 0; w0 < kPairs; w0 += NW * HV) {
-        int at = w0 + any, ti = 0;
-        // row of tiles ti has 2 (ti / 2 + 1) of them
+          for (int n = 0; n < MINE; ++n) {
+            const int at = any + n * W;
+            ti[n] = 0;
 #pragma unroll
-        for (int x = 0; x < TT - 1; ++x) {
-          const int have = 2 * (x / 2 + 1);
-          if (ti == x && at >= have) { at -= have; ++ti; }
-        }
-        if (w0 + any >= kPairs) continue;
-        const int tj = at;
-        Fl4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (tj <= ti) {
+            for (int x = 1; x < TT; ++x) ti[n] += at >= x * (x + 1) / 2;
+            tj[n] = at - ti[n] * (ti[n] + 1) / 2;
+            w[n] = Fl4{0.0f, 0.0f, 0.0f, 0.0f};
+          }
 #pragma unroll
           for (int kk = 0; kk < DQ / 32; ++kk) {
-            Bf8 a[NI], x[NI];
 #pragma unroll
-            for (int p = 0; p < NI; ++p) {
-              a[p] = *reinterpret_cast<const Bf8*>(&m.k[p][16 * tj + lc][32 * kk + 8 * lg]);
-              x[p] = *reinterpret_cast<const Bf8*>(&m.q[p][16 * ti + lc][32 * kk + 8 * lg]);
+            for (int n = 0; n < MINE; ++n) {
+              Bf8 a[NI], x[NI];
+#pragma unroll
+              for (int p = 0; p < NI; ++p) {
+                a[p] = *reinterpret_cast<const Bf8*>(&m.k[p][16 * tj[n] + lc][32 * kk + 8 * lg]);
+                x[p] = *reinterpret_cast<const Bf8*>(&m.q[p][16 * ti[n] + lc][32 * kk + 8 * lg]);
+              }
+              mul_parts(a, x, w[n]);
             }
-            mul_parts(a, x, acc);
+          }
+#pragma unroll
+          for (int n = 0; n < MINE; ++n) {
+            float y[4];
+            __bf16 o[NC][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int gap = 16 * (ti[n] - tj[n]) + lc - (4 * lg + i);
+              y[i] = gap >= 0 ? w[n][i] * (inner * m.pow[gap < 0 ? 0 : gap]) : 0.0f;
+            }
+            split(y, o);
+#pragma unroll
+            for (int x = 0; x < NC; ++x)
+              *reinterpret_cast<Bf4*>(&m.p[x][16 * ti[n] + lc][16 * tj[n] + 4 * lg]) = packed(o[x]);
           }
         }
-        float w[4];
-        __bf16 o[NC][4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int gap = 16 * (ti - tj) + lc - (4 * lg + i);
-          w[i] = gap >= 0 ? acc[i] * (inner * m.pow[gap < 0 ? 0 : gap]) : 0.0f;
-        }
-        split(w, o);
-#pragma unroll
-        for (int x = 0; x < NC; ++x) *reinterpret_cast<Bf4*>(&m.p[x][16 * ti + lc][16 * tj + 4 * lg]) = packed(o[x]);
-      }
+      };
+      if (any + (kMost - 1) * W < kTiles) products(std::integral_constant<int, kMost>{});
+      else products(std::integral_constant<int, kMost - 1>{});
       // S^T Q^T, columns i
       Fl4 acc[TT];
 #pragma unroll
