@@ -34,6 +34,7 @@ struct AttnRun {
   bool back, wide;      // steps from the last to the first; out in fp32
   float so, su;
   float* parts;         // states before (after attn_join_k) or of the segments that time is split into
+  int64_t pr, pc;       // strides of their rows and columns
   int64_t seg;          // steps of a segment
   int segs;
 };
@@ -367,7 +368,7 @@ __global__ __launch_bounds__(64 * NW * HV, NW * HV == 4 ? 2 : 1) void attn_run_k
   const bool split_time = r.segs > 1;
   const float* s0 = split_time ? r.parts + ((int64_t)bh * r.segs + seg) * r.Dq * r.Dv
                                : (r.s0 ? r.s0 + (int64_t)bh * r.Dq * r.Dv : nullptr);
-  const int64_t sr = split_time ? r.Dv : r.sr, sc = split_time ? 1 : r.sc;
+  const int64_t sr = split_time ? r.pr : r.sr, sc = split_time ? r.pc : r.sc;
   if (!OUT && split_time) s0 = nullptr;
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
@@ -636,7 +637,7 @@ __global__ __launch_bounds__(256) void attn_join_k(AttnRun r) {
   const double log2l = log2((double)l);
   const float whole = (float)exp2((double)r.seg * log2l);
   float* p = r.parts + (int64_t)blockIdx.y * r.segs * cells + i;
-  constexpr int kAhead = 16;   // loads that fly together
+  constexpr int kAhead = 32;   // loads that fly together
   for (int g0 = 0; g0 < r.segs; g0 += kAhead) {
     float own[kAhead];
 #pragma unroll
@@ -706,8 +707,10 @@ size_t parts_bytes(int64_t B, int64_t T, int H, int Dq, int Dv) {
   return g > 1 ? (size_t)B * H * g * Dq * Dv * sizeof(float) : 0;
 }
 
+// all of a run, or of one in segments the states that they start from (and the last one), or the result from these
+enum { kWhole = 0, kStates = 1, kResult = 2 };
 template <class E, int DQ, int NW, int HV, int C>
-hipError_t launch_runs(AttnRun r, int64_t B, hipStream_t st) {
+hipError_t launch_runs(AttnRun r, int64_t B, int what, hipStream_t st) {
   typedef RunLds<E, DQ, NW, HV, C> Lds;
   static std::atomic<uint64_t> done[2];
   hipError_t e = allow_lds(reinterpret_cast<const void*>(&attn_run_k<E, DQ, NW, HV, C, true>), sizeof(Lds), done[0]);
@@ -715,11 +718,11 @@ hipError_t launch_runs(AttnRun r, int64_t B, hipStream_t st) {
   if (e != hipSuccess) return e;
   const int cols = (r.Dv + Lds::DV - 1) / Lds::DV;
   const dim3 grid((unsigned)(B * r.H * cols), r.segs), block(64 * NW * HV);
-  if (r.segs > 1) {
+  if (r.segs > 1 && what != kResult) {
     hipLaunchKernelGGL((attn_run_k<E, DQ, NW, HV, C, false>), grid, block, sizeof(Lds), st, r);
     hipLaunchKernelGGL(attn_join_k, dim3((r.Dq * r.Dv + 255) / 256, (unsigned)(B * r.H)), dim3(256), 0, st, r);
     r.err = nullptr;
-    if (!r.out) return hipSuccess;
+    if (!r.out || what == kStates) return hipSuccess;
   }
   if (r.out) hipLaunchKernelGGL((attn_run_k<E, DQ, NW, HV, C, true>), grid, block, sizeof(Lds), st, r);
   else hipLaunchKernelGGL((attn_run_k<E, DQ, NW, HV, C, false>), grid, block, sizeof(Lds), st, r);
@@ -727,7 +730,7 @@ hipError_t launch_runs(AttnRun r, int64_t B, hipStream_t st) {
 }
 
 template <class E>
-hipError_t launch_run(AttnRun r, int64_t B, float* parts, hipStream_t st) {
+hipError_t launch_run(AttnRun r, int64_t B, float* parts, int what, hipStream_t st) {
   constexpr int dt = std::is_same<E, F32>::value ? SIM_DT_F32 : (std::is_same<E, F16>::value ? SIM_DT_F16 : SIM_DT_BF16);
   if (r.T <= kFew) {
     const dim3 grid((unsigned)(B * r.H), (r.Dv + 63) / 64), block(kStep);
@@ -744,13 +747,14 @@ hipError_t launch_run(AttnRun r, int64_t B, float* parts, hipStream_t st) {
     r.seg = (each + 63) / 64 * 64;
     r.segs = (int)((r.T + r.seg - 1) / r.seg);
     r.parts = parts;
+    if (r.pr == 0) { r.pr = r.Dv; r.pc = 1; }
   }
   constexpr int C64 = run_steps(dt, 64), C128 = run_steps(dt, 128), C256 = run_steps(dt, 256);
-  if (r.Dq > 128) return launch_runs<E, 256, 4, 2, C256>(r, B, st);
+  if (r.Dq > 128) return launch_runs<E, 256, 4, 2, C256>(r, B, what, st);
   if (r.Dq > 64)
-    return plan.columns == 128 ? launch_runs<E, 128, 8, 1, C128>(r, B, st) : launch_runs<E, 128, 4, 2, C128>(r, B, st);
-  return plan.columns == 128 ? launch_runs<E, 64, 8, 1, C64>(r, B, st)
-         : plan.halves == 2 ? launch_runs<E, 64, 4, 2, C64>(r, B, st) : launch_runs<E, 64, 4, 1, C64>(r, B, st);
+    return plan.columns == 128 ? launch_runs<E, 128, 8, 1, C128>(r, B, what, st) : launch_runs<E, 128, 4, 2, C128>(r, B, what, st);
+  return plan.columns == 128 ? launch_runs<E, 64, 8, 1, C64>(r, B, what, st)
+         : plan.halves == 2 ? launch_runs<E, 64, 4, 2, C64>(r, B, what, st) : launch_runs<E, 64, 4, 1, C64>(r, B, what, st);
 }
 
 In in_of(const sim_heads& x, int share) { return In{x.data, x.stride_b, x.stride_t, x.stride_h, share}; }
@@ -783,7 +787,7 @@ hipError_t launch_typed(const AttnArgs& a, bool grad, hipStream_t st) {
     dims(r, c.Dk, c.Dv, false);
     out(r, a.y);
     r.s0 = a.s0; r.state = a.state; r.so = c.scale; r.su = 1.0f;
-    return launch_run<E>(r, c.B, parts, st);
+    return launch_run<E>(r, c.B, parts, kWhole, st);
   }
   hipError_t e = hipSuccess;
   // lengths and decays are told of by the first run there is
@@ -793,16 +797,36 @@ hipError_t launch_typed(const AttnArgs& a, bool grad, hipStream_t st) {
     dims(r, c.Dv, c.Dk, true);
     out(r, a.dq);
     r.s0 = a.s0; r.so = c.scale; r.su = 1.0f;
-    if ((e = launch_run<E>(r, c.B, parts, st)) != hipSuccess) return e;
+    if ((e = launch_run<E>(r, c.B, parts, kWhole, st)) != hipSuccess) return e;
     f.err = nullptr;
   }
   f.back = true; f.lag = 1; f.so = 1.0f; f.su = c.scale;
+  AttnRun rk = f, rv = f;
+  rk.q = v; rk.k = dy; rk.v = q;
+  rk.s0 = rv.s0 = a.ds;
+  dims(rk, c.Dv, c.Dk, true);
+  rv.q = k; rv.k = q; rv.v = dy;
+  dims(rv, c.Dk, c.Dv, false);
+  // Both go by the same states, each other's turned: in segments they are formed once, for either alone too, so that
+  // a gradient is the same whichever others are wanted.
+  const int segs = plan_of(c.B, c.T, c.H, c.Dv, c.Dk).segs;
+  int what = kWhole;
+  if (segs > 1 && segs == plan_of(c.B, c.T, c.H, c.Dk, c.Dv).segs && (a.dk.data || a.dv.data || a.state)) {
+    AttnRun r = rk;
+    r.state = a.state;
+    if ((e = launch_run<E>(r, c.B, parts, kStates, st)) != hipSuccess) return e;
+    rk.err = rv.err = nullptr;
+    rv.pr = 1; rv.pc = c.Dk;
+    what = kResult;
+  } else {
+    rv.state = a.state;
+  }
   auto shared = [&](AttnRun& r, const sim_heads& o, int D) {
     out(r, o);
-    if (g == 1 || !r.out) return launch_run<E>(r, c.B, parts, st);
+    if (g == 1 || !r.out) return launch_run<E>(r, c.B, parts, what, st);
     r.out = shares; r.wide = true;
     r.oh = D; r.ot = (int64_t)c.H * D; r.ob = c.T * r.ot;
-    const hipError_t e = launch_run<E>(r, c.B, parts, st);
+    const hipError_t e = launch_run<E>(r, c.B, parts, what, st);
     if (e != hipSuccess) return e;
     const int64_t cells = c.B * c.T * c.Hk * D;
     hipLaunchKernelGGL(attn_share_k<E>, dim3((unsigned)std::min<int64_t>((cells + 255) / 256, 1 << 16)), dim3(256), 0, st,
@@ -810,20 +834,10 @@ hipError_t launch_typed(const AttnArgs& a, bool grad, hipStream_t st) {
     return hipSuccess;
   };
   if (a.dk.data) {
-    AttnRun r = f;
-    r.q = v; r.k = dy; r.v = q;
-    dims(r, c.Dv, c.Dk, true);
-    r.s0 = a.ds;
-    if ((e = shared(r, a.dk, c.Dk)) != hipSuccess) return e;
-    f.err = nullptr;
+    if ((e = shared(rk, a.dk, c.Dk)) != hipSuccess) return e;
+    rv.err = nullptr;
   }
-  if (a.dv.data || a.state) {   // the last one: ds0 may be written over dstate
-    AttnRun r = f;
-    r.q = k; r.k = q; r.v = dy;
-    dims(r, c.Dk, c.Dv, false);
-    r.s0 = a.ds; r.state = a.state;
-    e = shared(r, a.dv, c.Dv);
-  }
+  if (a.dv.data || rv.state) e = shared(rv, a.dv, c.Dv);   // the last one: ds0 may be written over dstate
   return e;
 }
 
