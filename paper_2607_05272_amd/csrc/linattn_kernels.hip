@@ -637,7 +637,7 @@ __global__ __launch_bounds__(256) void attn_join_k(AttnRun r) {
   const double log2l = log2((double)l);
   const float whole = (float)exp2((double)r.seg * log2l);
   float* p = r.parts + (int64_t)blockIdx.y * r.segs * cells + i;
-  constexpr int kAhead = 32;   // loads that fly together
+  constexpr int kAhead = 16;   // loads that fly together
   for (int g0 = 0; g0 < r.segs; g0 += kAhead) {
     float own[kAhead];
 #pragma unroll

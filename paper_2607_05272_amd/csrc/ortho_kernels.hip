@@ -73,7 +73,7 @@ Layout layout_of(const sim_ortho& o) {
   // Few tiles and many columns: K in shares of at least kShare (us, whole and in shares: bf16 64 x 16384 503, 101; 1024 x 16384
   // 812, 588; 768 x 2048 190, 169; fp32 2 x 40 x 4000 256, 117)
   const int64_t k = l.d.R / l.half, tiles = n * k * (k + 1) / 2;
-  l.split = (int)std::max<int64_t>(1, std::min<int64_t>((l.half == 256 ? 256 : kFillTiles) / tiles, l.d.C / kShare));
+  l.split = (int)std::max<int64_t>(1, std::min<int64_t>(kFillTiles / tiles, l.d.C / kShare));
   l.bytes = l.parts_at + (l.split > 1 ? n * l.split * l.a * sizeof(float) : 0);
   return l;
 }
