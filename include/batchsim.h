@@ -572,8 +572,9 @@ typedef struct sim_linear_attn {
  * Up to T = 16 steps are taken one after another. With more, a run of steps is taken at once: the
  * products q_t k_s, weighted by l^(t-s), and the state between runs are held in fp32 and multiplied, for y
  * alone, as bf16 parts that add up to them (two for 16-bit types, 16 bits of the value; three for fp32, all
- * 24), so they must be finite in fp32, and results differ from a step-by-step sum by rounding. An infinity or
- * NaN in v_t (of a live step) reaches y from the start of its run on, up to 63 steps before t. */
+ * 24), and results differ from a step-by-step sum by rounding. What the formulas make infinite or NaN, for
+ * an infinity or NaN of a live step or because fp32 (or bf16's largest, 3.39e38) is passed on the way, is
+ * infinite or NaN, not always the same of the two; what they make without it is not touched by it. */
 int linear_attn_work(const sim_linear_attn* s, size_t* bytes);
 int linear_attn(sim_ctx* ctx, const sim_linear_attn* s, const sim_heads* q, const sim_heads* k,
                 const sim_heads* v, const float* d_decay, const int32_t* d_len, const float* d_s0,
@@ -610,7 +611,7 @@ typedef struct sim_logprobs {
  * NULL; d_tokens may be NULL if d_logp is. A token of -1 (not with SIM_IT_U8) is none: its logp is 0; any
  * other outside [0, A) latches SIM_ESTATE and is taken as none. Rows with d_live [N] bytes (NULL: all) 0
  * are not looked at; they, and rows that allow no column, give nothing: logp 0, entropy 0, no
- * alternatives. Alternatives are best had of rows of adjacent columns, or of up to 384 columns.  */
+ * alternatives. Alternatives are best had of rows of adjacent columns, or of up to 960 columns.  */
 int token_logprobs_work(const sim_logprobs* c, size_t* bytes);
 int token_logprobs(sim_ctx* ctx, const sim_logprobs* c, const sim_mat* logits, const sim_mat* mask,
                    const void* d_tokens, const uint8_t* d_live, float* d_logp, float* d_entropy,

@@ -512,24 +512,54 @@ __global__ __launch_bounds__(64 * NW * HV, NW * HV == 4 ? 2 : 1) void attn_run_k
 #pragma unroll
         for (int t = 0; t < TO; ++t) y[t] += m.half[wave][hv][t][lane];
       }
+      Bf8 a[C / 32][NI];
+      uint32_t odd = 0;   // bits 15 and 31: all exponent bits of a value of this wave's columns
 #pragma unroll
       for (int j = 0; j < C / 32; ++j) {
-        Bf8 a[NI];
 #pragma unroll
         for (int p = 0; p < NI; ++p) {
           const __bf16* at = &m.v[p][32 * j + 4 * lg + lc / 4][wave * 16 + 4 * (lc % 4)];
-          a[p] = both(read_turned(at), read_turned(at + 16 * (DV + kPadTurned)));
+          a[j][p] = both(read_turned(at), read_turned(at + 16 * (DV + kPadTurned)));
         }
+        typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+        const U4 w = __builtin_bit_cast(U4, a[j][0]);
 #pragma unroll
-        for (int o = 2 * j / HV; o < TO; ++o) {   // tiles below the diagonal, those that stand on it in 32 x 32 among them
-          const int t = HV * o + hv;
-          Bf8 x[NC];
+        for (int i = 0; i < 4; ++i) odd |= (w[i] & 0x7F807F80u) + 0x00800080u;
+      }
+      if (!__any(odd & 0x80008000u)) {
 #pragma unroll
-          for (int p = 0; p < NC; ++p) {
-            const __bf16* row = &m.p[p][16 * t + lc][32 * j + 4 * lg];
-            x[p] = both(*reinterpret_cast<const Bf4*>(row), *reinterpret_cast<const Bf4*>(row + 16));
+        for (int j = 0; j < C / 32; ++j) {
+#pragma unroll
+          for (int o = 2 * j / HV; o < TO; ++o) {   // tiles below the diagonal, those that stand on it in 32 x 32 among them
+            const int t = HV * o + hv;
+            Bf8 x[NC];
+#pragma unroll
+            for (int p = 0; p < NC; ++p) {
+              const __bf16* row = &m.p[p][16 * t + lc][32 * j + 4 * lg];
+              x[p] = both(*reinterpret_cast<const Bf4*>(row), *reinterpret_cast<const Bf4*>(row + 16));
+            }
+            mul_parts(a[j], x, y[o]);
           }
-          mul_parts(a, x, y[o]);
+        }
+      } else {
+        // An infinity or NaN among the values: by the zeros above the diagonal it would reach steps before its own. What
+        // the look for it costs: 8 x 2048 x 16 heads x 128 111 and 115 us.
+#pragma unroll
+        for (int o = 0; o < TO; ++o) {
+          const int i = 16 * (HV * o + hv) + lc;
+#pragma unroll 1
+          for (int j = 0; j <= i; ++j) {
+            float w = 0.0f;
+#pragma unroll
+            for (int p = NC - 1; p >= 0; --p) w += (float)m.p[p][i][j];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float x = 0.0f;
+#pragma unroll
+              for (int p = NI - 1; p >= 0; --p) x += (float)m.v[p][j][wave * 16 + 4 * lg + e];
+              y[o][e] = fmaf(w, x, y[o][e]);
+            }
+          }
         }
       }
       either(full && now == C && !r.wide, [&](auto W) {

@@ -280,6 +280,37 @@ def test_an_infinity_stays_in_its_sequence(sim, T):
     assert not y[1, 0, 0, 0].isfinite()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32", "f16"])
+@pytest.mark.parametrize("T,Dk,Dv", [(9, 16, 24), (150, 16, 24), (150, 96, 40), (90, 128, 128), (70, 200, 40)])
+def test_what_is_not_finite_reaches_only_what_it_is_part_of(sim, T, Dk, Dv, dtype):
+    """An infinity or NaN in a live step: results that the formulas make without it are what they are without
+    it (the steps before it above all), the others are not finite."""
+    d = ac.inputs(2, T, 2, 2, Dk, Dv, TYPES[dtype], 17)
+
+    def call(d):
+        c = cuda(d)
+        y, s = sim.linear_attn(c["q"], c["k"], c["v"], c["decay"], c["s0"], None, c["scale"])
+        g = sim.linear_attn_grad(c["q"], c["k"], c["v"], c["decay"], c["dy"], c["s0"], c["dstate"], None, c["scale"])
+        sim.sync()
+        return [x.cpu() for x in (y, s, *g)]
+    clean = call(d)
+    for i, name in enumerate(("q", "k", "v", "dy")):
+        e = dict(d)
+        e[name] = d[name].clone()
+        e[name][1, (2 * T) // 3, 1, 3] = float("nan") if i % 2 else float("inf")
+        a = [e[n].double().numpy() for n in ("q", "k", "v", "decay", "dy", "s0", "dstate")]
+        with np.errstate(invalid="ignore"):
+            want = (*ops.linear_attn(*a[:4], a[5], None, d["scale"]), *ops.linear_attn_grad(*a, None, d["scale"]))
+        got = call(e)
+        mixed = []
+        for x, w, c in zip(got, want, clean):
+            free = torch.from_numpy(np.isfinite(w))
+            assert not x[~free].isfinite().any(), name
+            mixed.append(torch.where(free, x, c))
+        ac.check_forward(d, *mixed[:2])
+        ac.check_grad(d, *mixed[2:])
+
+
 @pytest.mark.parametrize("dtype,T", [("bf16", 1), ("bf16", 300), ("f32", 70), ("f16", 130)])
 def test_repeated_calls_and_graphs(sim, dtype, T):
     """The same bits each time; captured, replayed on new inputs between eager calls."""
