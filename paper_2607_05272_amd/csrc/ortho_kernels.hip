@@ -205,17 +205,17 @@ struct Mul {
   bool end;
 };
 constexpr int threads_of(int TM) { return TM == 256 ? 512 : 256; }
-template <int NP, int TM>
+template <int NP, int TM, int BK>
 struct Form {
-  static constexpr int kThreads = threads_of(TM), kRows = TM == 256 ? 4 : TM / 64, kCols = TM == 256 ? 2 : TM / 64;
-  static constexpr int BK = NP == 1 || TM == 64 ? 64 : 32, kStage = NP * TM * BK;   // elements of P or Q in half of LDS
-  static constexpr size_t kLds = 4 * kStage * sizeof(_Float16);
-  static_assert(64 * (TM + 1) * sizeof(float) <= kLds, "a band of the result");
+  static constexpr int kRows = TM == 256 ? 4 : TM / 64, kCols = TM == 256 ? 2 : TM / 64;
+  static constexpr int kStage = NP * TM * BK;   // elements of P or Q in half of LDS
+  static constexpr size_t kBand = 64 * (TM + 1) * sizeof(float);   // of the result
+  static constexpr size_t kLds = std::max(4 * kStage * sizeof(_Float16), kBand);
 };
-template <int NP, int TM, int KIND>
+template <int NP, int TM, int BK, int KIND>
 __global__ __launch_bounds__(threads_of(TM), TM == 256 ? 1 : 2) void ortho_mul_k(Mul m) {
-  typedef Form<NP, TM> Fm;
-  constexpr int BK = Fm::BK, CH = BK / 8, NT = Fm::kThreads, U = TM * BK / 8 / NT, WR = Fm::kRows, WC = Fm::kCols;
+  typedef Form<NP, TM, BK> Fm;
+  constexpr int CH = BK / 8, NT = threads_of(TM), U = TM * BK / 8 / NT, WR = Fm::kRows, WC = Fm::kCols;
   constexpr int AHEAD = TM == 64 && NP == 1 ? 3 : (TM == 256 ? 1 : 2);   // parts of K on their way
   constexpr int QC = TM / 8;   // chunks of a row of Q, turned
   extern __shared__ __align__(16) char raw[];
@@ -466,22 +466,26 @@ __global__ __launch_bounds__(256) void ortho_sum_k(const float* in, int shares, 
   for (int q = 0; q < NP; ++q) *reinterpret_cast<H4*>(out + q * cells + (size_t)(c0 + col) * R + r0 + rr) = w[q];
 }
 
-template <int NP, int TM, int KIND>
+template <int NP, int TM, int BK, int KIND>
 hipError_t launch_mul(const Mul& m, const Layout& l, hipStream_t st) {
   static std::atomic<uint64_t> done;
-  const size_t lds = Form<NP, TM>::kLds;
-  const hipError_t e = allow_lds(reinterpret_cast<const void*>(&ortho_mul_k<NP, TM, KIND>), lds, done);
+  const size_t lds = Form<NP, TM, BK>::kLds;
+  const hipError_t e = allow_lds(reinterpret_cast<const void*>(&ortho_mul_k<NP, TM, BK, KIND>), lds, done);
   if (e != hipSuccess) return e;
   const int64_t tr = l.d.R / TM, tc = l.d.C / TM;
   const dim3 grid((unsigned)(KIND == kStep ? tr * tc : tr * (tr + 1) / 2), (unsigned)l.d.n,
-                  KIND == kGram ? l.split : 1), block(Form<NP, TM>::kThreads);
-  hipLaunchKernelGGL((ortho_mul_k<NP, TM, KIND>), grid, block, lds, st, m);
+                  KIND == kGram ? l.split : 1), block(threads_of(TM));
+  hipLaunchKernelGGL((ortho_mul_k<NP, TM, BK, KIND>), grid, block, lds, st, m);
   return hipSuccess;
 }
 template <int NP, int KIND>
 hipError_t launch_mul(int tile, const Mul& m, const Layout& l, hipStream_t st) {
-  return tile == 256 ? launch_mul<NP, 256, KIND>(m, l, st)
-         : tile == 128 ? launch_mul<NP, 128, KIND>(m, l, st) : launch_mul<NP, 64, KIND>(m, l, st);
+  // Parts of K: 64 wide, or 32 where two parts of a value fill LDS and where K is short, so that four workgroups share a CU
+  // in place of two and the first part is there sooner (us, 64 and 32: bf16 12 x 512 x 1365 358, 340; 6 x 768 x 2048 435, 416;
+  // 8 x 1024 x 4096 1118, 1129; 2 x 2048 x 2048 695, 707)
+  if (tile == 256) return launch_mul<NP, 256, NP == 1 ? 64 : 32, KIND>(m, l, st);
+  if (tile == 64) return launch_mul<NP, 64, 64, KIND>(m, l, st);
+  return NP == 2 || m.K < 1024 ? launch_mul<NP, 128, 32, KIND>(m, l, st) : launch_mul<NP, 128, 64, KIND>(m, l, st);
 }
 
 template <int NP>
