@@ -223,9 +223,12 @@ __global__ __launch_bounds__(threads_of(TM), TM == 256 ? 1 : 2) void ortho_mul_k
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   constexpr int AC = TM / (32 * WC);   // waves along the columns
   const int wr = wave / AC * 32 * WR, wc = wave % AC * 32 * WC, l32 = lane & 31, half = lane >> 5;
-  // neighbours of a run of tiles per XCD share their operands in its L2; runs go down bands of eight rows of tiles
-  const int all = gridDim.x, xcd = blockIdx.x & 7, each = all >> 3, more = all & 7;
-  int id = xcd * each + (xcd < more ? xcd : more) + (blockIdx.x >> 3);
+  // a run of (share of K, matrix, tile) per XCD, so that neighbours share their operands in its L2 and many matrices are each
+  // read by few XCDs; runs go down bands of eight rows of tiles
+  const unsigned lin = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x, xcd = lin & 7;
+  const unsigned all = gridDim.x * gridDim.y * gridDim.z, each = all >> 3, more = all & 7;
+  const unsigned unit0 = xcd * each + (xcd < more ? xcd : more) + (lin >> 3);
+  const int id = unit0 % gridDim.x, i = unit0 / gridDim.x % gridDim.y, z = unit0 / gridDim.x / gridDim.y;
   int ti, tj;
   if (KIND == kStep) {
     const int band = id / (8 * m.cols), in = id - band * 8 * m.cols, high = m.rows - band * 8 < 8 ? m.rows - band * 8 : 8;
@@ -237,13 +240,13 @@ __global__ __launch_bounds__(threads_of(TM), TM == 256 ? 1 : 2) void ortho_mul_k
     while (ti * (ti + 1) / 2 > id) --ti;
     tj = id - ti * (ti + 1) / 2;
   }
-  const int i = blockIdx.y, r0 = ti * TM, c0 = tj * TM, ldk = m.K;
+  const int r0 = ti * TM, c0 = tj * TM, ldk = m.K;
   const bool shares = KIND == kGram && gridDim.z > 1;
   int K = ldk, from = 0;   // the steps of BK that are this workgroup's
   if (shares) {
     const int all_k = ldk / BK;
-    from = (int)((int64_t)all_k * blockIdx.z / gridDim.z) * BK;
-    K = (int)((int64_t)all_k * (blockIdx.z + 1) / gridDim.z) * BK - from;
+    from = (int)((int64_t)all_k * z / gridDim.z) * BK;
+    K = (int)((int64_t)all_k * (z + 1) / gridDim.z) * BK - from;
   }
   const _Float16* P = m.P + (size_t)i * NP * m.p + (size_t)r0 * ldk + from;
   const _Float16* Q = KIND == kStep ? m.Q + (size_t)i * NP * m.q + c0 : m.P + (size_t)i * NP * m.p + (size_t)c0 * ldk + from;
@@ -365,7 +368,7 @@ __global__ __launch_bounds__(threads_of(TM), TM == 256 ? 1 : 2) void ortho_mul_k
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = t[rr * S + c + e] * m.mul;
       if (shares) {
-        Fl4* to = reinterpret_cast<Fl4*>(m.parts + ((size_t)i * gridDim.z + blockIdx.z) * m.o + at);
+        Fl4* to = reinterpret_cast<Fl4*>(m.parts + ((size_t)i * gridDim.z + z) * m.o + at);
         to[0] = Fl4{v[0], v[1], v[2], v[3]};
         to[1] = Fl4{v[4], v[5], v[6], v[7]};
         continue;
