@@ -38,25 +38,41 @@ struct Layout {
 };
 constexpr int kNorm = 256, kFillTiles = 512, kShare = 512;
 int round_up(int v, int to) { return (v + to - 1) / to * to; }
-// The largest tile of which there are enough to fill the chip (256: a workgroup on each CU, of 128 and 64 several), measured
-// (us, tiles of the symmetric products / of X):
-//   bf16 4096 x 8192       64/64 4866, 128/128 3546, 128/256 3319, 256/256 3177
-//   bf16 2048 x 8192       64/64 1198, 64/128 1042, 64/256 1008, 128/256 1047, 256/256 1867
-//   bf16 8 x 1024 x 4096   64/64 1297, 64/128 1178, 128/128 1077, 128/256 1073, 256/256 1398
-//   bf16 2 x 2048 x 2048   64/64 752, 64/128 667, 128/128 671, 64/256 778
-//   bf16 32 x 512 x 512    64/64 355, 64/128 334, 128/128 351, 64/256 377
-//   fp32 4 x 256 x 256     64/64 111, 64/128 147, 128/128 214
-template <class F>
-int tile_for(F tiles, int64_t of256, int64_t of128) {
-  return tiles(256) >= of256 ? 256 : (tiles(128) >= of128 ? 128 : 64);
+// Tiles of X: of 256 where there are enough for the CUs (one takes a CU) and K is long, of 128 where they fill half of the chip's
+// places, and padding adds little; of the symmetric products larger than 64 where the rows are many and the products long.
+// Measured (us, tiles of the symmetric products / of X; * the rule's):
+//                         64/64   64/128  128/128  64/256  128/256  256/256
+//   bf16 4096 x 8192       4872     4121     3566    3884     3337    3158*
+//   bf16 2048 x 8192       1208     1049      957    1009      910*   1265
+//   fp32 2048 x 8192       2769     2433     2140    2295     1992*
+//   bf16 1536 x 6144        613      622      608     621*     599
+//   bf16 8 x 1024 x 4096   1213     1078     1062    1058     1051*   1300
+//   bf16 3000 x 3000       1190     1218     1108    1185     1073*
+//   bf16 3 x 1500 x 1500    623      553      530*    649      626
+//   bf16 2 x 2048 x 2048    748      670      672*    772      778    1073
+//   fp32 2048 x 3000       1243     1183     1118*   1413     1344    1801
+//   fp32 8 x 1024 x 1024    887      810*     832     902      928
+//   bf16 4 x 1024 x 1024    272      269*     317     391      442
+//   bf16 6 x 768 x 2048     394      375*     450     397      472     632
+//   fp32 8 x 700 x 1500     665*     719      753     694      728     998
+//   bf16 100 x 512 x 512    855      790*     806     831      835    1051
+//   bf16 12 x 1365 x 512    287      283*     349     323      410     569
+//   fp32 4 x 256 x 256      103*     142      210     242      308     444
+void pick_tiles(int64_t n, int64_t r, int64_t c, int* half, int* whole) {
+  auto up = [](int64_t v, int64_t t) { return (v + t - 1) / t; };
+  auto tiles = [&](int64_t t) { return n * up(r, t) * up(c, t); };
+  auto below = [&](int64_t t) { return n * up(r, t) * (up(r, t) + 1) / 2; };   // on and below the diagonal
+  auto close = [&](int64_t t) { return 16 * tiles(t) * t * t <= 17 * tiles(64) * 64 * 64; };
+  *whole = r >= 1024 && tiles(256) >= 140 && close(256) ? 256 : (tiles(128) >= 256 && close(128) ? 128 : 64);
+  *half = *whole == 256 && r >= 2048 && below(256) >= 128              ? 256
+          : *whole >= 128 && r >= 1024 && below(128) * (r + c) >= 640000 ? 128 : 64;
 }
 Layout layout_of(const sim_ortho& o) {
   Layout l;
   const bool t = o.M > o.N;
   l.d = OrthoDims{(int)o.n, (int)(t ? o.N : o.M), (int)(t ? o.M : o.N), 0, 0, t};
   const int64_t r = l.d.r, c = l.d.c, n = l.d.n;
-  l.half = tile_for([&](int64_t t) { const int64_t k = (r + t - 1) / t; return n * k * (k + 1) / 2; }, 128, 280);
-  l.whole = tile_for([&](int64_t t) { return n * ((r + t - 1) / t) * ((c + t - 1) / t); }, 200, 256);
+  pick_tiles(n, r, c, &l.half, &l.whole);
   l.parts = o.dtype == SIM_DT_BF16 ? 1 : 2;
   l.d.R = round_up(l.d.r, std::max(l.half, l.whole));
   l.d.C = round_up(l.d.c, l.whole);
