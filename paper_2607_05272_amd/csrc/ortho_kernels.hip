@@ -133,8 +133,8 @@ __device__ __forceinline__ void split(float x, _Float16 (&p)[2]) {
 }
 __device__ __forceinline__ void split(float x, _Float16 (&p)[1]) { p[0] = (_Float16)x; }
 
-// X's parts, padding included: tiles of 64 x 64, read along U's faster axis and written along X's rows, an element a thread at
-// once whatever the strides: bf16 4096 x 8192 64 us (2.1 TB/s), 2% of its call.
+// X's parts, padding included: tiles of 64 x 64, read along U's faster axis and written along X's rows, eight elements a thread at
+// once (one by one where they do not lie side by side, and at the edges). bf16 4096 x 8192 38 us (3.5 TB/s; one by one 65).
 template <class E, int NP>
 __global__ __launch_bounds__(256) void ortho_load_k(const void* u0, View v, OrthoDims d, const double* part, int parts,
                                                     double eps, _Float16* x) {
@@ -148,20 +148,42 @@ __global__ __launch_bounds__(256) void ortho_load_k(const void* u0, View v, Orth
   const double f = s == 0.0 ? 0.0 : (s - s == 0.0 ? (double)kUp / (sqrt(s) + eps) : __longlong_as_double(0x7FF8000000000000ll));
   const T* u = static_cast<const T*>(u0) + blockIdx.y * v.si;
   const bool rows = v.by_rows != d.turned;   // X's rows lie along the slow axis
-  for (int i = threadIdx.x; i < 64 * 64; i += 256) {
-    const int a = i >> 6, b = i & 63, r = r0 + (rows ? a : b), c = c0 + (rows ? b : a);
-    float w = 0.0f;
-    if (r < d.r && c < d.c) w = (float)((double)(float)u[(rows ? r : c) * v.slow + (rows ? c : r) * v.fast] * f);
-    t[rows ? a : b][rows ? b : a] = w;
+  const int s0 = rows ? r0 : c0, f0 = rows ? c0 : r0;
+  const bool whole = v.fast == 1 && s0 + 64 <= v.rows && f0 + 64 <= v.cols;
+  for (int k = threadIdx.x; k < 64 * 8; k += 256) {
+    typedef T Raw __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    typedef T Val __attribute__((ext_vector_type(8)));
+    const int sl = s0 + (k >> 3), fa = f0 + (k & 7) * 8, i = k >> 3, j = (k & 7) * 8;
+    float w[8];
+    if (whole) {
+      const Val y = __builtin_bit_cast(Val, *reinterpret_cast<const Raw*>(u + sl * v.slow + fa));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = (float)((double)(float)y[e] * f);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        w[e] = 0.0f;
+        if (sl < v.rows && fa + e < v.cols) w[e] = (float)((double)(float)u[sl * v.slow + (fa + e) * v.fast] * f);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[rows ? i : j + e][rows ? j + e : i] = w[e];
   }
   __syncthreads();
   const size_t cells = (size_t)d.R * d.C;
-  for (int i = threadIdx.x; i < 64 * 64; i += 256) {
-    _Float16 p[NP];
-    split(t[i >> 6][i & 63], p);
+  for (int k = threadIdx.x; k < 64 * 8; k += 256) {
+    const int i = k >> 3, j = (k & 7) * 8;
+    H8 w[NP];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      _Float16 p[NP];
+      split(t[i][j + e], p);
+#pragma unroll
+      for (int q = 0; q < NP; ++q) w[q][e] = p[q];
+    }
 #pragma unroll
     for (int q = 0; q < NP; ++q)
-      x[((size_t)blockIdx.y * NP + q) * cells + (size_t)(r0 + (i >> 6)) * d.C + c0 + (i & 63)] = p[q];
+      *reinterpret_cast<H8*>(x + ((size_t)blockIdx.y * NP + q) * cells + (size_t)(r0 + i) * d.C + c0 + j) = w[q];
   }
 }
 
@@ -206,7 +228,7 @@ __device__ __forceinline__ H4 read_turned(const _Float16* p) {
 // different banks. Tiles of 256 are shared by eight waves, 128 x 64 each (of 64 x 64 LDS feeds the matrix units too slowly:
 // it gives 128 bytes a cycle, and a wave needs 128 of them per 8 cycles of MFMA), smaller ones by four. Large ones are bound by
 // the matrix units (bf16 4096 x 8192: kStep 284 us, 968 TFLOP/s of the 1063 that a large library product reaches; kGram 187, 780
-// of the tiles that it forms; kPoly 131, 560: 136 tiles on 256 CUs), small ones by a tile's chain (fp32 4 x 256 x 256: 6.5 us each).
+// of the tiles that it forms; kPoly 131, 560: 136 tiles on 256 CUs), small ones by a tile's chain (fp32 4 x 256 x 256: 6.4 us each).
 enum { kGram = 0, kPoly = 1, kStep = 2 };
 struct Mul {
   const _Float16 *P, *Q;
@@ -446,7 +468,7 @@ __global__ __launch_bounds__(threads_of(TM), TM == 256 ? 1 : 2) void ortho_mul_k
 }
 
 // The shares' sums, in order, to A's parts: 16 x 64 at once, on and below the diagonal, and turned. Bound by HBM: three shares
-// of 4096 x 4096, 141 MB, 25 us.
+// of 4096 x 4096, 141 MB, 28 us.
 template <int NP>
 __global__ __launch_bounds__(256) void ortho_sum_k(const float* in, int shares, _Float16* out, int R, int half) {
   __shared__ float t[16][65];
