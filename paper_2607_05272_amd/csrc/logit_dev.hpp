@@ -661,7 +661,7 @@ __global__ __launch_bounds__(64 * W * GR) void loss_cols_k(typename OP::Args s, 
   typedef T Raw __attribute__((ext_vector_type(2), aligned(sizeof(T))));
   typedef T Val __attribute__((ext_vector_type(2)));
   typedef uint8_t Bytes __attribute__((ext_vector_type(2), aligned(1)));
-  struct Closed { float m, alpha, beta, delta; int act; };   // act -2: the sample gives nothing
+  struct Closed { float m, alpha, beta, delta; int act; };   // act: a column, -1 for none of them, -2: the sample gives nothing
   constexpr bool kShare = W > 1;
   // parts joined at once: two, or they and 24 logits spill (policy 40000 x 300 columns 40 -> 35 us); with 12
   // all of them (balance 30000 x 162 22.3 us, two at a time 23.2)
@@ -768,7 +768,8 @@ __global__ __launch_bounds__(64 * W * GR) void loss_cols_k(typename OP::Args s, 
       RowOut o{0.0f, 0.0f, 0.0f};
       const bool gives = on[v] && OP::close(s, t, rows[v], whole, taken[v], true, sums, o);
       if (!gives) OP::shut(s, t);
-      return Closed{whole.m == -INFINITY ? 0.0f : whole.m, o.alpha, o.beta, o.delta, gives ? (int)rows[v].act : -2};
+      const int column = rows[v].act >= 0 && rows[v].act < A ? (int)rows[v].act : -1;
+      return Closed{whole.m == -INFINITY ? 0.0f : whole.m, o.alpha, o.beta, o.delta, gives ? column : -2};
     };
     if constexpr (kShare) {
       static_assert(W >= 2, "a thread for each sample");
