@@ -646,11 +646,11 @@ typedef struct sim_ortho {
 /* X = U / (|U|_F + eps), then `steps` times, with A = X X^T (X^T X for M > N, which comes to the same),
  *   X = a X + (b A + c A A) X
  * and out = scale X. The norm is summed in fp64, sums of products in fp32; between products X, A and
- * b A + c A A are held as fp16 parts of the value times 2^10: one (11 bits) for bf16, whose own rounding is
- * coarser, two (22 bits) otherwise, in steps of 2^-34 at the finest (an update whose norm lies far below
- * eps keeps fewer bits). So singular values, and A's and the polynomial's, must stay below 60 (with the
- * usual coefficients they stay below 4). U and out may have any strides and be the same memory; a matrix
- * of zeros gives zeros, one that holds an infinity or NaN gives NaN.                         */
+ * b A + c A A are held as two fp16 parts (22 bits) of the value times 2^10, in steps of 2^-34 at the
+ * finest (an update whose norm lies far below eps keeps fewer bits). So singular values, and A's and the
+ * polynomial's, must stay below 60 (with the usual coefficients they stay below 4). U and out may have
+ * any strides and be the same memory; a matrix of zeros gives zeros, one that holds an infinity or NaN
+ * gives NaN.                                                                               */
 int orthogonalize_work(const sim_ortho* c, size_t* bytes);
 int orthogonalize(sim_ctx* ctx, const sim_ortho* c, const sim_mats* update, const sim_mats* out,
                   void* d_work, size_t work_bytes);
