@@ -19,6 +19,7 @@ def _p(t):
 
 _FLOAT = {torch.float64: 0, torch.float32: 1, torch.bfloat16: 2, torch.float16: 3}
 _INT = {torch.uint8: 0, torch.int32: 1, torch.int64: 2}
+_KEEP = 32 << 20   # bytes of an operator's work memory that a context holds on to, per thread
 
 
 def _a(t):
@@ -362,14 +363,16 @@ class Sim:
         from call to call, per thread, where calls follow one another on the context's stream;
         a captured call, whose replays do not, gets its own, and so does one from another
         stream, whose allocations torch orders by that stream, or made while another device is the
-        current one, whose capture alone torch tells of."""
+        current one, whose capture alone torch tells of, or that needs more than _KEEP bytes: those go
+        back to torch after the call (a context would hold them until it is closed; to be given them
+        again takes microseconds, where such a call's kernels run tens of them or more)."""
         sizes_p, need = C.byref(sizes), C.c_size_t()
         L.check(getattr(self.lib, name + "_work")(sizes_p, C.byref(need)), name)
         work, need = None, need.value
         same = torch._C._cuda_getCurrentRawStream(self._index) == self._raw_stream
         if need:
             work = getattr(self._work, "memory", None)
-            if (not same or torch.cuda.current_device() != self._index
+            if (not same or need > _KEEP or torch.cuda.current_device() != self._index
                     or torch.cuda.is_current_stream_capturing()):
                 work = torch.empty(need, dtype=torch.uint8, device=self._device)
             elif work is None or work.numel() < need:
