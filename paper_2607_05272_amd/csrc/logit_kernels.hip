@@ -21,7 +21,7 @@ __device__ __forceinline__ float grow(float d, float& rest) {
 
 // ---- the two losses ----------------------------------------------------------------------------
 struct PolicyOp {
-  static constexpr bool kBal = false, kSums = true;
+  static constexpr bool kBal = false, kSums = true, kClosed = false;
   static constexpr int kTargets = 1;
   typedef PolicyLossArgs Args;
   struct Row { float w, adv, old, ref; int64_t act; };
@@ -122,7 +122,7 @@ __device__ void fill_targets(const BalanceArgs& s, int nb, float* f);
 __device__ float target(const BalanceArgs& s, const float* f, int j);
 
 struct BalanceOp {
-  static constexpr bool kBal = true, kSums = true;
+  static constexpr bool kBal = true, kSums = true, kClosed = false;
   static constexpr int kTargets = kMaxTargets;
   typedef BalanceArgs Args;
   struct Row { int64_t act; };

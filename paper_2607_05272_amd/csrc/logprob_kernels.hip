@@ -10,7 +10,7 @@ namespace bsim {
 namespace {
 
 struct LogprobOp {
-  static constexpr bool kBal = false, kSums = false;
+  static constexpr bool kBal = false, kSums = false, kClosed = true;
   static constexpr int kTargets = 1;
   typedef LogprobArgs Args;
   struct Row { float g, h; int64_t act; };
@@ -34,7 +34,7 @@ struct LogprobOp {
     const bool none = r.act < 0 || r.act >= s.c.A;
     if (first && none && r.act != -1) atomicOr(s.err, ERR_ACTION);
     if (p.m == -INFINITY) return false;          // no allowed column
-    const float logS = log_of(p.S), rS = __builtin_amdgcn_rcpf(p.S);
+    const float logS = p.m == INFINITY ? NAN : log_of(p.S), rS = __builtin_amdgcn_rcpf(p.S);
     const float H = fmaf(-p.X, rS, logS);
     if (first) {
       if (s.logp) s.logp[n] = none ? 0.0f : (la == -INFINITY ? la : (la - p.m) - logS);
