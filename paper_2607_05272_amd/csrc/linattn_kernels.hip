@@ -710,36 +710,49 @@ constexpr int run_steps(int dtype, int DQ) {   // of a run: as many as LDS holds
 }
 // What a workgroup takes: columns of a state (128 by eight waves; 64 by four, or by eight that halve its rows), and a sequence's
 // steps or a segment of them, at the cost of reading k and v once more. By the sequences and heads there are and what their
-// registers leave room for, measured (us; bf16 but where stated; segments: of all heads together):
-//   8 x 2048 x 16 heads x 128 (ragged)   64 148, halves 108, 128 154, halves in two segments 177
-//   32 x 2048 x 16 x 128                 64 393, halves 435, 128 339
-//   1 x 4096 x 16 x 128                  128 in 256 segments 54, halves 58, whole 290
-//   4 x 2048 x 16 x 128 fp16             128 in 256 segments 112, halves 140, whole 218
-//   4 x 1024 x 16 x 128 fp32             128 in 256 segments 92, halves 120, whole 148
-//   16 x 2048 x 16 x 64                  64 102, halves 85
-//   1 x 32768 x 8 x 64, a training step  64 in 512 segments 266, in 256 333, halves 319 (with the states behind
-//                                        dk and dv formed twice; once: 243)
-//   16 x 385 x 6 x 72 and 80 fp32, same  halves 242, 128 316, halves in segments 335
-//   2 x 2048 x 16 x 256                  halves 161
+// registers leave room for. Measured on either side of each border (us; bf16 but where stated; segs: in segments of all heads
+// together, as many workgroups as stated; heads of B x H):
+//   Dv > 64: segments of 128 columns for few heads and many steps, halves while one round of workgroups (two a head) fits
+//   the CUs, 128 columns beyond
+//     T 2048, 128 x 128, heads 32 / 64 / 80 / 96 / 112 / 128 / 192 / 240 / 256 / 384
+//       128 in 256 segs    58    89   110   141   148   154
+//       halves            113   113   113   115   114   115   223   223   224   338
+//       128               158   157   157   158   159   163   168   171   171   331
+//     T 512, heads 128 / 144, fp32: halves 63 / 117, 128 83 / 84; fp16 46 / 87, 62 / 63; bf16 36 / 65, 47 / 48
+//     64 heads, T 300 / 512 / 768 / 1024 fp32: 128 in segs 51 / 57 / 60 / 88, halves 26 / 34 / 47 / 109; a training step
+//     208 / 234 / 246, 123 / 168 / 235 (fp32 of 768 336, 378)
+//   Dq > 64 >= Dv, 128 x 64: halves, in segs of 256 for few heads and many steps
+//     64 heads, T 512 / 1024: in segs 39 / 41, whole 33 / 59; 112 heads, T 1024: 63, 59
+//   64 x 64: segments of 64 columns for few heads and many steps, then halves for one round, then 64 columns, but not in
+//   fp32, of which no second workgroup fits a CU
+//     T 2048, heads 64 / 112 / 128 / 192 / 256: 64 in 512 segs 44 / 65 / 67 / 106 / 112, halves 85 / 86 / 86 / 86 / 87; fp32
+//     T 1024, heads 64 / 112 / 128: 54 / 94 / 95, 75 / 76 / 76
+//     T 700, heads 256 / 272, halves and 64: bf16 36 / 67, 44 / 53; fp16 47 / 89, 55 / 67; fp32 60 / 111, 75 / 142
+//     fp32 T 400, 384 / 768 heads: halves 76 / 118, 64 95 / 149;  bf16 T 2048, 368 heads: 167, 130
+//     64 heads, T 512 / 768: in segs 34 / 32, halves 26 / 35; training 137 / 132, 132 / 176
+//   Dq > 128: halves, in segs of 256; 32 heads of 256 x 256, T 512: in segs 73, whole 48; 768 fp32: 134, 130
 struct Plan { int columns, halves, segs; };
-constexpr int kLeast = 256;   // steps of a segment
-Plan plan_of(int64_t B, int64_t T, int H, int Dq, int Dv) {
+constexpr int kLeast = 256;       // steps of a segment
+constexpr int kSegsFrom = 512;    // steps beyond which there are segments: two of them cost more than they give
+Plan plan_of(int64_t B, int64_t T, int H, int Dq, int Dv, int dtype) {
   const int64_t heads = B * H;
   Plan p{64, 1, 1};
   if (T <= kFew || heads == 0) return p;
   int fill = 0;   // workgroups that are resident at once: segments make no more
   if (Dq > 128) { p.halves = 2; fill = 256; }
-  else if (Dv > 64 && (heads < 96 || heads >= 256)) { p.columns = 128; fill = heads < 96 ? 256 : 0; }
+  else if (Dv > 64 && heads > 128) p.columns = 128;
+  else if (Dv > 64 && heads < 96 && T > kSegsFrom) { p.columns = 128; fill = 256; }
   else if (Dv > 64) p.halves = 2;
   else if (Dq > 64) { p.halves = 2; fill = heads < 128 ? 256 : 0; }
-  else if (heads < 128) fill = 512;
-  else if (heads < 384) p.halves = 2;
+  else if (heads < 128 && T > kSegsFrom) fill = 512;
+  else if (heads <= 256 || dtype == SIM_DT_F32) p.halves = 2;
+  if (T <= kSegsFrom) return p;
   const int64_t groups = heads * ((Dv + p.columns - 1) / p.columns);
   p.segs = (int)std::max<int64_t>(1, std::min<int64_t>((T + kLeast - 1) / kLeast, fill / groups));
   return p;
 }
-size_t parts_bytes(int64_t B, int64_t T, int H, int Dq, int Dv) {
-  const int g = plan_of(B, T, H, Dq, Dv).segs;
+size_t parts_bytes(int64_t B, int64_t T, int H, int Dq, int Dv, int dtype) {
+  const int g = plan_of(B, T, H, Dq, Dv, dtype).segs;
   return g > 1 ? (size_t)B * H * g * Dq * Dv * sizeof(float) : 0;
 }
 
@@ -775,7 +788,7 @@ hipError_t launch_run(AttnRun r, int64_t B, float* parts, int what, hipStream_t 
     else hipLaunchKernelGGL((attn_step_k<E, 16>), grid, block, 0, st, r);
     return hipSuccess;
   }
-  const Plan plan = plan_of(B, r.T, r.H, r.Dq, r.Dv);
+  const Plan plan = plan_of(B, r.T, r.H, r.Dq, r.Dv, dt);
   r.segs = plan.segs;
   r.seg = r.T;
   if (r.segs > 1) {   // whole runs
@@ -845,9 +858,9 @@ hipError_t launch_typed(const AttnArgs& a, bool grad, hipStream_t st) {
   dims(rv, c.Dk, c.Dv, false);
   // Both go by the same states, each other's turned: in segments they are formed once, for either alone too, so that
   // a gradient is the same whichever others are wanted.
-  const int segs = plan_of(c.B, c.T, c.H, c.Dv, c.Dk).segs;
+  const int segs = plan_of(c.B, c.T, c.H, c.Dv, c.Dk, c.dtype).segs;
   int what = kWhole;
-  if (segs > 1 && segs == plan_of(c.B, c.T, c.H, c.Dk, c.Dv).segs && (a.dk.data || a.dv.data || a.state)) {
+  if (segs > 1 && segs == plan_of(c.B, c.T, c.H, c.Dk, c.Dv, c.dtype).segs && (a.dk.data || a.dv.data || a.state)) {
     AttnRun r = rk;
     r.state = a.state;
     if ((e = launch_run<E>(r, c.B, parts, kStates, st)) != hipSuccess) return e;
@@ -880,8 +893,8 @@ hipError_t launch_typed(const AttnArgs& a, bool grad, hipStream_t st) {
 }  // namespace
 
 size_t attn_work_bytes(const sim_linear_attn& c, bool grad) {
-  size_t parts = parts_bytes(c.B, c.T, c.H, c.Dk, c.Dv);
-  if (grad) parts = std::max(parts, parts_bytes(c.B, c.T, c.H, c.Dv, c.Dk));
+  size_t parts = parts_bytes(c.B, c.T, c.H, c.Dk, c.Dv, c.dtype);
+  if (grad) parts = std::max(parts, parts_bytes(c.B, c.T, c.H, c.Dv, c.Dk, c.dtype));
   return share_cells(c, grad) * sizeof(float) + parts;
 }
 
