@@ -235,8 +235,10 @@ __device__ __forceinline__ uint64_t key_at(uint64_t k, int lane) {
 // Longer rows: a workgroup takes a row or one of gridDim.y parts of it, its waves every fourth stretch of 512 logits. A wave
 // keeps its 64 largest keys, one a lane, and collects in LDS what could be among the row's largest `top`: logits not
 // below the least of the `top` that any wave has kept (at first, of its lanes' largest ones). 64 of them are sorted and
-// joined at once, by moves within the vector unit: after the first stretches few logits are collected at all. Bound by HBM
-// for many rows, and for few by the chains of that: bf16 32 x 131072, twenty alternatives, 15.8 us and 4.0 for the parts, for
+// joined at once, by moves within the vector unit: after the first stretches few logits are collected at all. Many rows
+// are bound by what is done with each logit and by loads that a wave waits for two chunks at a time, not by HBM: twenty
+// alternatives of 4096 x 50257 take 193 us in bf16 (2.1 TB/s) as in fp32 (4.3 TB/s), five of fp32 1000 x 20000 34 us (2.4 TB/s).
+// Few rows are bound by the chains of all that: bf16 32 x 131072, twenty alternatives, 15.8 us and 4.0 for the parts, for
 // 1.7 of HBM.
 constexpr int kLong = 256, kLongWaves = kLong / 64;
 struct LongPart {
@@ -489,7 +491,7 @@ int parts_of(int64_t N, int A) {
 
 template <class E, bool COLS>
 void launch_short(const LogprobArgs& a, hipStream_t st) {
-  // 32 samples turned at once: of 64 a wave's passes over them follow each other (16384 x 96 14.4 us against 18.6)
+  // 32 samples turned at once: of 64 a wave's passes over them follow each other (16384 x 96 12.2 us against 18.6)
   const int A = a.c.A, S = A <= 480 ? 32 : 16;
   const int per = COLS ? S : (A <= 256 ? kGroups / 16 : kGroups / 64);
   const dim3 grid(blocks_for(a.c.N, per, 1 << 16)), block(kGroups);
